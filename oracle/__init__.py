@@ -28,3 +28,4 @@ from .moe import route_topk, routing_tables, moe_ffn  # noqa: F401
 from .pipeline import af_decode_layer_steps, af_layer_steps  # noqa: F401
 from .block import kv_append, kv_write, linear, moe_block, rmsnorm  # noqa: F401
 from .prefill import attention_prefill  # noqa: F401
+from . import longctx  # noqa: F401

@@ -18,6 +18,7 @@ import torch
 _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libaflex.so")
 HEADER = os.path.join(os.path.dirname(_PKG), "include", "aflex.h")
+LONGCTX_HEADER = os.path.join(os.path.dirname(_PKG), "include", "aflex_longctx.h")
 
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_ALIGNMENT, ERR_WORKSPACE, ERR_HIP = range(6)
 
@@ -74,6 +75,33 @@ class LayerArgs(ctypes.Structure):
                 ("x_in", _p), ("norm_weight", _p), ("router_weight", _p), ("eps", ctypes.c_float)]
 
 
+class RopeArgs(ctypes.Structure):
+    _fields_ = [("q", _p), ("k_new", _p), ("v_new", _p), ("rope", _p), ("positions", _p), ("cu_seqlens", _p),
+                ("q_out", _p), ("k_cache", _p), ("v_cache", _p), ("block_keys", _p), ("block_exp", _p),
+                ("block_table", _p), ("context_lens", _p),
+                ("B", _i), ("T", _i), ("Hq", _i), ("Hkv", _i), ("D", _i), ("rotary_dim", _i),
+                ("interleaved", _i), ("rope_len", _i), ("max_seqlen", _i), ("block_size", _i),
+                ("max_blocks_per_seq", _i), ("num_blocks", _i), ("q_stride", _i), ("k_stride", _i), ("v_stride", _i)]
+
+
+class BlockSummaryArgs(ctypes.Structure):
+    _fields_ = [("k_cache", _p), ("block_keys", _p), ("block_exp", _p), ("block_table", _p), ("context_lens", _p),
+                ("B", _i), ("Hkv", _i), ("D", _i), ("block_size", _i), ("max_blocks_per_seq", _i),
+                ("num_blocks", _i), ("max_context_len", _i)]
+
+
+class BlockSelectArgs(ctypes.Structure):
+    _fields_ = [("q", _p), ("block_keys", _p), ("block_exp", _p), ("block_table", _p), ("context_lens", _p),
+                ("selected", _p),
+                ("B", _i), ("Hq", _i), ("Hkv", _i), ("D", _i), ("block_size", _i), ("max_blocks_per_seq", _i),
+                ("num_blocks", _i), ("max_context_len", _i), ("top_blocks", _i), ("sink_blocks", _i),
+                ("recent_blocks", _i)]
+
+
+class AttnSparseArgs(ctypes.Structure):
+    _fields_ = [("attn", AttnArgs), ("selected", _p), ("top_blocks", _i)]
+
+
 class AflexError(RuntimeError):
     def __init__(self, status: int, message: str):
         super().__init__(f"aflex status {status}: {message}")
@@ -84,9 +112,9 @@ _lib = None
 _SZ = ctypes.POINTER(ctypes.c_size_t)
 
 
-def exported_names():
-    """Function names declared in include/aflex.h."""
-    with open(HEADER) as f:
+def exported_names(header=HEADER):
+    """Function names declared in include/aflex.h (or another header)."""
+    with open(header) as f:
         text = f.read()
     return sorted(set(re.findall(r"^\s*(?:const\s+)?\w+\s*\*?\s*(aflex_\w+)\s*\(", text, re.M)))
 
@@ -122,6 +150,13 @@ def load():
         "aflex_kv_write": [ctypes.POINTER(KvWriteArgs), _p],
         "aflex_pool_streams_create": [ctypes.c_int32, ctypes.POINTER(_p), ctypes.POINTER(_p)],
         "aflex_pool_streams_destroy": [_p, _p],
+        "aflex_rope_append": [ctypes.POINTER(RopeArgs), _p],
+        "aflex_rope_write": [ctypes.POINTER(RopeArgs), _p],
+        "aflex_block_summary": [ctypes.POINTER(BlockSummaryArgs), _p],
+        "aflex_block_select_workspace": [ctypes.POINTER(BlockSelectArgs), _SZ],
+        "aflex_block_select": [ctypes.POINTER(BlockSelectArgs), _p, ctypes.c_size_t, _p],
+        "aflex_attn_sparse_decode_workspace": [ctypes.POINTER(AttnSparseArgs), _SZ],
+        "aflex_attn_sparse_decode": [ctypes.POINTER(AttnSparseArgs), _p, ctypes.c_size_t, _p],
     }
     for name, args in sig.items():
         fn = getattr(lib, name)
@@ -512,3 +547,238 @@ def af_layer_step(a, w, layer, k: int, mb_sizes, L: int = 1, y=None, stream_a=No
     if join:
         torch.cuda.current_stream(a.q.device).wait_stream(stream_f)
     return y
+
+
+# --------------------------------------------------------------------------
+# Long-context operators (include/aflex_longctx.h). These check what the C
+# interface cannot see (types, sizes, devices, strides), run on the device of
+# their tensors, and keep a default workspace per stream; outputs that they
+# allocate belong to the stream they run on.
+class BlockSummary:
+    """Key summaries of a cache's blocks: ``keys`` int8 [num_blocks, Hkv, D] and
+    ``exp`` int8 [num_blocks, Hkv] (mean key about keys * 2^exp)."""
+
+    def __init__(self, keys, exp):
+        self.keys, self.exp = keys, exp
+
+    @classmethod
+    def of(cls, a):
+        """Zeroed summaries for a's pools."""
+        d = a.k_cache.device
+        return cls(torch.zeros(a.num_blocks, a.Hkv, a.D, dtype=torch.int8, device=d),
+                   torch.zeros(a.num_blocks, a.Hkv, dtype=torch.int8, device=d))
+
+
+def rope_table(positions: int, rotary_dim: int, base: float = 10000.0, device="cpu"):
+    """fp32 [positions, rotary_dim] for rope_append / rope_write: cosines, then sines,
+    of p * base^(-2 i / rotary_dim), the angles in float64."""
+    f = base ** (-torch.arange(0, rotary_dim, 2, dtype=torch.float64) / rotary_dim)
+    ang = torch.arange(positions, dtype=torch.float64)[:, None] * f
+    return torch.cat([ang.cos(), ang.sin()], 1).float().to(device)
+
+
+def _want(t, name, numel, dtype, dev):
+    """A dense tensor of the cache's device, of this many elements."""
+    if t.dtype is not dtype or t.numel() != numel or not t.is_contiguous() or t.get_device() != dev:
+        raise ValueError(f"{name}: expected {numel} dense {dtype} elements on cuda:{dev}, but got {tuple(t.shape)} "
+                         f"{t.dtype} on {t.device}, strides {t.stride()}")
+
+
+def _want_cache(a, dev, pools=("k_cache", "v_cache")):
+    for name in pools:
+        _want(getattr(a, name), name, a.num_blocks * a.Hkv * 16 * a.D, torch.bfloat16, dev)
+    _want(a.block_table, "block_table", a.B * a.max_blocks, torch.int32, dev)
+    _want(a.context_lens, "context_lens", a.B, torch.int32, dev)
+
+
+def _want_summary(a, s, dev):
+    _want(s.keys, "summary keys", a.num_blocks * a.Hkv * a.D, torch.int8, dev)
+    _want(s.exp, "summary exponents", a.num_blocks * a.Hkv, torch.int8, dev)
+
+
+def _row_stride(t, name, T, H, D, dev):
+    """Elements between the token rows of t [T, H, D], whose heads are dense."""
+    st = t.stride()
+    if (t.dtype is not torch.bfloat16 or t.shape != (T, H, D) or t.get_device() != dev
+            or st[2] != 1 or (st[1] != D and H > 1) or (T > 1 and st[0] < H * D)):
+        raise ValueError(f"{name}: expected bf16 [{T}, {H}, {D}] on cuda:{dev} with dense, disjoint rows, but got "
+                         f"{tuple(t.shape)} {t.dtype} on {t.device}, strides {st}")
+    return st[0] if T > 1 else 0
+
+
+def _device_of(t):
+    dev = t.get_device()
+    if dev < 0:
+        _need_gpu(t.device)
+    return dev
+
+
+class _On:
+    """The tensors' device as the current one (nothing to do where it is)."""
+
+    def __init__(self, dev):
+        self.dev = dev
+
+    def __enter__(self):
+        self.was = torch._C._cuda_getDevice()
+        if self.was != self.dev:
+            torch._C._cuda_setDevice(self.dev)
+
+    def __exit__(self, *exc):
+        if self.was != self.dev:
+            torch._C._cuda_setDevice(self.was)
+
+
+def _empty(stream, dev, *shape, dtype=torch.bfloat16):
+    if stream is None:
+        return torch.empty(*shape, dtype=dtype, device=f"cuda:{dev}")
+    with torch.cuda.stream(stream):
+        return torch.empty(*shape, dtype=dtype, device=f"cuda:{dev}")
+
+
+def _run_own_ws(name, args, ws, stream):
+    """Call an entry point with a workspace on the current device. The default
+    one belongs to the (device, stream) that the call runs on, so calls on two
+    streams do not share it; while a graph is captured the call gets one of the
+    graph's own memory."""
+    ref, handle = ctypes.byref(args), _stream(stream)
+    dev = torch._C._cuda_getDevice()
+    if ws is None:
+        if torch.cuda.is_current_stream_capturing():
+            ws = Workspace()
+        else:
+            ws = _default_ws.setdefault((name, dev, handle), Workspace())
+    fn = getattr(_lib, name)
+    if ws.buf is not None and ws.buf.get_device() == dev:
+        status = fn(ref, ws.buf.data_ptr(), ws.buf.numel(), handle)
+        if status != ERR_WORKSPACE:
+            return _check(status)
+    n = ctypes.c_size_t()
+    _check(getattr(_lib, name + "_workspace")(ref, ctypes.byref(n)))
+    if stream is None:
+        buf = ws.get(n.value, f"cuda:{dev}")
+    else:
+        with torch.cuda.stream(stream):
+            buf = ws.get(n.value, f"cuda:{dev}")
+    _check(fn(ref, buf.data_ptr(), buf.numel(), handle))
+
+
+def _rope(name, a, q, k_new, v_new, rope, cu_seqlens, max_seqlen, interleaved, positions, summary, q_out, stream):
+    lib = load()
+    dev = _device_of(q)
+    T = q.shape[0]
+    _want_cache(a, dev)
+    qs = _row_stride(q, "q", T, a.Hq, a.D, dev)
+    ks = _row_stride(k_new, "k_new", T, a.Hkv, a.D, dev)
+    vs = _row_stride(v_new, "v_new", T, a.Hkv, a.D, dev)
+    rot = 0
+    if rope is not None:
+        rot = rope.shape[1]
+        _want(rope, "rope", rope.shape[0] * rot, torch.float32, dev)
+    if positions is not None:
+        _want(positions, "positions", T, torch.int32, dev)
+    if cu_seqlens is not None:
+        _want(cu_seqlens, "cu_seqlens", a.B + 1, torch.int32, dev)
+    elif T != a.B:
+        raise ValueError(f"q: expected one row for each of {a.B} sequences, but got {T}")
+    keys = exp = None
+    if summary is not None:
+        _want_summary(a, summary, dev)
+        keys, exp = summary.keys.data_ptr(), summary.exp.data_ptr()
+    with _On(dev):
+        if q_out is None:
+            q_out = _empty(stream, dev, T, a.Hq, a.D)
+        else:
+            _want(q_out, "q_out", T * a.Hq * a.D, torch.bfloat16, dev)
+        args = RopeArgs(q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), _ptr(rope), _ptr(positions),
+                        _ptr(cu_seqlens), q_out.data_ptr(), a.k_cache.data_ptr(), a.v_cache.data_ptr(), keys, exp,
+                        a.block_table.data_ptr(), a.context_lens.data_ptr(), a.B, T, a.Hq, a.Hkv, a.D, rot,
+                        int(interleaved), 0 if rope is None else rope.shape[0], max_seqlen, a.block_size,
+                        a.max_blocks, a.num_blocks, qs, ks, vs)
+        _check(getattr(lib, name)(ctypes.byref(args), _stream(stream)))
+    return q_out
+
+
+def rope_append(a, q, k_new, v_new, rope, interleaved: bool = False, positions=None, summary=None, q_out=None,
+                stream=None):
+    """Rotate each sequence's new query and key, and append key and value to a's paged pools in place
+    (position ctx-1, or row ``positions[b]`` of ``rope``; rope=None: no rotation). q [B, Hq, D], k_new and
+    v_new [B, Hkv, D] may be slices of one projection's output. With ``summary`` (BlockSummary) the blocks
+    that get full are summarised. Returns the rotated queries [B, Hq, D]."""
+    return _rope("aflex_rope_append", a, q, k_new, v_new, rope, None, 0, interleaved, positions, summary, q_out,
+                 stream)
+
+
+def rope_write(a, q, k_new, v_new, cu_seqlens, rope, max_seqlen=None, interleaved: bool = False, positions=None,
+               summary=None, q_out=None, stream=None):
+    """rope_append for packed new tokens: rows cu[b] .. cu[b+1]-1 are the newest of sequence b's context.
+    ``max_seqlen`` bounds the prompts' lengths (None: read from cu_seqlens, which waits for the device)."""
+    if max_seqlen is None:
+        c = cu_seqlens.cpu()
+        max_seqlen = int((c[1:] - c[:-1]).max()) if c.numel() > 1 else 0
+    return _rope("aflex_rope_write", a, q, k_new, v_new, rope, cu_seqlens, max_seqlen, interleaved, positions,
+                 summary, q_out, stream)
+
+
+def block_summary(a, summary=None, stream=None):
+    """Summaries of every full block of a's sequences (for caches written without them), in place."""
+    lib = load()
+    dev = _device_of(a.k_cache)
+    _want_cache(a, dev, ("k_cache",))
+    with _On(dev):
+        if summary is None:
+            if stream is None:
+                summary = BlockSummary.of(a)
+            else:
+                with torch.cuda.stream(stream):
+                    summary = BlockSummary.of(a)
+        _want_summary(a, summary, dev)
+        args = BlockSummaryArgs(a.k_cache.data_ptr(), summary.keys.data_ptr(), summary.exp.data_ptr(),
+                                a.block_table.data_ptr(), a.context_lens.data_ptr(), a.B, a.Hkv, a.D, a.block_size,
+                                a.max_blocks, a.num_blocks, a.max_context_len)
+        _check(lib.aflex_block_summary(ctypes.byref(args), _stream(stream)))
+    return summary
+
+
+def block_select(a, q, summary, top_blocks: int, sink_blocks: int = 1, recent_blocks: int = 1, out=None, stream=None,
+                 ws=None):
+    """The ``top_blocks`` cache blocks that each (sequence, kv head) attends for the rotated queries q [B, Hq, D]:
+    the first ``sink_blocks``, the last ``recent_blocks`` and the best scoring others. int32 [B, Hkv, top_blocks],
+    ascending, -1 behind a shorter list."""
+    load()
+    dev = _device_of(q)
+    _want_cache(a, dev, ())
+    _want_summary(a, summary, dev)
+    _want(q, "q", a.B * a.Hq * a.D, torch.bfloat16, dev)
+    with _On(dev):
+        if out is None:
+            out = _empty(stream, dev, a.B, a.Hkv, max(top_blocks, 0), dtype=torch.int32)
+        else:
+            _want(out, "out", a.B * a.Hkv * top_blocks, torch.int32, dev)
+        args = BlockSelectArgs(q.data_ptr(), summary.keys.data_ptr(), summary.exp.data_ptr(),
+                               a.block_table.data_ptr(), a.context_lens.data_ptr(), out.data_ptr(), a.B, a.Hq, a.Hkv,
+                               a.D, a.block_size, a.max_blocks, a.num_blocks, a.max_context_len, top_blocks,
+                               sink_blocks, recent_blocks)
+        _run_own_ws("aflex_block_select", args, ws, stream)
+    return out
+
+
+def attn_sparse_decode(a, selected, q=None, out=None, scale: float = 0.0, stream=None, ws=None):
+    """Decode attention of q (default a.q) [B, Hq, D] over the blocks that selected [B, Hkv, top_blocks] lists."""
+    load()
+    q = a.q if q is None else q
+    dev = _device_of(q)
+    _want_cache(a, dev)
+    _want(q, "q", a.B * a.Hq * a.D, torch.bfloat16, dev)
+    top = selected.shape[-1]
+    _want(selected, "selected", a.B * a.Hkv * top, torch.int32, dev)
+    with _On(dev):
+        if out is None:
+            out = _empty(stream, dev, a.B, a.Hq, a.D)
+        else:
+            _want(out, "out", a.B * a.Hq * a.D, torch.bfloat16, dev)
+        attn = AttnArgs(q.data_ptr(), a.k_cache.data_ptr(), a.v_cache.data_ptr(), a.block_table.data_ptr(),
+                        a.context_lens.data_ptr(), out.data_ptr(), a.B, a.Hq, a.Hkv, a.D, a.block_size, a.max_blocks,
+                        a.num_blocks, a.max_context_len, scale, 0)
+        _run_own_ws("aflex_attn_sparse_decode", AttnSparseArgs(attn, selected.data_ptr(), top), ws, stream)
+    return out

@@ -8,12 +8,15 @@
 #include <vector>
 
 #include "aflex.h"
+#include "api_common.h"
 #include "kernels.h"
 #include "profile.h"
 
 namespace {
-
 thread_local char g_err[512] = "";
+}  // namespace
+
+namespace aflex {
 
 aflex_status fail(aflex_status s, const char* fmt, ...) {
   va_list ap;
@@ -22,13 +25,6 @@ aflex_status fail(aflex_status s, const char* fmt, ...) {
   va_end(ap);
   return s;
 }
-
-bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15u) == 0; }
-
-#define REQUIRE(cond, status, ...) \
-  do {                             \
-    if (!(cond)) return fail(status, __VA_ARGS__); \
-  } while (0)
 
 aflex_status check_attn(const aflex_attn_args* a, bool need_out) {
   REQUIRE(a, AFLEX_ERR_INVALID_ARG, "attn: args is NULL");
@@ -62,6 +58,28 @@ aflex_status check_attn(const aflex_attn_args* a, bool need_out) {
   return AFLEX_OK;
 }
 
+aflex_status check_ws(void* ws, size_t have, size_t need, const char* who) {
+  REQUIRE(have >= need, AFLEX_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu required", who, have, need);
+  REQUIRE(need == 0 || ws, AFLEX_ERR_WORKSPACE, "%s: workspace is NULL", who);
+  REQUIRE(((uintptr_t)ws & 255u) == 0, AFLEX_ERR_ALIGNMENT, "%s: workspace must be 256-byte aligned", who);
+  return AFLEX_OK;
+}
+
+aflex_status hip_status(hipError_t e, const char* who) {
+  if (e == hipSuccess) return AFLEX_OK;
+  return fail(AFLEX_ERR_HIP, "%s: HIP error %d (%s)", who, (int)e, hipGetErrorString(e));
+}
+
+}  // namespace aflex
+
+using aflex::aligned16;
+using aflex::check_attn;
+using aflex::check_ws;
+using aflex::fail;
+using aflex::hip_status;
+
+namespace {
+
 aflex_status check_ffn(const aflex_ffn_args* f, bool moe, bool need_x) {
   const char* who = moe ? "moe" : "swiglu";
   REQUIRE(f, AFLEX_ERR_INVALID_ARG, "%s: args is NULL", who);
@@ -82,18 +100,6 @@ aflex_status check_ffn(const aflex_ffn_args* f, bool moe, bool need_x) {
     REQUIRE((long long)f->T * f->k < (1ll << 30), AFLEX_ERR_UNSUPPORTED, "moe: too many token/slot pairs");
   }
   return AFLEX_OK;
-}
-
-aflex_status check_ws(void* ws, size_t have, size_t need, const char* who) {
-  REQUIRE(have >= need, AFLEX_ERR_WORKSPACE, "%s: workspace of %zu bytes, %zu required", who, have, need);
-  REQUIRE(need == 0 || ws, AFLEX_ERR_WORKSPACE, "%s: workspace is NULL", who);
-  REQUIRE(((uintptr_t)ws & 255u) == 0, AFLEX_ERR_ALIGNMENT, "%s: workspace must be 256-byte aligned", who);
-  return AFLEX_OK;
-}
-
-aflex_status hip_status(hipError_t e, const char* who) {
-  if (e == hipSuccess) return AFLEX_OK;
-  return fail(AFLEX_ERR_HIP, "%s: HIP error %d (%s)", who, (int)e, hipGetErrorString(e));
 }
 
 // ---------------------------------------------------------------------------

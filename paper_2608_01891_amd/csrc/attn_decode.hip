@@ -75,6 +75,8 @@ struct AttnParams {
   int unit_cost;                 // extra cost of a unit in block positions (0 with fixed pieces)
   int rounds;                    // 3: range sizes weighted by dispatch round (see split_of); else 1
   float scale_log2;              // softmax scale * log2(e)
+  const int32_t* sel;            // [U][top] chosen blocks of each unit (SPARSE kernels only)
+  int top;
 };
 
 constexpr int kWaves = 4;
@@ -92,6 +94,13 @@ __device__ __forceinline__ int clamp_ctx(const AttnParams& p, int b) {
 }
 
 __device__ __forceinline__ int nblk_of(int ctx) { return (ctx + 15) >> 4; }
+
+// Blocks that a unit of sequence b attends: all of them, or the chosen ones.
+template <bool SPARSE>
+__device__ __forceinline__ int unit_blocks(const AttnParams& p, int b) {
+  const int n = nblk_of(clamp_ctx(p, b));
+  return SPARSE ? min(n, p.top) : n;
+}
 
 // K/V tile loads; NT marks them non-temporal (each cached byte is read once).
 template <bool NT>
@@ -120,32 +129,46 @@ __device__ __forceinline__ int wave_incl_scan(int v, int lane) {
   return v;
 }
 
-// Block id of local block jb of sequence b's table, or -1 when jb is past the
-// piece's end or the table entry is out of range (its tokens are masked).
-__device__ __forceinline__ int load_block_id(const AttnParams& p, int b, int jb, int j_end) {
-  int id = -1;
+// A block of a unit's list: its pool id, or -1 when it is past the piece's end
+// or out of range (its tokens are masked), and its place in the sequence (the
+// list's own index where every block is attended).
+struct BlockRef {
+  int id, j;
+};
+
+template <bool SPARSE>
+__device__ __forceinline__ BlockRef load_block(const AttnParams& p, int b, int kvh, int jb, int j_end) {
+  BlockRef r{-1, jb};
   if (jb < j_end) {
-    id = p.bt[(size_t)b * p.max_blocks + jb];
-    if (id < 0 || id >= p.num_blocks) id = -1;
+    if constexpr (SPARSE) {
+      const int32_t* row = p.sel + ((size_t)b * p.Hkv + kvh) * p.top;
+      const int prev = jb > 0 ? row[jb - 1] : -1;
+      r.j = row[jb];
+      if (r.j <= prev || r.j < 0 || r.j >= nblk_of(clamp_ctx(p, b))) return BlockRef{-1, 0};
+    }
+    r.id = p.bt[(size_t)b * p.max_blocks + r.j];
+    if (r.id < 0 || r.id >= p.num_blocks) r.id = -1;
   }
-  return id;
+  return r;
 }
 
 // Positions a (sequence, kv head) unit of sequence b takes in the flattened
 // range: its blocks plus a fixed charge for the piece it adds (zero for a
 // sequence with no cached token, which has no unit).
+template <bool SPARSE>
 __device__ __forceinline__ int unit_len(const AttnParams& p, int b) {
-  const int n = nblk_of(clamp_ctx(p, b));
+  const int n = unit_blocks<SPARSE>(p, b);
   return n > 0 ? n + p.unit_cost : 0;
 }
 
 // Partition of the flattened range, as the decode kernel computes it: the
 // total over all units (W) and the positions per work-group.
+template <bool SPARSE>
 __device__ __forceinline__ int chunk_of(const AttnParams& p, int P, int lane, int* W_out) {
   int total = 0;
   for (int c = 0; c < p.B; c += 64) {
     const int b = c + lane;
-    total += wave_sum_i(b < p.B ? unit_len(p, b) : 0);
+    total += wave_sum_i(b < p.B ? unit_len<SPARSE>(p, b) : 0);
   }
   const int W = __builtin_amdgcn_readfirstlane(total) * p.Hkv;
   *W_out = W;
@@ -207,8 +230,9 @@ __device__ __forceinline__ int split_owner(int R, int c0, int c1, int c2, int x)
 }
 
 // UNIT: one work-group per (sequence, kv head) unit, written whole (no
-// partials); otherwise the even split of the flattened range.
-template <int D, bool NT, bool UNIT, int NW = kWaves>
+// partials); otherwise the even split of the flattened range. SPARSE: a unit's
+// blocks are those that its row of p.sel lists, not the whole context.
+template <int D, bool NT, bool UNIT, int NW = kWaves, bool SPARSE = false>
 __global__ __launch_bounds__(64 * NW, 12 / NW) void attn_decode_kernel(AttnParams p) {
   constexpr int NC = D / 32;   // k-chunks of the QK product
   constexpr int NMT = D / 16;  // d-tiles of the PV product
@@ -257,7 +281,7 @@ __global__ __launch_bounds__(64 * NW, 12 / NW) void attn_decode_kernel(AttnParam
   int W = 0;
   int sR = P, sc0 = 1 << 30, sc1 = 1 << 30, sc2 = 1 << 30;
   if constexpr (!UNIT) {
-    const int C = chunk_of(p, P, lane, &W);
+    const int C = chunk_of<SPARSE>(p, P, lane, &W);
     if constexpr (NW == kWaves) {  // the grid of three work-groups per CU
       split_of(p, P, W, C, sR, sc0, sc1, sc2);
     } else {
@@ -265,7 +289,7 @@ __global__ __launch_bounds__(64 * NW, 12 / NW) void attn_decode_kernel(AttnParam
     }
   }
   const int ub = UNIT ? wg / Hkv : 0;
-  const int unb = UNIT ? (ub < p.B ? nblk_of(clamp_ctx(p, ub)) : 0) : 0;
+  const int unb = UNIT ? (ub < p.B ? unit_blocks<SPARSE>(p, ub) : 0) : 0;
   const int x0 = __builtin_amdgcn_readfirstlane(UNIT ? (wg - ub * Hkv) * unb : split_start(sR, sc0, sc1, sc2, wg));
   if (UNIT ? unb == 0 : x0 >= W) return;
   const int x1 = __builtin_amdgcn_readfirstlane(UNIT ? x0 + unb : min(x0 + split_size(sR, sc0, sc1, sc2, wg), W));
@@ -279,7 +303,7 @@ __global__ __launch_bounds__(64 * NW, 12 / NW) void attn_decode_kernel(AttnParam
   if constexpr (!UNIT) {
     for (int c = 0; c < p.B; c += 64) {
       const int bb = c + lane;
-      const int n = bb < p.B ? unit_len(p, bb) : 0;
+      const int n = bb < p.B ? unit_len<SPARSE>(p, bb) : 0;
       const int incl = wave_incl_scan(n, lane);
       const unsigned long long past = __ballot((base + incl) * Hkv > x0);
       if (past) {
@@ -295,7 +319,7 @@ __global__ __launch_bounds__(64 * NW, 12 / NW) void attn_decode_kernel(AttnParam
   b = __builtin_amdgcn_readfirstlane(b);
   base = __builtin_amdgcn_readfirstlane(base);
   const int uc = UNIT ? 0 : p.unit_cost;
-  int nb = nblk_of(clamp_ctx(p, b));
+  int nb = unit_blocks<SPARSE>(p, b);
   int kvh = (x0 - base * Hkv) / (nb + uc);
 
   // Token slots. QK tile row rr (lane rr loads it) holds token
@@ -316,10 +340,10 @@ __global__ __launch_bounds__(64 * NW, 12 / NW) void attn_decode_kernel(AttnParam
   // First block-id chunk of the current piece; each piece loads the next
   // piece's first chunk while it streams, so a new piece starts with its K/V
   // loads instead of a round trip for its block ids.
-  int piece_ids;
+  BlockRef piece_ids;
   {
     const int us = base * Hkv + kvh * (nb + uc) + uc;
-    piece_ids = load_block_id(p, b, max(x0 - us, 0) + lane, min(nb, x1 - us));
+    piece_ids = load_block<SPARSE>(p, b, kvh, max(x0 - us, 0) + lane, min(nb, x1 - us));
   }
   while (x < x1) {
     const int ctx = clamp_ctx(p, b);
@@ -340,10 +364,11 @@ __global__ __launch_bounds__(64 * NW, 12 / NW) void attn_decode_kernel(AttnParam
       basen = base + nb + uc;
       do {
         ++bn;
-      } while (xn < x1 && bn < p.B && nblk_of(clamp_ctx(p, bn)) == 0);
-      nbn = (xn < x1) ? nblk_of(clamp_ctx(p, bn)) : 0;
+      } while (xn < x1 && bn < p.B && unit_blocks<SPARSE>(p, bn) == 0);
+      nbn = (xn < x1) ? unit_blocks<SPARSE>(p, bn) : 0;
     }
-    const int next_piece_ids = (xn < x1) ? load_block_id(p, bn, lane, min(nbn, x1 - xn - uc)) : -1;
+    const BlockRef next_piece_ids =
+        (xn < x1) ? load_block<SPARSE>(p, bn, kvhn, lane, min(nbn, x1 - xn - uc)) : BlockRef{-1, 0};
     if (j1 <= j0) break;  // the range ends inside the unit's leading charge
 
     // q as the B operand of the QK product: column g = r, k = d in [c*32 + qg*8, +8).
@@ -356,8 +381,8 @@ __global__ __launch_bounds__(64 * NW, 12 / NW) void attn_decode_kernel(AttnParam
 
     // Block ids of the piece, 64 per wave register (lane l: local block
     // j0 + 64 c + l of chunk c); the next chunk is loaded one chunk ahead.
-    int my_id = piece_ids;
-    int next_id = (npairs > 32) ? load_block_id(p, b, j0 + 64 + lane, j1) : -1;
+    BlockRef my_id = piece_ids;
+    BlockRef next_id = (npairs > 32) ? load_block<SPARSE>(p, b, kvh, j0 + 64 + lane, j1) : BlockRef{-1, 0};
     int cur_chunk = 0;
 
     float m_run = kNegInf;
@@ -370,11 +395,15 @@ __global__ __launch_bounds__(64 * NW, 12 / NW) void attn_decode_kernel(AttnParam
       if ((pr >> 5) != cur_chunk) {  // advances by at most one chunk per step
         cur_chunk = pr >> 5;
         my_id = next_id;
-        next_id = ((cur_chunk + 1) * 32 < npairs) ? load_block_id(p, b, j0 + (cur_chunk + 1) * 64 + lane, j1) : -1;
+        next_id = ((cur_chunk + 1) * 32 < npairs)
+                      ? load_block<SPARSE>(p, b, kvh, j0 + (cur_chunk + 1) * 64 + lane, j1)
+                      : BlockRef{-1, 0};
       }
-      const int idA = __builtin_amdgcn_readlane(my_id, (2 * pr) & 63);
-      const int idB = __builtin_amdgcn_readlane(my_id, (2 * pr + 1) & 63);
-      const int tA = (j0 + 2 * pr) * 16;
+      const int idA = __builtin_amdgcn_readlane(my_id.id, (2 * pr) & 63);
+      const int idB = __builtin_amdgcn_readlane(my_id.id, (2 * pr + 1) & 63);
+      // first tokens of the pair's blocks
+      const int tA = (SPARSE ? __builtin_amdgcn_readlane(my_id.j, (2 * pr) & 63) : j0 + 2 * pr) * 16;
+      const int tB = SPARSE ? __builtin_amdgcn_readlane(my_id.j, (2 * pr + 1) & 63) * 16 : tA + 16;
 
       bf16x8 k1[NC], k2[NC], vf[NMT];
       const int pk = ksel ? idB : idA;
@@ -390,7 +419,7 @@ __global__ __launch_bounds__(64 * NW, 12 / NW) void attn_decode_kernel(AttnParam
         for (int c = 0; c < NC; ++c) k1[c] = k2[c] = zero_bf16x8();
       }
       const int pv = vsel ? idB : idA;
-      const int tb = tA + vsel * 16 + vtok;  // first token of this lane's 8-token slice
+      const int tb = (SPARSE ? (vsel ? tB : tA) : tA + vsel * 16) + vtok;  // first token of this lane's 8-token slice
       const int nv = (pv >= 0) ? ctx - tb : 0;
       if (pv >= 0) {
         const uint16_t* vb = p.vc + ((size_t)pv * Hkv + kvh) * D * 16 + vtok;
@@ -662,8 +691,15 @@ constexpr int kManyPieces = 8;
 
 static int unit_cost(const aflex_attn_args& a) { return a.split_tokens > 0 ? 0 : kUnitCost; }
 
-static long long work_bound(const aflex_attn_args& a) {
-  return (long long)a.B * a.Hkv * ((a.max_context_len + 15) / 16 + unit_cost(a));
+// Bound on a unit's blocks: those of the longest context, or of the longest list
+// of chosen ones (top > 0).
+static int max_unit_blocks(const aflex_attn_args& a, int top) {
+  const int n = (a.max_context_len + 15) / 16;
+  return top > 0 && top < n ? top : n;
+}
+
+static long long work_bound(const aflex_attn_args& a, int top = 0) {
+  return (long long)a.B * a.Hkv * (max_unit_blocks(a, top) + unit_cost(a));
 }
 
 // Contexts of at most this many tokens take one work-group per (sequence, kv
@@ -672,17 +708,18 @@ static long long work_bound(const aflex_attn_args& a) {
 // sizes costs more than the imbalance between units, is skipped.
 constexpr int kUnitPerWgMaxCtx = 512;
 
-static bool unit_per_wg(const aflex_attn_args& a) {
-  return a.split_tokens == 0 && a.max_context_len <= kUnitPerWgMaxCtx && (long long)a.B * a.Hkv <= resident_wgs();
+static bool unit_per_wg(const aflex_attn_args& a, int top = 0) {
+  return a.split_tokens == 0 && max_unit_blocks(a, top) <= kUnitPerWgMaxCtx / 16 &&
+         (long long)a.B * a.Hkv <= resident_wgs();
 }
 
 // Grid size: one work-group per unit for short contexts (above); with a fixed
 // piece size, enough work-groups for the bound on the blocks; otherwise the
 // resident work-groups, fewer when the bound cannot give each of them a pair
 // per wave.
-static int attn_grid(const aflex_attn_args& a, bool wide = false) {
-  if (unit_per_wg(a)) return a.B * a.Hkv > 0 ? a.B * a.Hkv : 1;
-  const long long wb = work_bound(a);
+static int attn_grid(const aflex_attn_args& a, bool wide = false, int top = 0) {
+  if (unit_per_wg(a, top)) return a.B * a.Hkv > 0 ? a.B * a.Hkv : 1;
+  const long long wb = work_bound(a, top);
   long long P;
   if (a.split_tokens > 0) {
     P = (wb + a.split_tokens / 16 - 1) / (a.split_tokens / 16);
@@ -700,15 +737,17 @@ static int attn_grid(const aflex_attn_args& a, bool wide = false) {
 bool attn_shape_fits(const aflex_attn_args& a) { return work_bound(a) < (1ll << 30); }
 
 // (sized for the narrow grid, which is never smaller than the wide one)
-size_t attn_workspace_bytes(const aflex_attn_args& a) {
+size_t attn_workspace_bytes(const aflex_attn_args& a, int top) {
   const size_t U = (size_t)a.B * a.Hkv;
-  const size_t segs = U + (size_t)attn_grid(a);
+  const size_t segs = U + (size_t)attn_grid(a, false, top);
   const size_t G = (size_t)(a.Hq / a.Hkv);
   return align_up(segs * G * a.D * sizeof(float), 256) + align_up(segs * G * 2 * sizeof(float), 256) +
          align_up(U * sizeof(int2), 256);
 }
 
-hipError_t launch_attn_decode(const aflex_attn_args& a, void* ws, hipStream_t stream, AttnForm form) {
+// Everything of the kernels' parameters that the two entry points share; P
+// work-groups (attn_grid).
+static AttnParams attn_params(const aflex_attn_args& a, void* ws, int P) {
   AttnParams p;
   p.q = a.q;
   p.kc = a.k_cache;
@@ -725,18 +764,12 @@ hipError_t launch_attn_decode(const aflex_attn_args& a, void* ws, hipStream_t st
   p.max_ctx = a.max_context_len;
   p.chunk_blocks = a.split_tokens > 0 ? a.split_tokens / 16 : 0;
   p.unit_cost = unit_cost(a);
-  const bool unit = unit_per_wg(a);
-  const bool wide = form == AttnForm::kWide && !unit && a.split_tokens == 0;
+  p.rounds = 1;
   const float scale = a.scale != 0.f ? a.scale : 1.0f / sqrtf((float)a.D);
   p.scale_log2 = scale * kLog2e;
-  const int P = attn_grid(a, wide);
-  // weighted rounds for the full grid of three 4-wave work-groups per CU
-  // (beside other work the dispatch order no longer places the rounds: the
-  // layer step, whose attention runs beside the MoE stream, took 2.78 ms with
-  // the weighting and 2.75 ms without)
-  p.rounds = (form == AttnForm::kAlone && !unit && a.split_tokens == 0 && P == resident_wgs() && P % 3 == 0) ? 3 : 1;
-  const size_t U = (size_t)a.B * a.Hkv;
-  const size_t segs = U + (size_t)P;
+  p.sel = nullptr;
+  p.top = 0;
+  const size_t segs = (size_t)a.B * a.Hkv + (size_t)P;
   const size_t G = (size_t)p.G;
   char* w = static_cast<char*>(ws);
   p.part_o = reinterpret_cast<float*>(w);
@@ -744,6 +777,34 @@ hipError_t launch_attn_decode(const aflex_attn_args& a, void* ws, hipStream_t st
   p.part_ml = reinterpret_cast<float*>(w);
   w += align_up(segs * G * 2 * sizeof(float), 256);
   p.span = reinterpret_cast<int2*>(w);
+  return p;
+}
+
+// Merge of the units that the even split cut between the P work-groups.
+static void launch_merge(const AttnParams& p, int D, int P, hipStream_t stream) {
+  ProfScope ps("attn_merge", stream);
+  const int U = p.B * p.Hkv;
+  const bool many = P >= kManyPieces * (long long)U;
+  if (many && D == 128)
+    attn_merge_many_kernel<128><<<U * p.G, 256, 0, stream>>>(p);
+  else if (many)
+    attn_merge_many_kernel<64><<<U * p.G, 256, 0, stream>>>(p);
+  else if (D == 128)
+    attn_merge_kernel<128><<<U, 256, 0, stream>>>(p);
+  else
+    attn_merge_kernel<64><<<U, 256, 0, stream>>>(p);
+}
+
+hipError_t launch_attn_decode(const aflex_attn_args& a, void* ws, hipStream_t stream, AttnForm form) {
+  const bool unit = unit_per_wg(a);
+  const bool wide = form == AttnForm::kWide && !unit && a.split_tokens == 0;
+  const int P = attn_grid(a, wide);
+  AttnParams p = attn_params(a, ws, P);
+  // weighted rounds for the full grid of three 4-wave work-groups per CU
+  // (beside other work the dispatch order no longer places the rounds: the
+  // layer step, whose attention runs beside the MoE stream, took 2.78 ms with
+  // the weighting and 2.75 ms without)
+  p.rounds = (form == AttnForm::kAlone && !unit && a.split_tokens == 0 && P == resident_wgs() && P % 3 == 0) ? 3 : 1;
   {
     ProfScope ps("attn_decode", stream);
     if (a.D == 128) {
@@ -762,18 +823,32 @@ hipError_t launch_attn_decode(const aflex_attn_args& a, void* ws, hipStream_t st
         attn_decode_kernel<64, true, false><<<P, 256, 0, stream>>>(p);
     }
   }
-  if (P > 1 && !unit) {  // with one work-group, or one per unit, no unit is split
-    ProfScope ps("attn_merge", stream);
-    const bool many = P >= kManyPieces * (long long)a.B * a.Hkv;
-    if (many && a.D == 128)
-      attn_merge_many_kernel<128><<<a.B * a.Hkv * p.G, 256, 0, stream>>>(p);
-    else if (many)
-      attn_merge_many_kernel<64><<<a.B * a.Hkv * p.G, 256, 0, stream>>>(p);
+  if (P > 1 && !unit) launch_merge(p, a.D, P, stream);  // with one work-group, or one per unit, no unit is split
+  return hipGetLastError();
+}
+
+// Attention over chosen blocks: the same work-groups over lists of at most
+// top_blocks blocks per unit.
+hipError_t launch_attn_sparse(const aflex_attn_sparse_args& s, void* ws, hipStream_t stream) {
+  const aflex_attn_args& a = s.attn;
+  const bool unit = unit_per_wg(a, s.top_blocks);
+  const int P = attn_grid(a, false, s.top_blocks);
+  AttnParams p = attn_params(a, ws, P);
+  p.rounds = !unit && P == resident_wgs() && P % 3 == 0 ? 3 : 1;
+  p.sel = s.selected;
+  p.top = s.top_blocks;
+  {
+    ProfScope ps("attn_sparse", stream);
+    if (a.D == 128 && unit)
+      attn_decode_kernel<128, true, true, kWaves, true><<<P, 256, 0, stream>>>(p);
     else if (a.D == 128)
-      attn_merge_kernel<128><<<a.B * a.Hkv, 256, 0, stream>>>(p);
+      attn_decode_kernel<128, true, false, kWaves, true><<<P, 256, 0, stream>>>(p);
+    else if (unit)
+      attn_decode_kernel<64, true, true, kWaves, true><<<P, 256, 0, stream>>>(p);
     else
-      attn_merge_kernel<64><<<a.B * a.Hkv, 256, 0, stream>>>(p);
+      attn_decode_kernel<64, true, false, kWaves, true><<<P, 256, 0, stream>>>(p);
   }
+  if (P > 1 && !unit) launch_merge(p, a.D, P, stream);
   return hipGetLastError();
 }
 

@@ -4,6 +4,7 @@
 #include <stddef.h>
 
 #include "aflex.h"
+#include "aflex_longctx.h"
 
 namespace aflex {
 
@@ -19,7 +20,8 @@ hipError_t static_scratch(void** ptr);
 // Decode attention (attn_decode.hip). attn_shape_fits: the flattened block
 // range B * Hkv * ceil(max_context_len / 16) stays below 2^30.
 bool attn_shape_fits(const aflex_attn_args& a);
-size_t attn_workspace_bytes(const aflex_attn_args& a);
+// top > 0: at most that many chosen blocks per (sequence, kv head)
+size_t attn_workspace_bytes(const aflex_attn_args& a, int top = 0);
 // K/V tiles stream with non-temporal loads: every cached byte is read once,
 // alone and next to the FFN's weight stream in the two-stream step alike
 // (that step: 2.785 -> 2.730 ms against ordinary loads). The form of the even
@@ -31,6 +33,17 @@ size_t attn_workspace_bytes(const aflex_attn_args& a);
 enum class AttnForm { kAlone, kWide, kShared };
 hipError_t launch_attn_decode(const aflex_attn_args& a, void* ws, hipStream_t stream,
                               AttnForm form = AttnForm::kAlone);
+
+// Attention over chosen blocks (attn_decode.hip; workspace: attn_workspace_bytes
+// of its attn and top_blocks) and the choice (block_select.hip).
+hipError_t launch_attn_sparse(const aflex_attn_sparse_args& s, void* ws, hipStream_t stream);
+size_t block_select_workspace_bytes(const aflex_block_select_args& a);
+hipError_t launch_block_select(const aflex_block_select_args& a, void* ws, hipStream_t stream);
+
+// Rotation, cache write and block summaries (rope.hip).
+hipError_t launch_rope_append(const aflex_rope_args& a, hipStream_t stream);
+hipError_t launch_rope_write(const aflex_rope_args& a, hipStream_t stream);
+hipError_t launch_block_summary(const aflex_block_summary_args& a, hipStream_t stream);
 
 // Dense SwiGLU FFN (ffn.hip).
 size_t swiglu_workspace_bytes(const aflex_ffn_args& f);

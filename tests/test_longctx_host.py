@@ -1,0 +1,194 @@
+"""Host-side checks of the long-context entry points (no GPU needed): exports,
+refusals before any launch, workspace sizes, and what the binding refuses."""
+import ctypes
+
+import pytest
+import torch
+
+from paper_2608_01891_amd import aflex, synth
+
+FAKE = 0x10000000  # aligned, never dereferenced: validation fails before any launch
+INVALID, UNSUP, ALIGN, WS = (aflex.ERR_INVALID_ARG, aflex.ERR_UNSUPPORTED, aflex.ERR_ALIGNMENT, aflex.ERR_WORKSPACE)
+
+
+@pytest.fixture(scope="module")
+def lib():
+    return aflex.load()
+
+
+def test_exports_every_declared_symbol(lib):
+    names = aflex.exported_names(aflex.LONGCTX_HEADER)
+    assert len(names) == 7
+    for n in names:
+        assert hasattr(lib, n), n
+
+
+def _fill(cls, kw, **base):
+    a = cls(**base)
+    for k, v in kw.items():
+        setattr(a, k, v)
+    return a
+
+
+def _rope(**kw):
+    return _fill(aflex.RopeArgs, kw, q=FAKE, k_new=FAKE, v_new=FAKE, rope=FAKE, positions=None, cu_seqlens=FAKE,
+                 q_out=FAKE, k_cache=FAKE, v_cache=FAKE, block_keys=FAKE, block_exp=FAKE, block_table=FAKE,
+                 context_lens=FAKE, B=2, T=20, Hq=8, Hkv=2, D=64, rotary_dim=64, interleaved=0, rope_len=100,
+                 max_seqlen=15, block_size=16, max_blocks_per_seq=4, num_blocks=8)
+
+
+BOTH = [(dict(q=None), INVALID), (dict(k_new=None), INVALID), (dict(q_out=None), INVALID), (dict(rope=None), INVALID),
+        (dict(block_keys=None), INVALID), (dict(block_exp=None), INVALID), (dict(B=0), INVALID), (dict(Hq=0), INVALID),
+        (dict(Hkv=0), INVALID), (dict(num_blocks=0), INVALID), (dict(max_blocks_per_seq=0), INVALID),
+        (dict(max_blocks_per_seq=(1 << 26) + 1), UNSUP),
+        (dict(D=96), UNSUP), (dict(block_size=32), UNSUP), (dict(rotary_dim=65), INVALID),
+        (dict(rotary_dim=24), INVALID), (dict(rotary_dim=-16), INVALID), (dict(rotary_dim=80), INVALID),
+        (dict(rope_len=0), INVALID), (dict(q_stride=504), INVALID), (dict(q_stride=516), INVALID),
+        (dict(k_stride=64), INVALID), (dict(v_stride=-128), INVALID), (dict(q=FAKE + 8), ALIGN),
+        (dict(v_cache=FAKE + 2), ALIGN), (dict(rope=FAKE + 4), ALIGN), (dict(block_keys=FAKE + 1), ALIGN),
+        (dict(context_lens=FAKE + 2), ALIGN), (dict(positions=FAKE + 1), ALIGN), (dict(Hq=1 << 25), UNSUP)]
+
+
+@pytest.mark.parametrize("kw,status", BOTH + [(dict(B=1 << 28, Hq=8), UNSUP)])
+def test_rope_append_rejects(lib, kw, status):
+    assert lib.aflex_rope_append(ctypes.byref(_rope(**kw)), None) == status
+    assert lib.aflex_last_error().startswith(b"rope_append")
+
+
+@pytest.mark.parametrize("kw,status", BOTH + [
+    (dict(cu_seqlens=None), INVALID), (dict(T=-1), INVALID), (dict(max_seqlen=-1), INVALID),
+    (dict(max_seqlen=21), INVALID), (dict(B=70000), UNSUP), (dict(Hq=8192), UNSUP), (dict(cu_seqlens=FAKE + 1), ALIGN)])
+def test_rope_write_rejects(lib, kw, status):
+    assert lib.aflex_rope_write(ctypes.byref(_rope(**kw)), None) == status
+    assert lib.aflex_last_error().startswith(b"rope_write")
+
+
+def test_nothing_to_write_is_no_launch(lib):
+    assert lib.aflex_rope_write(ctypes.byref(_rope(T=0, max_seqlen=0)), None) == aflex.OK
+    assert lib.aflex_rope_write(ctypes.byref(_rope(rotary_dim=0, rope=None, rope_len=0, block_keys=None,
+                                                   block_exp=None, T=0, max_seqlen=0)), None) == aflex.OK
+    assert lib.aflex_block_summary(ctypes.byref(_summary(max_context_len=15)), None) == aflex.OK
+
+
+def _summary(**kw):
+    return _fill(aflex.BlockSummaryArgs, kw, k_cache=FAKE, block_keys=FAKE, block_exp=FAKE, block_table=FAKE,
+                 context_lens=FAKE, B=2, Hkv=2, D=64, block_size=16, max_blocks_per_seq=4, num_blocks=8,
+                 max_context_len=64)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(k_cache=None), INVALID), (dict(block_exp=None), INVALID), (dict(B=0), INVALID), (dict(B=65536), UNSUP),
+    (dict(D=32), UNSUP), (dict(block_size=8), UNSUP), (dict(max_context_len=65), INVALID),
+    (dict(max_context_len=-1), INVALID), (dict(k_cache=FAKE + 8), ALIGN), (dict(block_table=FAKE + 2), ALIGN)])
+def test_block_summary_rejects(lib, kw, status):
+    assert lib.aflex_block_summary(ctypes.byref(_summary(**kw)), None) == status
+    assert lib.aflex_last_error().startswith(b"block_summary")
+
+
+def _select(**kw):
+    return _fill(aflex.BlockSelectArgs, kw, q=FAKE, block_keys=FAKE, block_exp=FAKE, block_table=FAKE,
+                 context_lens=FAKE, selected=FAKE, B=2, Hq=8, Hkv=2, D=64, block_size=16, max_blocks_per_seq=40,
+                 num_blocks=80, max_context_len=640, top_blocks=8, sink_blocks=1, recent_blocks=2)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(q=None), INVALID), (dict(selected=None), INVALID), (dict(B=0), INVALID), (dict(Hq=7), INVALID),
+    (dict(Hq=34), UNSUP), (dict(D=256), UNSUP), (dict(block_size=64), UNSUP), (dict(max_context_len=641), INVALID),
+    (dict(top_blocks=2), INVALID), (dict(top_blocks=0, sink_blocks=0, recent_blocks=0), INVALID),
+    (dict(recent_blocks=0), INVALID), (dict(sink_blocks=-1), INVALID),
+    (dict(sink_blocks=(1 << 31) - 1, recent_blocks=(1 << 31) - 1), INVALID),
+    (dict(B=1 << 20, Hkv=8, max_blocks_per_seq=1 << 20, max_context_len=1 << 24), UNSUP),
+    (dict(B=1 << 20, top_blocks=1 << 10), UNSUP),
+    (dict(q=FAKE + 2), ALIGN), (dict(selected=FAKE + 2), ALIGN)])
+def test_block_select_rejects(lib, kw, status):
+    n = ctypes.c_size_t()
+    a = _select(**kw)
+    assert lib.aflex_block_select(ctypes.byref(a), ctypes.c_void_p(FAKE), 1 << 40, None) == status
+    assert lib.aflex_last_error().startswith(b"block_select")
+    assert lib.aflex_block_select_workspace(ctypes.byref(a), ctypes.byref(n)) == status
+
+
+def test_block_select_workspace(lib):
+    n = ctypes.c_size_t()
+    a = _select()
+    assert lib.aflex_block_select_workspace(ctypes.byref(a), ctypes.byref(n)) == aflex.OK
+    need = n.value
+    assert lib.aflex_block_select_workspace(ctypes.byref(a), None) == INVALID
+    if need:
+        assert lib.aflex_block_select(ctypes.byref(a), ctypes.c_void_p(FAKE), need - 1, None) == WS
+        assert lib.aflex_block_select(ctypes.byref(a), None, need, None) == WS
+        assert lib.aflex_block_select(ctypes.byref(a), ctypes.c_void_p(FAKE + 128), need, None) == ALIGN
+
+
+def _sparse(top_blocks=8, selected=FAKE, **kw):
+    a = aflex.AttnArgs(q=FAKE, k_cache=FAKE, v_cache=FAKE, block_table=FAKE, context_lens=FAKE, out=FAKE, B=4, Hq=8,
+                       Hkv=2, D=64, block_size=16, max_blocks_per_seq=130, num_blocks=320, max_context_len=2000,
+                       scale=0.0, split_tokens=0)
+    for k, v in kw.items():
+        setattr(a, k, v)
+    return aflex.AttnSparseArgs(a, selected, top_blocks)
+
+
+@pytest.mark.parametrize("kw,status", [
+    (dict(selected=None), INVALID), (dict(top_blocks=0), INVALID), (dict(out=None), INVALID), (dict(q=None), INVALID),
+    (dict(split_tokens=128), UNSUP), (dict(D=96), UNSUP), (dict(Hq=34), UNSUP), (dict(scale=-1.0), INVALID),
+    (dict(top_blocks=(1 << 31) - 1), UNSUP), (dict(selected=FAKE + 2), ALIGN), (dict(q=FAKE + 8), ALIGN)])
+def test_attn_sparse_rejects(lib, kw, status):
+    a = _sparse(**kw)
+    assert lib.aflex_attn_sparse_decode(ctypes.byref(a), ctypes.c_void_p(FAKE), 1 << 40, None) == status
+    assert lib.aflex_last_error()
+
+
+def test_attn_sparse_workspace_goes_by_the_chosen_blocks(lib):
+    n = ctypes.c_size_t()
+    sizes = []
+    for top in (1, 64, 1 << 20):
+        a = _sparse(top_blocks=top, B=64, Hq=64, Hkv=8, D=128, max_blocks_per_seq=4096, max_context_len=65536)
+        assert lib.aflex_attn_sparse_decode_workspace(ctypes.byref(a), ctypes.byref(n)) == aflex.OK
+        assert n.value >= 64 * 8 * 8 * (128 + 2) * 4
+        assert lib.aflex_attn_sparse_decode(ctypes.byref(a), ctypes.c_void_p(FAKE), n.value - 1, None) == WS
+        sizes.append(n.value)
+    assert sizes[0] <= sizes[1] <= sizes[2]
+
+
+def _calls():
+    a = synth.custom_attention(0, 2, 8, 2, 64, [20, 33], ctx_hi=64)
+    s = aflex.BlockSummary.of(a)
+    k = torch.zeros(2, 2, 64, dtype=torch.bfloat16)
+    rope = aflex.rope_table(64, 64)
+    cu = torch.tensor([0, 1, 2], dtype=torch.int32)
+    sel = torch.zeros(2, 2, 3, dtype=torch.int32)
+    return {
+        "rope_append": lambda: aflex.rope_append(a, a.q, k, k, rope, summary=s),
+        "rope_write": lambda: aflex.rope_write(a, a.q, k, k, cu, rope, max_seqlen=1),
+        "block_summary": lambda: aflex.block_summary(a, s),
+        "block_select": lambda: aflex.block_select(a, a.q, s, 3),
+        "attn_sparse_decode": lambda: aflex.attn_sparse_decode(a, sel),
+    }
+
+
+@pytest.mark.parametrize("op", list(_calls()))
+def test_host_tensors_are_refused_before_any_library_call(lib, monkeypatch, op):
+    calls = []
+
+    class Stub:
+        def __getattr__(self, name):
+            return lambda *a: calls.append(name) or aflex.OK
+
+    monkeypatch.setattr(aflex, "_lib", Stub())
+    with pytest.raises(ValueError, match="cuda device"):
+        _calls()[op]()
+    assert calls == []
+
+
+def test_rows_that_the_binding_refuses():
+    x = torch.zeros(3, 12, 64, dtype=torch.bfloat16)
+    assert aflex._row_stride(x[:, 2:10], "q", 3, 8, 64, -1) == 12 * 64
+    assert aflex._row_stride(x[:1, :1], "q", 1, 1, 64, -1) == 0
+    for bad in (x.float()[:, :8], x[:, :7], x[:, 0:8].transpose(0, 1).contiguous().transpose(0, 1),
+                x[:1, :8].expand(3, 8, 64), x[..., ::2], x[:, ::2]):
+        with pytest.raises(ValueError, match="q: expected"):
+            aflex._row_stride(bad, "q", 3, 8, 64, -1)
+    for bad in (x[:, :8], x.float(), torch.zeros(5, dtype=torch.bfloat16)):
+        with pytest.raises(ValueError, match="dense"):
+            aflex._want(bad, "t", 3 * 12 * 64, torch.bfloat16, -1)
