@@ -284,25 +284,48 @@ __global__ __launch_bounds__(256) void rope_write_kernel(aflex_rope_args a, int 
 constexpr int kTilesPerWave = 4;
 
 template <int D>
-__global__ __launch_bounds__(256) void block_summary_kernel(aflex_block_summary_args a) {
+__global__ __launch_bounds__(256, 6) void block_summary_kernel(aflex_block_summary_args a) {
   constexpr int U = TileLanes<D>::U, NR = TileLanes<D>::NR, RS = TileLanes<D>::RS;
   const int lane = threadIdx.x & 63;
   const int b = blockIdx.y;
   const int ctx = min(max(a.context_lens[b], 0), a.max_context_len);
   const long long tiles = (long long)(ctx / 16) * a.Hkv;
-  const long long t0 = ((long long)blockIdx.x * 4 + (threadIdx.x >> 6)) * kTilesPerWave;
+  const long long t0 =
+      ((long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * kTilesPerWave;
+  if (t0 >= tiles) return;
   const int u = lane % U, r = lane / U;
-  for (long long t = t0; t < min(t0 + kTilesPerWave, tiles); ++t) {
-    const int j = (int)(t / a.Hkv), g = (int)(t - (long long)j * a.Hkv);
-    const int blk = a.block_table[(size_t)b * a.max_blocks_per_seq + j];
-    if (blk < 0 || blk >= a.num_blocks) continue;
-    const size_t tile = (size_t)blk * a.Hkv + g;
-    uint4 row[NR][2];
+  const int32_t* table = a.block_table + (size_t)b * a.max_blocks_per_seq;
+  int j = (int)(t0 / a.Hkv), g = (int)(t0 - (long long)j * a.Hkv);
+  const int count = (int)min((long long)kTilesPerWave, tiles - t0);
+  // (tiles of a block one after the other in memory; the next one's loads go out first)
+  auto tile_of = [&]() -> long long {
+    const int blk = table[j];
+    return blk < 0 || blk >= a.num_blocks ? -1 : (long long)blk * a.Hkv + g;
+  };
+  auto load = [&](long long tile, uint4(&row)[NR][2]) {
+    const uint16_t* p = a.k_cache + (size_t)max(tile, 0ll) * 16 * D + r * D + u * 16;
 #pragma unroll
     for (int i = 0; i < NR; ++i)
 #pragma unroll
-      for (int c = 0; c < 2; ++c) row[i][c] = ld4(a.k_cache + tile * 16 * D + (r + i * RS) * D + u * 16 + c * 8);
-    block_codes<D>(row, u * 16, u * 16 + 8, lane, a.block_keys + tile * D, a.block_exp + tile);
+      for (int c = 0; c < 2; ++c) row[i][c] = ld4(p + i * RS * D + c * 8);
+  };
+  long long tile = tile_of();
+  uint4 row[NR][2];
+  load(tile, row);
+  for (int k = 0; k < count; ++k) {
+    uint4 next[NR][2];
+    long long next_tile = -1;
+    if (k + 1 < count) {
+      if (++g == a.Hkv) g = 0, ++j;
+      next_tile = tile_of();
+      load(next_tile, next);
+    }
+    if (tile >= 0) block_codes<D>(row, u * 16, u * 16 + 8, lane, a.block_keys + tile * D, a.block_exp + tile);
+    tile = next_tile;
+#pragma unroll
+    for (int i = 0; i < NR; ++i)
+#pragma unroll
+      for (int c = 0; c < 2; ++c) row[i][c] = next[i][c];
   }
 }
 
