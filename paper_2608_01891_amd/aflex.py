@@ -12,6 +12,7 @@ import ctypes
 import gc
 import os
 import re
+import struct
 
 import torch
 
@@ -102,6 +103,18 @@ class AttnSparseArgs(ctypes.Structure):
     _fields_ = [("attn", AttnArgs), ("selected", _p), ("top_blocks", _i)]
 
 
+def _packer(cls):
+    """struct.Struct.pack of an argument block's fields, flattened (a third of a Structure's cost per call)."""
+    def codes(c):
+        return "".join({_p: "P", _i: "i", ctypes.c_float: "f"}.get(f) or codes(f) for _, f in c._fields_)
+    s = codes(cls)
+    return struct.Struct(f"{s}{ctypes.sizeof(cls) - struct.calcsize(s)}x").pack
+
+
+_pack_rope, _pack_block_summary, _pack_block_select, _pack_attn_sparse = map(
+    _packer, (RopeArgs, BlockSummaryArgs, BlockSelectArgs, AttnSparseArgs))
+
+
 class AflexError(RuntimeError):
     def __init__(self, status: int, message: str):
         super().__init__(f"aflex status {status}: {message}")
@@ -150,13 +163,13 @@ def load():
         "aflex_kv_write": [ctypes.POINTER(KvWriteArgs), _p],
         "aflex_pool_streams_create": [ctypes.c_int32, ctypes.POINTER(_p), ctypes.POINTER(_p)],
         "aflex_pool_streams_destroy": [_p, _p],
-        "aflex_rope_append": [ctypes.POINTER(RopeArgs), _p],
-        "aflex_rope_write": [ctypes.POINTER(RopeArgs), _p],
-        "aflex_block_summary": [ctypes.POINTER(BlockSummaryArgs), _p],
-        "aflex_block_select_workspace": [ctypes.POINTER(BlockSelectArgs), _SZ],
-        "aflex_block_select": [ctypes.POINTER(BlockSelectArgs), _p, ctypes.c_size_t, _p],
-        "aflex_attn_sparse_decode_workspace": [ctypes.POINTER(AttnSparseArgs), _SZ],
-        "aflex_attn_sparse_decode": [ctypes.POINTER(AttnSparseArgs), _p, ctypes.c_size_t, _p],
+        "aflex_rope_append": [_p, _p],
+        "aflex_rope_write": [_p, _p],
+        "aflex_block_summary": [_p, _p],
+        "aflex_block_select_workspace": [_p, _SZ],
+        "aflex_block_select": [_p, _p, ctypes.c_size_t, _p],
+        "aflex_attn_sparse_decode_workspace": [_p, _SZ],
+        "aflex_attn_sparse_decode": [_p, _p, ctypes.c_size_t, _p],
     }
     for name, args in sig.items():
         fn = getattr(lib, name)
@@ -613,20 +626,16 @@ def _device_of(t):
     return dev
 
 
-class _On:
-    """The tensors' device as the current one (nothing to do where it is)."""
+def _on_device(f):
+    """Run f(dev, ...) with the device of its tensors as the current one."""
+    get = torch._C._cuda_getDevice
 
-    def __init__(self, dev):
-        self.dev = dev
-
-    def __enter__(self):
-        self.was = torch._C._cuda_getDevice()
-        if self.was != self.dev:
-            torch._C._cuda_setDevice(self.dev)
-
-    def __exit__(self, *exc):
-        if self.was != self.dev:
-            torch._C._cuda_setDevice(self.was)
+    def run(dev, *args):
+        if dev == get():
+            return f(dev, *args)
+        with torch.cuda.device(dev):
+            return f(dev, *args)
+    return run
 
 
 def _empty(stream, dev, *shape, dtype=torch.bfloat16):
@@ -636,66 +645,69 @@ def _empty(stream, dev, *shape, dtype=torch.bfloat16):
         return torch.empty(*shape, dtype=dtype, device=f"cuda:{dev}")
 
 
-def _run_own_ws(name, args, ws, stream):
+def _run_own_ws(name, args, dev, ws, stream):
     """Call an entry point with a workspace on the current device. The default
     one belongs to the (device, stream) that the call runs on, so calls on two
     streams do not share it; while a graph is captured the call gets one of the
     graph's own memory."""
-    ref, handle = ctypes.byref(args), _stream(stream)
-    dev = torch._C._cuda_getDevice()
+    handle = _stream(stream)
     if ws is None:
         if torch.cuda.is_current_stream_capturing():
             ws = Workspace()
         else:
-            ws = _default_ws.setdefault((name, dev, handle), Workspace())
+            key = (name, dev, handle)
+            ws = _default_ws.get(key) or _default_ws.setdefault(key, Workspace())
+    elif stream is not None and ws.buf is not None:
+        ws.buf.record_stream(stream)  # (a caller's may be used on several)
     fn = getattr(_lib, name)
     if ws.buf is not None and ws.buf.get_device() == dev:
-        status = fn(ref, ws.buf.data_ptr(), ws.buf.numel(), handle)
+        status = fn(args, ws.buf.data_ptr(), ws.buf.numel(), handle)
         if status != ERR_WORKSPACE:
             return _check(status)
     n = ctypes.c_size_t()
-    _check(getattr(_lib, name + "_workspace")(ref, ctypes.byref(n)))
+    _check(getattr(_lib, name + "_workspace")(args, ctypes.byref(n)))
     if stream is None:
         buf = ws.get(n.value, f"cuda:{dev}")
     else:
         with torch.cuda.stream(stream):
             buf = ws.get(n.value, f"cuda:{dev}")
-    _check(fn(ref, buf.data_ptr(), buf.numel(), handle))
+    _check(fn(args, buf.data_ptr(), buf.numel(), handle))
 
 
-def _rope(name, a, q, k_new, v_new, rope, cu_seqlens, max_seqlen, interleaved, positions, summary, q_out, stream):
-    lib = load()
-    dev = _device_of(q)
-    T = q.shape[0]
+def _null(t):
+    return 0 if t is None else t.data_ptr()
+
+
+@_on_device
+def _rope(dev, name, a, q, k_new, v_new, rope, cu_seqlens, max_seqlen, interleaved, positions, summary, q_out, stream):
+    T, Hq, Hkv, D = q.shape[0], a.Hq, a.Hkv, a.D
     _want_cache(a, dev)
-    qs = _row_stride(q, "q", T, a.Hq, a.D, dev)
-    ks = _row_stride(k_new, "k_new", T, a.Hkv, a.D, dev)
-    vs = _row_stride(v_new, "v_new", T, a.Hkv, a.D, dev)
-    rot = 0
+    qs = _row_stride(q, "q", T, Hq, D, dev)
+    ks = _row_stride(k_new, "k_new", T, Hkv, D, dev)
+    vs = _row_stride(v_new, "v_new", T, Hkv, D, dev)
+    rows = rot = 0
     if rope is not None:
-        rot = rope.shape[1]
-        _want(rope, "rope", rope.shape[0] * rot, torch.float32, dev)
+        rows, rot = rope.shape
+        _want(rope, "rope", rows * rot, torch.float32, dev)
     if positions is not None:
         _want(positions, "positions", T, torch.int32, dev)
     if cu_seqlens is not None:
         _want(cu_seqlens, "cu_seqlens", a.B + 1, torch.int32, dev)
     elif T != a.B:
         raise ValueError(f"q: expected one row for each of {a.B} sequences, but got {T}")
-    keys = exp = None
+    keys = exp = 0
     if summary is not None:
         _want_summary(a, summary, dev)
         keys, exp = summary.keys.data_ptr(), summary.exp.data_ptr()
-    with _On(dev):
-        if q_out is None:
-            q_out = _empty(stream, dev, T, a.Hq, a.D)
-        else:
-            _want(q_out, "q_out", T * a.Hq * a.D, torch.bfloat16, dev)
-        args = RopeArgs(q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), _ptr(rope), _ptr(positions),
-                        _ptr(cu_seqlens), q_out.data_ptr(), a.k_cache.data_ptr(), a.v_cache.data_ptr(), keys, exp,
-                        a.block_table.data_ptr(), a.context_lens.data_ptr(), a.B, T, a.Hq, a.Hkv, a.D, rot,
-                        int(interleaved), 0 if rope is None else rope.shape[0], max_seqlen, a.block_size,
-                        a.max_blocks, a.num_blocks, qs, ks, vs)
-        _check(getattr(lib, name)(ctypes.byref(args), _stream(stream)))
+    if q_out is None:
+        q_out = _empty(stream, dev, T, Hq, D)
+    else:
+        _want(q_out, "q_out", T * Hq * D, torch.bfloat16, dev)
+    args = _pack_rope(q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), _null(rope), _null(positions),
+                      _null(cu_seqlens), q_out.data_ptr(), a.k_cache.data_ptr(), a.v_cache.data_ptr(), keys, exp,
+                      a.block_table.data_ptr(), a.context_lens.data_ptr(), a.B, T, Hq, Hkv, D, rot, interleaved,
+                      rows, max_seqlen, a.block_size, a.max_blocks, a.num_blocks, qs, ks, vs)
+    _check(getattr(_lib, name)(args, _stream(stream)))
     return q_out
 
 
@@ -705,39 +717,62 @@ def rope_append(a, q, k_new, v_new, rope, interleaved: bool = False, positions=N
     (position ctx-1, or row ``positions[b]`` of ``rope``; rope=None: no rotation). q [B, Hq, D], k_new and
     v_new [B, Hkv, D] may be slices of one projection's output. With ``summary`` (BlockSummary) the blocks
     that get full are summarised. Returns the rotated queries [B, Hq, D]."""
-    return _rope("aflex_rope_append", a, q, k_new, v_new, rope, None, 0, interleaved, positions, summary, q_out,
-                 stream)
+    load()
+    return _rope(_device_of(q), "aflex_rope_append", a, q, k_new, v_new, rope, None, 0, interleaved, positions,
+                 summary, q_out, stream)
 
 
 def rope_write(a, q, k_new, v_new, cu_seqlens, rope, max_seqlen=None, interleaved: bool = False, positions=None,
                summary=None, q_out=None, stream=None):
     """rope_append for packed new tokens: rows cu[b] .. cu[b+1]-1 are the newest of sequence b's context.
     ``max_seqlen`` bounds the prompts' lengths (None: read from cu_seqlens, which waits for the device)."""
+    load()
+    dev = _device_of(q)
     if max_seqlen is None:
         c = cu_seqlens.cpu()
         max_seqlen = int((c[1:] - c[:-1]).max()) if c.numel() > 1 else 0
-    return _rope("aflex_rope_write", a, q, k_new, v_new, rope, cu_seqlens, max_seqlen, interleaved, positions,
+    return _rope(dev, "aflex_rope_write", a, q, k_new, v_new, rope, cu_seqlens, max_seqlen, interleaved, positions,
                  summary, q_out, stream)
+
+
+@_on_device
+def _block_summary(dev, a, summary, stream):
+    _want_cache(a, dev, ("k_cache",))
+    if summary is None:
+        if stream is None:
+            summary = BlockSummary.of(a)
+        else:
+            with torch.cuda.stream(stream):
+                summary = BlockSummary.of(a)
+    _want_summary(a, summary, dev)
+    args = _pack_block_summary(a.k_cache.data_ptr(), summary.keys.data_ptr(), summary.exp.data_ptr(),
+                               a.block_table.data_ptr(), a.context_lens.data_ptr(), a.B, a.Hkv, a.D, a.block_size,
+                               a.max_blocks, a.num_blocks, a.max_context_len)
+    _check(_lib.aflex_block_summary(args, _stream(stream)))
+    return summary
 
 
 def block_summary(a, summary=None, stream=None):
     """Summaries of every full block of a's sequences (for caches written without them), in place."""
-    lib = load()
-    dev = _device_of(a.k_cache)
-    _want_cache(a, dev, ("k_cache",))
-    with _On(dev):
-        if summary is None:
-            if stream is None:
-                summary = BlockSummary.of(a)
-            else:
-                with torch.cuda.stream(stream):
-                    summary = BlockSummary.of(a)
-        _want_summary(a, summary, dev)
-        args = BlockSummaryArgs(a.k_cache.data_ptr(), summary.keys.data_ptr(), summary.exp.data_ptr(),
-                                a.block_table.data_ptr(), a.context_lens.data_ptr(), a.B, a.Hkv, a.D, a.block_size,
-                                a.max_blocks, a.num_blocks, a.max_context_len)
-        _check(lib.aflex_block_summary(ctypes.byref(args), _stream(stream)))
-    return summary
+    load()
+    return _block_summary(_device_of(a.k_cache), a, summary, stream)
+
+
+@_on_device
+def _block_select(dev, a, q, summary, top_blocks, sink_blocks, recent_blocks, out, stream, ws):
+    _want_cache(a, dev, ())
+    _want_summary(a, summary, dev)
+    _want(q, "q", a.B * a.Hq * a.D, torch.bfloat16, dev)
+    if out is None:
+        out = _empty(stream, dev, a.B, a.Hkv, max(top_blocks, 0), dtype=torch.int32)
+    else:
+        _want(out, "out", a.B * a.Hkv * top_blocks, torch.int32, dev)
+    args = _pack_block_select(q.data_ptr(), summary.keys.data_ptr(), summary.exp.data_ptr(),
+                              a.block_table.data_ptr(), a.context_lens.data_ptr(), out.data_ptr(), a.B, a.Hq, a.Hkv,
+                              a.D, a.block_size, a.max_blocks, a.num_blocks, a.max_context_len, top_blocks,
+                              sink_blocks, recent_blocks)
+    _run_own_ws("aflex_block_select", args, dev, ws, stream)
+    return out
 
 
 def block_select(a, q, summary, top_blocks: int, sink_blocks: int = 1, recent_blocks: int = 1, out=None, stream=None,
@@ -746,20 +781,23 @@ def block_select(a, q, summary, top_blocks: int, sink_blocks: int = 1, recent_bl
     the first ``sink_blocks``, the last ``recent_blocks`` and the best scoring others. int32 [B, Hkv, top_blocks],
     ascending, -1 behind a shorter list."""
     load()
-    dev = _device_of(q)
-    _want_cache(a, dev, ())
-    _want_summary(a, summary, dev)
+    return _block_select(_device_of(q), a, q, summary, top_blocks, sink_blocks, recent_blocks, out, stream, ws)
+
+
+@_on_device
+def _attn_sparse(dev, a, selected, q, out, scale, stream, ws):
+    _want_cache(a, dev)
     _want(q, "q", a.B * a.Hq * a.D, torch.bfloat16, dev)
-    with _On(dev):
-        if out is None:
-            out = _empty(stream, dev, a.B, a.Hkv, max(top_blocks, 0), dtype=torch.int32)
-        else:
-            _want(out, "out", a.B * a.Hkv * top_blocks, torch.int32, dev)
-        args = BlockSelectArgs(q.data_ptr(), summary.keys.data_ptr(), summary.exp.data_ptr(),
-                               a.block_table.data_ptr(), a.context_lens.data_ptr(), out.data_ptr(), a.B, a.Hq, a.Hkv,
-                               a.D, a.block_size, a.max_blocks, a.num_blocks, a.max_context_len, top_blocks,
-                               sink_blocks, recent_blocks)
-        _run_own_ws("aflex_block_select", args, ws, stream)
+    top = selected.shape[-1]
+    _want(selected, "selected", a.B * a.Hkv * top, torch.int32, dev)
+    if out is None:
+        out = _empty(stream, dev, a.B, a.Hq, a.D)
+    else:
+        _want(out, "out", a.B * a.Hq * a.D, torch.bfloat16, dev)
+    args = _pack_attn_sparse(q.data_ptr(), a.k_cache.data_ptr(), a.v_cache.data_ptr(), a.block_table.data_ptr(),
+                             a.context_lens.data_ptr(), out.data_ptr(), a.B, a.Hq, a.Hkv, a.D, a.block_size,
+                             a.max_blocks, a.num_blocks, a.max_context_len, scale, 0, selected.data_ptr(), top)
+    _run_own_ws("aflex_attn_sparse_decode", args, dev, ws, stream)
     return out
 
 
@@ -767,18 +805,4 @@ def attn_sparse_decode(a, selected, q=None, out=None, scale: float = 0.0, stream
     """Decode attention of q (default a.q) [B, Hq, D] over the blocks that selected [B, Hkv, top_blocks] lists."""
     load()
     q = a.q if q is None else q
-    dev = _device_of(q)
-    _want_cache(a, dev)
-    _want(q, "q", a.B * a.Hq * a.D, torch.bfloat16, dev)
-    top = selected.shape[-1]
-    _want(selected, "selected", a.B * a.Hkv * top, torch.int32, dev)
-    with _On(dev):
-        if out is None:
-            out = _empty(stream, dev, a.B, a.Hq, a.D)
-        else:
-            _want(out, "out", a.B * a.Hq * a.D, torch.bfloat16, dev)
-        attn = AttnArgs(q.data_ptr(), a.k_cache.data_ptr(), a.v_cache.data_ptr(), a.block_table.data_ptr(),
-                        a.context_lens.data_ptr(), out.data_ptr(), a.B, a.Hq, a.Hkv, a.D, a.block_size, a.max_blocks,
-                        a.num_blocks, a.max_context_len, scale, 0)
-        _run_own_ws("aflex_attn_sparse_decode", AttnSparseArgs(attn, selected.data_ptr(), top), ws, stream)
-    return out
+    return _attn_sparse(_device_of(q), a, selected, q, out, scale, stream, ws)

@@ -10,6 +10,7 @@
 // nothing.
 #include "common.h"
 #include "kernels.h"
+#include "kv_tile.h"
 #include "profile.h"
 
 namespace aflex {
@@ -35,10 +36,6 @@ __global__ __launch_bounds__(256) void kv_append_kernel(aflex_kv_append_args a) 
   uint16_t* vdst = a.v_cache + (((size_t)blk * a.Hkv + h) * a.D + c * 8) * 16 + o;
 #pragma unroll
   for (int e = 0; e < 8; ++e) vdst[e * 16] = static_cast<uint16_t>(w[e >> 1] >> ((e & 1) * 16));
-}
-
-__device__ __forceinline__ uint32_t chunk_word(const uint4& v, int i) {
-  return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w;
 }
 
 // Packed multi-token write: one work-group per (cache block slot, sequence, K or
@@ -85,36 +82,8 @@ __global__ __launch_bounds__(XCHG ? 256 : 1024) void kv_write_kernel(aflex_kv_wr
     for (int o = 0; o < 16; ++o)
       if (o >= o0 && o < o1) *reinterpret_cast<uint4*>(kc + (size_t)o * a.D) = row[o];
   } else if (!FEW && o1 - o0 == 16) {
-    uint4 out[16];  // this thread's 8 rows of the V tile, 256 contiguous bytes
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const uint32_t sel = (e & 1) ? 0x07060302u : 0x05040100u;
-      uint32_t r[8];
-#pragma unroll
-      for (int o = 0; o < 8; ++o)
-        r[o] = __builtin_amdgcn_perm(chunk_word(row[2 * o + 1], e >> 1), chunk_word(row[2 * o], e >> 1), sel);
-      out[2 * e] = make_uint4(r[0], r[1], r[2], r[3]);
-      out[2 * e + 1] = make_uint4(r[4], r[5], r[6], r[7]);
-    }
-    const int t = threadIdx.x & 15;
-    if (XCHG && (int)(threadIdx.x | 15) < a.Hkv * chunks) {
-      // 16 threads (4 KiB of contiguous V rows) exchange through LDS, so that
-      // each store of theirs covers 256 contiguous bytes instead of 16 in every
-      // 256. Piece x of thread t sits at x ^ t.
-      extern __shared__ __attribute__((aligned(16))) uint8_t sm[];
-      uint8_t* grp = sm + (threadIdx.x >> 4) * 4096;
-#pragma unroll
-      for (int x = 0; x < 16; ++x) *reinterpret_cast<uint4*>(grp + t * 256 + ((x ^ t) << 4)) = out[x];
-      __builtin_amdgcn_s_waitcnt(0xc07f);  // lgkmcnt(0): the 16 threads are lanes of one wave
-      __builtin_amdgcn_wave_barrier();
-      uint16_t* vt = vc - t * 128;  // the first thread's bytes
-#pragma unroll
-      for (int i = 0; i < 16; ++i)
-        *reinterpret_cast<uint4*>(vt + i * 128 + t * 8) = *reinterpret_cast<const uint4*>(grp + i * 256 + ((t ^ i) << 4));
-    } else {
-#pragma unroll
-      for (int x = 0; x < 16; ++x) *reinterpret_cast<uint4*>(vc + x * 8) = out[x];
-    }
+    extern __shared__ __attribute__((aligned(16))) uint8_t sm[];
+    store_v_rows(row, vc, XCHG && (int)(threadIdx.x | 15) < a.Hkv * chunks, sm);
   } else {
 #pragma unroll
     for (int o = 0; o < 16; ++o)

@@ -15,6 +15,7 @@
 // the tile that the summary is made of.
 #include "block_codes.h"
 #include "kernels.h"
+#include "kv_tile.h"
 #include "profile.h"
 
 namespace aflex {
@@ -174,7 +175,11 @@ __global__ __launch_bounds__(256) void rope_append_kernel(aflex_rope_args a) {
 // logical block max(start, 0) / 16 + jj, start = ctx_b - n_b, as in the plain
 // cache write. The parts share its 16 rows: V (transposed into the
 // token-fastest tile), the key heads, the query heads.
+// A wave takes up to kHeadsPerWave heads with the angles it has loaded, one where
+// that leaves fewer waves than the GPU holds (113 tokens, 32 + 8 heads: 10.5 us
+// with four heads in a row).
 constexpr int kHeadsPerWave = 4;
+constexpr long long kManyWaves = 16384;
 
 struct Slot {
   int blk;         // pool block, or -1
@@ -210,38 +215,46 @@ __device__ __forceinline__ int slot_pos(const aflex_rope_args& a, const Slot& s,
 }
 
 template <int D, bool INTER>
-__global__ __launch_bounds__(256) void rope_write_kernel(aflex_rope_args a, int vparts, int kparts) {
+__global__ __launch_bounds__(256) void rope_write_kernel(aflex_rope_args a, int vparts, int kparts,
+                                                            int per_wave) {
   constexpr int U = TileLanes<D>::U, NR = TileLanes<D>::NR, RS = TileLanes<D>::RS;
   Slot s;
   if (!find_slot(a, blockIdx.z, blockIdx.x, s)) return;
   int part = blockIdx.y;
   const int rot = a.rotary_dim;
   if (part < vparts) {
-    // V: a thread per (kv head, 8 channels) with the block's rows
+    // V: a thread per (kv head, 8 channels) with the block's rows, all loaded
+    // before the first is stored
     if (s.blk < 0) return;
     constexpr int C = D / 8;
+    extern __shared__ __attribute__((aligned(16))) uint8_t sm[];
     const int t = part * 256 + threadIdx.x;
     const int g = t / C, c = t % C;
     if (g >= a.Hkv) return;
     const uint16_t* src = a.v_new + (size_t)g * D + c * 8;
     uint16_t* vt = a.v_cache + (((size_t)s.blk * a.Hkv + g) * D + c * 8) * 16;
-#pragma unroll 4
-    for (int o = 0; o < 16; ++o) {
-      if (slot_pos(a, s, o) < 0) continue;
-      const uint4 v = ld4(src + (size_t)(s.src + o) * a.v_stride);
-      const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+    uint4 row[16];
+    uint32_t live = 0;  // rows that are written, the same for all threads
 #pragma unroll
-      for (int e = 0; e < 8; ++e) vt[e * 16 + o] = (uint16_t)(w[e >> 1] >> ((e & 1) * 16));
-    }
+    for (int o = 0; o < 16; ++o) live |= slot_pos(a, s, o) >= 0 ? 1u << o : 0u;
+    live = __builtin_amdgcn_readfirstlane(live);
+    if (live == 0) return;
+    // (rows that are not written repeat one that is)
+    const int first = __builtin_ctz(live);
+#pragma unroll
+    for (int o = 0; o < 16; ++o) row[o] = ld4(src + (size_t)(s.src + (live >> o & 1 ? o : first)) * a.v_stride);
+    if (live == 0xffffu)
+      store_v_rows<true>(row, vt, (t | 15) < a.Hkv * C, sm);
+    else
+      store_v_part(row, vt, live);
     return;
   }
   part -= vparts;
   const bool key = part < kparts;
   if (!key) part -= kparts;
-  if (key && s.blk < 0) return;
   const int heads = key ? a.Hkv : a.Hq;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int h0 = (part * 4 + wave) * kHeadsPerWave;
+  const int h0 = (part * 4 + wave) * per_wave;
   const int u = lane % U, r = lane / U;
   int d0, d1;
   unit_channels<INTER>(u, rot, d0, d1);
@@ -252,12 +265,12 @@ __global__ __launch_bounds__(256) void rope_write_kernel(aflex_rope_args a, int 
     pos[i] = slot_pos(a, s, r + i * RS);
     if (pos[i] >= 0 && u * 16 < rot) an[i] = load_angles(a.rope, pos[i], rot, u);
   }
-  const bool full = key && a.block_keys && slot_pos(a, s, 15) >= 0;  // this write fills the block
-  for (int h = h0; h < min(h0 + kHeadsPerWave, heads); ++h) {
+  const bool full = key && s.blk >= 0 && a.block_keys && slot_pos(a, s, 15) >= 0;  // this write fills the block
+  for (int h = h0; h < min(h0 + per_wave, heads); ++h) {
     uint4 row[NR][2];
     const uint16_t* src = (key ? a.k_new : a.q) + (size_t)h * D;
     const size_t stride = key ? a.k_stride : a.q_stride;
-    const size_t tile = key ? (size_t)s.blk * a.Hkv + h : 0;
+    const size_t tile = key ? (size_t)max(s.blk, 0) * a.Hkv + h : 0;
     uint16_t* kt = a.k_cache + tile * 16 * D;
 #pragma unroll
     for (int i = 0; i < NR; ++i) {
@@ -267,6 +280,7 @@ __global__ __launch_bounds__(256) void rope_write_kernel(aflex_rope_args a, int 
         row[i][0] = ld4(p + d0);
         row[i][1] = ld4(p + d1);
         if (u * 16 < rot) rotate_unit<INTER>(row[i][0], row[i][1], an[i]);
+        if (key && s.blk < 0) continue;
         uint16_t* dst = key ? kt + o * D : a.q_out + ((size_t)(s.src + o) * a.Hq + h) * D;
         st4(dst + d0, row[i][0]);
         st4(dst + d1, row[i][1]);
@@ -360,18 +374,21 @@ hipError_t launch_rope_write(const aflex_rope_args& in, hipStream_t stream) {
   if (in.T == 0 || in.max_seqlen == 0) return hipSuccess;
   const aflex_rope_args a = with_strides(in);
   const int vparts = (a.Hkv * (a.D / 8) + 255) / 256;
-  const int per = 4 * kHeadsPerWave;
+  const int slots = (a.max_seqlen + 15) / 16 + 1;
+  const int per_wave = (long long)slots * a.B * (a.Hq + a.Hkv) >= kManyWaves * kHeadsPerWave ? kHeadsPerWave : 1;
+  const int per = 4 * per_wave;
   const int kparts = (a.Hkv + per - 1) / per, qparts = (a.Hq + per - 1) / per;
-  const dim3 grid((a.max_seqlen + 15) / 16 + 1, vparts + kparts + qparts, a.B);
+  const dim3 grid(slots, vparts + kparts + qparts, a.B);
+  const size_t lds = 256 / 16 * 2048;  // the exchange of V rows
   ProfScope ps("rope_write", stream);
   if (a.D == 128 && a.interleaved)
-    rope_write_kernel<128, true><<<grid, 256, 0, stream>>>(a, vparts, kparts);
+    rope_write_kernel<128, true><<<grid, 256, lds, stream>>>(a, vparts, kparts, per_wave);
   else if (a.D == 128)
-    rope_write_kernel<128, false><<<grid, 256, 0, stream>>>(a, vparts, kparts);
+    rope_write_kernel<128, false><<<grid, 256, lds, stream>>>(a, vparts, kparts, per_wave);
   else if (a.interleaved)
-    rope_write_kernel<64, true><<<grid, 256, 0, stream>>>(a, vparts, kparts);
+    rope_write_kernel<64, true><<<grid, 256, lds, stream>>>(a, vparts, kparts, per_wave);
   else
-    rope_write_kernel<64, false><<<grid, 256, 0, stream>>>(a, vparts, kparts);
+    rope_write_kernel<64, false><<<grid, 256, lds, stream>>>(a, vparts, kparts, per_wave);
   return hipGetLastError();
 }
 
