@@ -365,26 +365,33 @@ __device__ __forceinline__ void find_bounds(const Each& each, int& need, int pas
     if (threadIdx.x < 64) {  // one wave: lane l has 32 bins, from the top
       const int row = kBins / 32 - 1 - lane;
       const uint4* mine = reinterpret_cast<const uint4*>(hist + row * 32);
-      int sum = 0;
+      int four[8], sum = 0;  // of 4 bins each, from the top
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const uint4 v = mine[i ^ (row & 7)];
-        sum += v.x + v.y + v.z + v.w;
+        const uint4 v = mine[(7 - i) ^ (row & 7)];
+        four[i] = v.x + v.y + v.z + v.w;
+        sum += four[i];
       }
       int before = wave_scan(sum) - sum;
       if (before < need && need <= before + sum) {
-        int at = 0, above = before, inside = 0;
-        for (int i = 0; i < 8; ++i) {
-          const uint4 v = mine[(7 - i) ^ (row & 7)];
-          const int c[4] = {(int)v.w, (int)v.z, (int)v.y, (int)v.x};
+        int group = 0, start = before;
 #pragma unroll
-          for (int m = 0; m < 4; ++m) {
-            const bool here = before < need && need <= before + c[m];
-            at = here ? 4 * i + m : at;
-            above = here ? before : above;
-            inside = here ? c[m] : inside;
-            before += c[m];
-          }
+        for (int i = 0; i < 8; ++i) {
+          const bool here = before < need && need <= before + four[i];
+          group = here ? i : group;
+          start = here ? before : start;
+          before += four[i];
+        }
+        const uint4 v = mine[(7 - group) ^ (row & 7)];
+        const int c[4] = {(int)v.w, (int)v.z, (int)v.y, (int)v.x};
+        int at = 0, above = start, inside = 0;
+#pragma unroll
+        for (int m = 0; m < 4; ++m) {
+          const bool here = start < need && need <= start + c[m];
+          at = here ? 4 * group + m : at;
+          above = here ? start : above;
+          inside = here ? c[m] : inside;
+          start += c[m];
         }
         sh.bin = kBins - 1 - 32 * lane - at;
         sh.above = above;

@@ -266,30 +266,45 @@ __global__ __launch_bounds__(256) void rope_write_kernel(aflex_rope_args a, int 
     if (pos[i] >= 0 && u * 16 < rot) an[i] = load_angles(a.rope, pos[i], rot, u);
   }
   const bool full = key && s.blk >= 0 && a.block_keys && slot_pos(a, s, 15) >= 0;  // this write fills the block
-  for (int h = h0; h < min(h0 + per_wave, heads); ++h) {
-    uint4 row[NR][2];
-    const uint16_t* src = (key ? a.k_new : a.q) + (size_t)h * D;
-    const size_t stride = key ? a.k_stride : a.q_stride;
-    const size_t tile = key ? (size_t)max(s.blk, 0) * a.Hkv + h : 0;
-    uint16_t* kt = a.k_cache + tile * 16 * D;
+  const size_t stride = key ? a.k_stride : a.q_stride;
+  const uint16_t* base = key ? a.k_new : a.q;
+  uint16_t* tiles = a.k_cache + (size_t)max(s.blk, 0) * a.Hkv * 16 * D;  // key: of the block's heads
+  // Rows of head h: new ones, and the older keys of a block that this write fills.
+  auto load = [&](int h, uint4(&row)[NR][2]) {
 #pragma unroll
     for (int i = 0; i < NR; ++i) {
       const int o = r + i * RS;
-      if (pos[i] >= 0) {
-        const uint16_t* p = src + (size_t)(s.src + o) * stride;
+      const uint16_t* p = pos[i] >= 0 ? base + (size_t)(s.src + o) * stride + (size_t)h * D
+                                      : tiles + ((size_t)h * 16 + o) * D;
+      if (pos[i] >= 0 || full) {
         row[i][0] = ld4(p + d0);
         row[i][1] = ld4(p + d1);
-        if (u * 16 < rot) rotate_unit<INTER>(row[i][0], row[i][1], an[i]);
-        if (key && s.blk < 0) continue;
-        uint16_t* dst = key ? kt + o * D : a.q_out + ((size_t)(s.src + o) * a.Hq + h) * D;
-        st4(dst + d0, row[i][0]);
-        st4(dst + d1, row[i][1]);
-      } else if (full) {  // an older key of the block that this write fills
-        row[i][0] = ld4(kt + o * D + d0);
-        row[i][1] = ld4(kt + o * D + d1);
       }
     }
-    if (full) block_codes<D>(row, d0, d1, lane, a.block_keys + tile * D, a.block_exp + tile);
+  };
+  const int h1 = min(h0 + per_wave, heads);
+  if (h0 >= h1) return;
+  uint4 next[NR][2];
+  load(h0, next);
+  for (int h = h0; h < h1; ++h) {
+    uint4 row[NR][2];
+#pragma unroll
+    for (int i = 0; i < NR; ++i) row[i][0] = next[i][0], row[i][1] = next[i][1];
+    if (h + 1 < h1) load(h + 1, next);
+#pragma unroll
+    for (int i = 0; i < NR; ++i) {
+      const int o = r + i * RS;
+      if (pos[i] < 0) continue;
+      if (u * 16 < rot) rotate_unit<INTER>(row[i][0], row[i][1], an[i]);
+      if (key && s.blk < 0) continue;
+      uint16_t* dst = key ? tiles + ((size_t)h * 16 + o) * D : a.q_out + ((size_t)(s.src + o) * a.Hq + h) * D;
+      st4(dst + d0, row[i][0]);
+      st4(dst + d1, row[i][1]);
+    }
+    if (full) {
+      const size_t tile = (size_t)s.blk * a.Hkv + h;
+      block_codes<D>(row, d0, d1, lane, a.block_keys + tile * D, a.block_exp + tile);
+    }
   }
 }
 
