@@ -99,7 +99,8 @@ typedef struct aflex_block_summary_args {
   int32_t max_context_len;     /* host-known bound on the context lengths; larger device values are clamped */
 } aflex_block_summary_args;
 
-/* Supported: D in {64, 128}, block_size == 16, B <= 65535. No workspace.      */
+/* Supported: D in {64, 128}, block_size == 16, B <= 65535,                    */
+/* max_context_len / 16 * Hkv < 2^30. No workspace.                            */
 aflex_status aflex_block_summary(const aflex_block_summary_args *a, aflex_stream stream);
 
 /* ------------------------------------------------------------------------ */

@@ -138,8 +138,8 @@ aflex_status aflex_block_summary(const aflex_block_summary_args* a, aflex_stream
   if (s == AFLEX_OK) s = check_context(who, a->max_context_len, a->max_blocks_per_seq);
   if (s != AFLEX_OK) return s;
   REQUIRE(a->B <= 65535, AFLEX_ERR_UNSUPPORTED, "%s: B %d above 65535", who, a->B);
-  REQUIRE((a->max_context_len / 16ll) * a->Hkv < (1ll << 34), AFLEX_ERR_UNSUPPORTED,
-          "%s: max_context_len / 16 * Hkv must stay below 2^34", who);
+  REQUIRE((a->max_context_len / 16ll) * a->Hkv < (1ll << 30), AFLEX_ERR_UNSUPPORTED,
+          "%s: max_context_len / 16 * Hkv must stay below 2^30", who);
   REQUIRE(aligned16(a->k_cache) && aligned16(a->block_keys), AFLEX_ERR_ALIGNMENT,
           "%s: k_cache and block_keys must be 16-byte aligned", who);
   REQUIRE(aligned4(a->block_table) && aligned4(a->context_lens), AFLEX_ERR_ALIGNMENT,

@@ -689,7 +689,13 @@ constexpr int kWideWaves = 12;
 // Work-groups per unit from which the merge shares a unit's pieces among lanes.
 constexpr int kManyPieces = 8;
 
-static int unit_cost(const aflex_attn_args& a) { return a.split_tokens > 0 ? 0 : kUnitCost; }
+// Lists of chosen blocks of few units are cut into many pieces each: the charge
+// would only leave work-groups without blocks (one sequence of 8 KV heads, 256
+// blocks each: 12.3 us without it, 13.8 with; 512 units of 128 blocks: 100.8 and
+// 99.8).
+static int unit_cost(const aflex_attn_args& a, int top = 0) {
+  return a.split_tokens > 0 || (top > 0 && (long long)a.B * a.Hkv * kManyPieces <= resident_wgs()) ? 0 : kUnitCost;
+}
 
 // Bound on a unit's blocks: those of the longest context, or of the longest list
 // of chosen ones (top > 0).
@@ -699,7 +705,7 @@ static int max_unit_blocks(const aflex_attn_args& a, int top) {
 }
 
 static long long work_bound(const aflex_attn_args& a, int top = 0) {
-  return (long long)a.B * a.Hkv * (max_unit_blocks(a, top) + unit_cost(a));
+  return (long long)a.B * a.Hkv * (max_unit_blocks(a, top) + unit_cost(a, top));
 }
 
 // Contexts of at most this many tokens take one work-group per (sequence, kv
@@ -835,6 +841,7 @@ hipError_t launch_attn_sparse(const aflex_attn_sparse_args& s, void* ws, hipStre
   const int P = attn_grid(a, false, s.top_blocks);
   AttnParams p = attn_params(a, ws, P);
   p.rounds = !unit && P == resident_wgs() && P % 3 == 0 ? 3 : 1;
+  p.unit_cost = unit_cost(a, s.top_blocks);
   p.sel = s.selected;
   p.top = s.top_blocks;
   {

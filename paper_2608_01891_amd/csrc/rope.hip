@@ -176,8 +176,8 @@ __global__ __launch_bounds__(256) void rope_append_kernel(aflex_rope_args a) {
 // cache write. The parts share its 16 rows: V (transposed into the
 // token-fastest tile), the key heads, the query heads.
 // A wave takes up to kHeadsPerWave heads with the angles it has loaded, one where
-// that leaves fewer waves than the GPU holds (113 tokens, 32 + 8 heads: 10.5 us
-// with four heads in a row).
+// that leaves few waves (113 tokens, 32 + 8 heads: 5.3 us, with four heads in a
+// row 7.5).
 constexpr int kHeadsPerWave = 4;
 constexpr long long kManyWaves = 16384;
 
@@ -310,7 +310,9 @@ __global__ __launch_bounds__(256) void rope_write_kernel(aflex_rope_args a, int 
 
 // ---------------------------------------------------------------------------
 // Summaries of full blocks that are in the cache: a wave per tile.
-constexpr int kTilesPerWave = 4;
+// Tiles in a row per wave (375 MB of keys and summaries / 16 short contexts: one
+// tile 77.3 / 5.5 us, two 76.3 / 6.3, four 78.7 / 7.6, eight 82.2 / 11.9).
+constexpr int kTilesPerWave = 2;
 
 template <int D>
 __global__ __launch_bounds__(256, 6) void block_summary_kernel(aflex_block_summary_args a) {
@@ -318,14 +320,13 @@ __global__ __launch_bounds__(256, 6) void block_summary_kernel(aflex_block_summa
   const int lane = threadIdx.x & 63;
   const int b = blockIdx.y;
   const int ctx = min(max(a.context_lens[b], 0), a.max_context_len);
-  const long long tiles = (long long)(ctx / 16) * a.Hkv;
-  const long long t0 =
-      ((long long)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * kTilesPerWave;
+  const int tiles = ctx / 16 * a.Hkv;
+  const int t0 = (int)(blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * kTilesPerWave;
   if (t0 >= tiles) return;
   const int u = lane % U, r = lane / U;
   const int32_t* table = a.block_table + (size_t)b * a.max_blocks_per_seq;
-  int j = (int)(t0 / a.Hkv), g = (int)(t0 - (long long)j * a.Hkv);
-  const int count = (int)min((long long)kTilesPerWave, tiles - t0);
+  int j = t0 / a.Hkv, g = t0 - j * a.Hkv;
+  const int count = min(kTilesPerWave, tiles - t0);
   // (tiles of a block one after the other in memory; the next one's loads go out first)
   auto tile_of = [&]() -> long long {
     const int blk = table[j];

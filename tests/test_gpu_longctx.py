@@ -328,6 +328,41 @@ def test_block_select_ties_and_odd_values(gpu_lib):
             _choice(43 + seed, [900, 640, 1500], heads, top, 2, 2, edit=edit)
 
 
+@pytest.mark.parametrize("heads", HEADS + [(16, 1, 64), (32, 2, 128), (18, 9, 64)])
+@pytest.mark.parametrize("top,sink,recent", [(9, 1, 2), (200, 0, 1)])
+def test_block_select_ragged_with_one_long(gpu_lib, heads, top, sink, recent):
+    _choice(48, [17000, 300, 0, 16400, 1, 3300, 63, 4096], heads, top, sink, recent)
+
+
+@pytest.mark.parametrize("n", [1100, 5000, 33000])
+@pytest.mark.parametrize("top", [64, 1500])
+def test_block_select_long_with_equal_scores(gpu_lib, n, top):
+    """More equal scores than the short lists hold, and a few that stand out at the ends."""
+    def equal(a, s):
+        s.keys.fill_(1), s.exp.fill_(-7)
+
+    def two(a, s):
+        equal(a, s)
+        s.exp[a.block_table[0, 5::7].long()] = -6
+        s.exp[a.block_table[0, n - 3].long()] = -8
+
+    for edit in (equal, two):
+        _choice(49, [16 * n - 5], (4, 1, 64), top, 1, 1, edit=edit)
+
+
+def test_block_select_heads_far_apart_in_size(gpu_lib):
+    """Heads of one group whose scales differ by more than fp32's range, both with whole codes."""
+    def far(a, s):
+        a.q[:, 0], a.q[:, 1] = a.q[:, 0] * 1e30, a.q[:, 1].abs() * -1e-25
+        a.q[0, 2:4] *= 1e-20
+        s.exp[::2] = -118
+        s.exp[1::5] = 100
+        s.keys[::3] = 0
+
+    for ctx in ([900, 640], [17000, 400]):
+        _choice(50, ctx, (8, 2, 128), 12, 1, 1, edit=far)
+
+
 def test_block_select_takes_no_more_than_the_host_bound(gpu_lib):
     """Device contexts over max_context_len are cut to it, negative ones are empty."""
     a = synth.custom_attention(47, 3, 8, 2, 64, [320, 100, 300], ctx_hi=320)
