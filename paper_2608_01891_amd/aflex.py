@@ -122,6 +122,7 @@ class AflexError(RuntimeError):
 
 
 _lib = None
+_dense = _rows = None  # of _tensor_args (see load)
 _SZ = ctypes.POINTER(ctypes.c_size_t)
 
 
@@ -134,11 +135,17 @@ def exported_names(header=HEADER):
 
 def load():
     """Open the built library (cached). Raises if it has not been built."""
-    global _lib
+    global _lib, _dense, _rows
     if _lib is not None:
         return _lib
     if not os.path.exists(LIB_PATH):
         raise RuntimeError(f"{LIB_PATH} is missing: build it with `python -m paper_2608_01891_amd.build`")
+    try:
+        from . import _tensor_args
+    except ImportError as e:
+        raise RuntimeError(f"{_PKG}/_tensor_args.so cannot be loaded: build it with "
+                           "`python -m paper_2608_01891_amd.build`") from e
+    _dense, _rows = _tensor_args.dense, _tensor_args.rows
     lib = ctypes.CDLL(LIB_PATH)
     AP, FP = ctypes.POINTER(AttnArgs), ctypes.POINTER(FfnArgs)
     I32P = ctypes.POINTER(ctypes.c_int32)
@@ -564,8 +571,9 @@ def af_layer_step(a, w, layer, k: int, mb_sizes, L: int = 1, y=None, stream_a=No
 
 # --------------------------------------------------------------------------
 # Long-context operators (include/aflex_longctx.h). These check what the C
-# interface cannot see (types, sizes, devices, strides), run on the device of
-# their tensors, and keep a default workspace per stream; outputs that they
+# interface cannot see (types, sizes, devices, strides; in _tensor_args, since
+# in Python the checks took longer than the rest of a call), run on the device
+# of their tensors, and keep a default workspace per stream; outputs that they
 # allocate belong to the stream they run on.
 class BlockSummary:
     """Key summaries of a cache's blocks: ``keys`` int8 [num_blocks, Hkv, D] and
@@ -590,48 +598,18 @@ def rope_table(positions: int, rotary_dim: int, base: float = 10000.0, device="c
     return torch.cat([ang.cos(), ang.sin()], 1).float().to(device)
 
 
-def _want(t, name, numel, dtype, dev):
-    """A dense tensor of the cache's device, of this many elements."""
-    if t.dtype is not dtype or t.numel() != numel or not t.is_contiguous() or t.get_device() != dev:
-        raise ValueError(f"{name}: expected {numel} dense {dtype} elements on cuda:{dev}, but got {tuple(t.shape)} "
-                         f"{t.dtype} on {t.device}, strides {t.stride()}")
-
-
-def _want_cache(a, dev, pools=("k_cache", "v_cache")):
-    for name in pools:
-        _want(getattr(a, name), name, a.num_blocks * a.Hkv * 16 * a.D, torch.bfloat16, dev)
-    _want(a.block_table, "block_table", a.B * a.max_blocks, torch.int32, dev)
-    _want(a.context_lens, "context_lens", a.B, torch.int32, dev)
-
-
-def _want_summary(a, s, dev):
-    _want(s.keys, "summary keys", a.num_blocks * a.Hkv * a.D, torch.int8, dev)
-    _want(s.exp, "summary exponents", a.num_blocks * a.Hkv, torch.int8, dev)
-
-
-def _row_stride(t, name, T, H, D, dev):
-    """Elements between the token rows of t [T, H, D], whose heads are dense."""
-    st = t.stride()
-    if (t.dtype is not torch.bfloat16 or t.shape != (T, H, D) or t.get_device() != dev
-            or st[2] != 1 or (st[1] != D and H > 1) or (T > 1 and st[0] < H * D)):
-        raise ValueError(f"{name}: expected bf16 [{T}, {H}, {D}] on cuda:{dev} with dense, disjoint rows, but got "
-                         f"{tuple(t.shape)} {t.dtype} on {t.device}, strides {st}")
-    return st[0] if T > 1 else 0
-
-
-def _device_of(t):
-    dev = t.get_device()
-    if dev < 0:
-        _need_gpu(t.device)
-    return dev
+_BF16, _F32, _I32, _I8 = range(4)  # type codes of _tensor_args.dense
 
 
 def _on_device(f):
-    """Run f(dev, ...) with the device of its tensors as the current one."""
-    get = torch._C._cuda_getDevice
-
-    def run(dev, *args):
-        if dev == get():
+    """f(dev, ...) from a function of a tensor on that device: with it as the current device, the library loaded."""
+    def run(t, *args):
+        if _lib is None:
+            load()
+        dev = t.get_device()
+        if dev < 0:
+            _need_gpu(t.device)
+        if dev == torch._C._cuda_getDevice():
             return f(dev, *args)
         with torch.cuda.device(dev):
             return f(dev, *args)
@@ -674,39 +652,28 @@ def _run_own_ws(name, args, dev, ws, stream):
     _check(fn(args, buf.data_ptr(), buf.numel(), handle))
 
 
-def _null(t):
-    return 0 if t is None else t.data_ptr()
-
-
 @_on_device
 def _rope(dev, name, a, q, k_new, v_new, rope, cu_seqlens, max_seqlen, interleaved, positions, summary, q_out, stream):
-    T, Hq, Hkv, D = q.shape[0], a.Hq, a.Hkv, a.D
-    _want_cache(a, dev)
-    qs = _row_stride(q, "q", T, Hq, D, dev)
-    ks = _row_stride(k_new, "k_new", T, Hkv, D, dev)
-    vs = _row_stride(v_new, "v_new", T, Hkv, D, dev)
-    rows = rot = 0
-    if rope is not None:
-        rows, rot = rope.shape
-        _want(rope, "rope", rows * rot, torch.float32, dev)
-    if positions is not None:
-        _want(positions, "positions", T, torch.int32, dev)
-    if cu_seqlens is not None:
-        _want(cu_seqlens, "cu_seqlens", a.B + 1, torch.int32, dev)
-    elif T != a.B:
-        raise ValueError(f"q: expected one row for each of {a.B} sequences, but got {T}")
-    keys = exp = 0
-    if summary is not None:
-        _want_summary(a, summary, dev)
-        keys, exp = summary.keys.data_ptr(), summary.exp.data_ptr()
+    B, T, Hq, Hkv, D, blocks = a.B, q.shape[0], a.Hq, a.Hkv, a.D, a.num_blocks
+    if cu_seqlens is None and T != B:
+        raise ValueError(f"q: expected one row for each of {B} sequences, but got {T}")
+    qp, qs = _rows(dev, "q", q, T, Hq, D)
+    kp, ks = _rows(dev, "k_new", k_new, T, Hkv, D)
+    vp, vs = _rows(dev, "v_new", v_new, T, Hkv, D)
+    rows, rot = (0, 0) if rope is None else rope.shape
+    keys, exp = (None, None) if summary is None else (summary.keys, summary.exp)
     if q_out is None:
         q_out = _empty(stream, dev, T, Hq, D)
-    else:
-        _want(q_out, "q_out", T * Hq * D, torch.bfloat16, dev)
-    args = _pack_rope(q.data_ptr(), k_new.data_ptr(), v_new.data_ptr(), _null(rope), _null(positions),
-                      _null(cu_seqlens), q_out.data_ptr(), a.k_cache.data_ptr(), a.v_cache.data_ptr(), keys, exp,
-                      a.block_table.data_ptr(), a.context_lens.data_ptr(), a.B, T, Hq, Hkv, D, rot, interleaved,
-                      rows, max_seqlen, a.block_size, a.max_blocks, a.num_blocks, qs, ks, vs)
+    tiles = blocks * Hkv
+    rest = _dense(dev, "rope", rope, _F32, rows * rot, "positions", positions, _I32, T,
+                  "cu_seqlens", cu_seqlens, _I32, B + 1, "q_out", q_out, _BF16, T * Hq * D,
+                  "k_cache", a.k_cache, _BF16, tiles * 16 * D, "v_cache", a.v_cache, _BF16, tiles * 16 * D,
+                  "summary keys", keys, _I8, tiles * D, "summary exponents", exp, _I8, tiles,
+                  "block_table", a.block_table, _I32, B * a.max_blocks, "context_lens", a.context_lens, _I32, B)
+    if T == 0:  # (empty tensors have no address)
+        return q_out
+    args = _pack_rope(qp, kp, vp, *rest, B, T, Hq, Hkv, D, rot, interleaved, rows, max_seqlen, a.block_size,
+                      a.max_blocks, blocks, qs, ks, vs)
     _check(getattr(_lib, name)(args, _stream(stream)))
     return q_out
 
@@ -717,8 +684,7 @@ def rope_append(a, q, k_new, v_new, rope, interleaved: bool = False, positions=N
     (position ctx-1, or row ``positions[b]`` of ``rope``; rope=None: no rotation). q [B, Hq, D], k_new and
     v_new [B, Hkv, D] may be slices of one projection's output. With ``summary`` (BlockSummary) the blocks
     that get full are summarised. Returns the rotated queries [B, Hq, D]."""
-    load()
-    return _rope(_device_of(q), "aflex_rope_append", a, q, k_new, v_new, rope, None, 0, interleaved, positions,
+    return _rope(q, "aflex_rope_append", a, q, k_new, v_new, rope, None, 0, interleaved, positions,
                  summary, q_out, stream)
 
 
@@ -726,51 +692,47 @@ def rope_write(a, q, k_new, v_new, cu_seqlens, rope, max_seqlen=None, interleave
                summary=None, q_out=None, stream=None):
     """rope_append for packed new tokens: rows cu[b] .. cu[b+1]-1 are the newest of sequence b's context.
     ``max_seqlen`` bounds the prompts' lengths (None: read from cu_seqlens, which waits for the device)."""
-    load()
-    dev = _device_of(q)
     if max_seqlen is None:
+        _need_gpu(q.device)
         c = cu_seqlens.cpu()
         max_seqlen = int((c[1:] - c[:-1]).max()) if c.numel() > 1 else 0
-    return _rope(dev, "aflex_rope_write", a, q, k_new, v_new, rope, cu_seqlens, max_seqlen, interleaved, positions,
+    return _rope(q, "aflex_rope_write", a, q, k_new, v_new, rope, cu_seqlens, max_seqlen, interleaved, positions,
                  summary, q_out, stream)
 
 
 @_on_device
 def _block_summary(dev, a, summary, stream):
-    _want_cache(a, dev, ("k_cache",))
     if summary is None:
         if stream is None:
             summary = BlockSummary.of(a)
         else:
             with torch.cuda.stream(stream):
                 summary = BlockSummary.of(a)
-    _want_summary(a, summary, dev)
-    args = _pack_block_summary(a.k_cache.data_ptr(), summary.keys.data_ptr(), summary.exp.data_ptr(),
-                               a.block_table.data_ptr(), a.context_lens.data_ptr(), a.B, a.Hkv, a.D, a.block_size,
-                               a.max_blocks, a.num_blocks, a.max_context_len)
+    tiles = a.num_blocks * a.Hkv
+    ptrs = _dense(dev, "k_cache", a.k_cache, _BF16, tiles * 16 * a.D, "summary keys", summary.keys, _I8, tiles * a.D,
+                  "summary exponents", summary.exp, _I8, tiles,
+                  "block_table", a.block_table, _I32, a.B * a.max_blocks, "context_lens", a.context_lens, _I32, a.B)
+    args = _pack_block_summary(*ptrs, a.B, a.Hkv, a.D, a.block_size, a.max_blocks, a.num_blocks, a.max_context_len)
     _check(_lib.aflex_block_summary(args, _stream(stream)))
     return summary
 
 
 def block_summary(a, summary=None, stream=None):
     """Summaries of every full block of a's sequences (for caches written without them), in place."""
-    load()
-    return _block_summary(_device_of(a.k_cache), a, summary, stream)
+    return _block_summary(a.k_cache, a, summary, stream)
 
 
 @_on_device
 def _block_select(dev, a, q, summary, top_blocks, sink_blocks, recent_blocks, out, stream, ws):
-    _want_cache(a, dev, ())
-    _want_summary(a, summary, dev)
-    _want(q, "q", a.B * a.Hq * a.D, torch.bfloat16, dev)
+    B, Hq, Hkv, D, tiles = a.B, a.Hq, a.Hkv, a.D, a.num_blocks * a.Hkv
     if out is None:
-        out = _empty(stream, dev, a.B, a.Hkv, max(top_blocks, 0), dtype=torch.int32)
-    else:
-        _want(out, "out", a.B * a.Hkv * top_blocks, torch.int32, dev)
-    args = _pack_block_select(q.data_ptr(), summary.keys.data_ptr(), summary.exp.data_ptr(),
-                              a.block_table.data_ptr(), a.context_lens.data_ptr(), out.data_ptr(), a.B, a.Hq, a.Hkv,
-                              a.D, a.block_size, a.max_blocks, a.num_blocks, a.max_context_len, top_blocks,
-                              sink_blocks, recent_blocks)
+        out = _empty(stream, dev, B, Hkv, max(top_blocks, 0), dtype=torch.int32)
+    ptrs = _dense(dev, "q", q, _BF16, B * Hq * D, "summary keys", summary.keys, _I8, tiles * D,
+                  "summary exponents", summary.exp, _I8, tiles,
+                  "block_table", a.block_table, _I32, B * a.max_blocks, "context_lens", a.context_lens, _I32, B,
+                  "out", out, _I32, B * Hkv * max(top_blocks, 0))
+    args = _pack_block_select(*ptrs, B, Hq, Hkv, D, a.block_size, a.max_blocks, a.num_blocks, a.max_context_len,
+                              top_blocks, sink_blocks, recent_blocks)
     _run_own_ws("aflex_block_select", args, dev, ws, stream)
     return out
 
@@ -780,29 +742,26 @@ def block_select(a, q, summary, top_blocks: int, sink_blocks: int = 1, recent_bl
     """The ``top_blocks`` cache blocks that each (sequence, kv head) attends for the rotated queries q [B, Hq, D]:
     the first ``sink_blocks``, the last ``recent_blocks`` and the best scoring others. int32 [B, Hkv, top_blocks],
     ascending, -1 behind a shorter list."""
-    load()
-    return _block_select(_device_of(q), a, q, summary, top_blocks, sink_blocks, recent_blocks, out, stream, ws)
+    return _block_select(q, a, q, summary, top_blocks, sink_blocks, recent_blocks, out, stream, ws)
 
 
 @_on_device
 def _attn_sparse(dev, a, selected, q, out, scale, stream, ws):
-    _want_cache(a, dev)
-    _want(q, "q", a.B * a.Hq * a.D, torch.bfloat16, dev)
-    top = selected.shape[-1]
-    _want(selected, "selected", a.B * a.Hkv * top, torch.int32, dev)
+    B, Hq, Hkv, D, top = a.B, a.Hq, a.Hkv, a.D, selected.shape[-1]
     if out is None:
-        out = _empty(stream, dev, a.B, a.Hq, a.D)
-    else:
-        _want(out, "out", a.B * a.Hq * a.D, torch.bfloat16, dev)
-    args = _pack_attn_sparse(q.data_ptr(), a.k_cache.data_ptr(), a.v_cache.data_ptr(), a.block_table.data_ptr(),
-                             a.context_lens.data_ptr(), out.data_ptr(), a.B, a.Hq, a.Hkv, a.D, a.block_size,
-                             a.max_blocks, a.num_blocks, a.max_context_len, scale, 0, selected.data_ptr(), top)
+        out = _empty(stream, dev, B, Hq, D)
+    pool = a.num_blocks * Hkv * 16 * D
+    *ptrs, sel = _dense(dev, "q", q, _BF16, B * Hq * D, "k_cache", a.k_cache, _BF16, pool,
+                        "v_cache", a.v_cache, _BF16, pool, "block_table", a.block_table, _I32, B * a.max_blocks,
+                        "context_lens", a.context_lens, _I32, B, "out", out, _BF16, B * Hq * D,
+                        "selected", selected, _I32, B * Hkv * top)
+    args = _pack_attn_sparse(*ptrs, B, Hq, Hkv, D, a.block_size, a.max_blocks, a.num_blocks, a.max_context_len, scale,
+                             0, sel, top)
     _run_own_ws("aflex_attn_sparse_decode", args, dev, ws, stream)
     return out
 
 
 def attn_sparse_decode(a, selected, q=None, out=None, scale: float = 0.0, stream=None, ws=None):
     """Decode attention of q (default a.q) [B, Hq, D] over the blocks that selected [B, Hkv, top_blocks] lists."""
-    load()
     q = a.q if q is None else q
-    return _attn_sparse(_device_of(q), a, selected, q, out, scale, stream, ws)
+    return _attn_sparse(q, a, selected, q, out, scale, stream, ws)

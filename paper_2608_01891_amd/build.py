@@ -2,8 +2,10 @@
 
     python -m paper_2608_01891_amd.build
 
-Every source under csrc/ is compiled for gfx950 with packed-fp32 code
-generation disabled, then linked into ``paper_2608_01891_amd/libaflex.so``.
+Every .hip source under csrc/ is compiled for gfx950 with packed-fp32 code
+generation disabled, then linked into ``paper_2608_01891_amd/libaflex.so``;
+``csrc/tensor_args.cpp`` (host code: the binding's checks of its tensors)
+becomes the module ``paper_2608_01891_amd/_tensor_args.so``.
 """
 from __future__ import annotations
 
@@ -12,6 +14,7 @@ import os
 import shutil
 import subprocess
 import sys
+import sysconfig
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
@@ -19,6 +22,7 @@ CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 BUILD = os.path.join(ROOT, "_build")
 LIB = os.path.join(PKG, "libaflex.so")
+TENSOR_ARGS = os.path.join(PKG, "_tensor_args.so")
 
 ARCH = "gfx950"
 HIPCC = os.environ.get("HIPCC", shutil.which("hipcc") or "/opt/rocm/bin/hipcc")
@@ -53,12 +57,29 @@ def _compile(src: str) -> str:
     return obj
 
 
+def _tensor_args() -> None:
+    import torch
+    root = os.path.dirname(torch.__file__)
+    tmp = TENSOR_ARGS + ".tmp"
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-w",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           f"-I{sysconfig.get_paths()['include']}", f"-I{root}/include", f"-I{root}/include/torch/csrc/api/include",
+           os.path.join(CSRC, "tensor_args.cpp"), "-o", tmp,
+           f"-L{root}/lib", "-ltorch_python", "-ltorch_cpu", "-lc10"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"g++ failed for tensor_args.cpp:\n{r.stderr}")
+    os.replace(tmp, TENSOR_ARGS)
+
+
 def build(verbose: bool = True) -> str:
     os.makedirs(BUILD, exist_ok=True)
     srcs = sources()
     jobs = min(len(srcs), max(1, min(16, os.cpu_count() or 1)))
-    with cf.ThreadPoolExecutor(jobs) as ex:
+    with cf.ThreadPoolExecutor(jobs + 1) as ex:
+        host = ex.submit(_tensor_args)
         objs = list(ex.map(_compile, srcs))
+        host.result()
     tmp = LIB + ".tmp"
     cmd = [HIPCC, f"--offload-arch={ARCH}", "-shared", "-fPIC", "-o", tmp, *objs]
     r = subprocess.run(cmd, capture_output=True, text=True)

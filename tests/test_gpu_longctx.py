@@ -236,6 +236,15 @@ def test_write_longer_than_the_cache_and_out_of_range(gpu_lib):
     assert torch.equal(sd.keys.cpu(), keys) and torch.equal(sd.exp.cpu(), exp)
 
 
+def test_write_of_nothing(gpu_lib):
+    a = synth.custom_attention(19, 2, 8, 2, 64, [20, 33], ctx_hi=48).to(DEV)
+    before = a.k_cache.clone()
+    e = torch.empty(0, 8, 64, dtype=torch.bfloat16, device=DEV)
+    out = aflex.rope_write(a, e, e[:, :2], e[:, :2], torch.zeros(3, dtype=torch.int32, device=DEV),
+                           aflex.rope_table(48, 64).to(DEV))
+    assert out.shape == (0, 8, 64) and torch.equal(a.k_cache, before)
+
+
 def test_write_of_single_tokens_is_append(gpu_lib):
     heads = (28, 4, 128)
     a = synth.custom_attention(25, 9, *heads, [1, 16, 17, 32, 64, 65, 7, 48, 50], ctx_hi=80)

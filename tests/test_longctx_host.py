@@ -1,6 +1,7 @@
 """Host-side checks of the long-context entry points (no GPU needed): exports,
 refusals before any launch, workspace sizes, and what the binding refuses."""
 import ctypes
+import os
 
 import pytest
 import torch
@@ -13,6 +14,9 @@ INVALID, UNSUP, ALIGN, WS = (aflex.ERR_INVALID_ARG, aflex.ERR_UNSUPPORTED, aflex
 
 @pytest.fixture(scope="module")
 def lib():
+    from paper_2608_01891_amd import build
+    if not (os.path.exists(aflex.LIB_PATH) and os.path.exists(build.TENSOR_ARGS)):
+        build.build(verbose=False)
     return aflex.load()
 
 
@@ -181,14 +185,29 @@ def test_host_tensors_are_refused_before_any_library_call(lib, monkeypatch, op):
     assert calls == []
 
 
-def test_rows_that_the_binding_refuses():
+def test_rows_that_the_binding_refuses(lib):
+    rows, dense = aflex._rows, aflex._dense
     x = torch.zeros(3, 12, 64, dtype=torch.bfloat16)
-    assert aflex._row_stride(x[:, 2:10], "q", 3, 8, 64, -1) == 12 * 64
-    assert aflex._row_stride(x[:1, :1], "q", 1, 1, 64, -1) == 0
+    y = x[:, 2:10]
+    assert rows(-1, "q", y, 3, 8, 64) == (y.data_ptr(), 12 * 64)
+    assert rows(-1, "q", x[:1, :1], 1, 1, 64) == (x.data_ptr(), 0)
+    assert rows(-1, "q", x[:0], 0, 12, 64)[1] == 0
     for bad in (x.float()[:, :8], x[:, :7], x[:, 0:8].transpose(0, 1).contiguous().transpose(0, 1),
-                x[:1, :8].expand(3, 8, 64), x[..., ::2], x[:, ::2]):
-        with pytest.raises(ValueError, match="q: expected"):
-            aflex._row_stride(bad, "q", 3, 8, 64, -1)
-    for bad in (x[:, :8], x.float(), torch.zeros(5, dtype=torch.bfloat16)):
-        with pytest.raises(ValueError, match="dense"):
-            aflex._want(bad, "t", 3 * 12 * 64, torch.bfloat16, -1)
+                x[:1, :8].expand(3, 8, 64), x[..., ::2], x[:, ::2], x[:2, :8], x[0, :8]):
+        with pytest.raises(ValueError, match="q: expected bf16"):
+            rows(-1, "q", bad, 3, 8, 64)
+    n = x.numel()
+    assert dense(-1, "t", x, 0, n, "u", None, 1, 5) == (x.data_ptr(), 0)
+    for bad, code, count in ((x[:, :8], 0, 3 * 8 * 64), (x.float(), 0, n), (x, 1, n), (x, 0, n + 1), (x.to("meta"), 0, n)):
+        with pytest.raises(ValueError, match="t: expected .* dense"):
+            dense(-1, "t", bad, code, count)
+    for f in (lambda: rows(0, "q", x, 3, 12, 64), lambda: dense(0, "q", x, 0, n)):  # a host tensor where cuda:0 is meant
+        with pytest.raises(ValueError, match="cuda:0"):
+            f()
+    with pytest.raises(TypeError, match="t: expected a tensor"):
+        dense(-1, "t", 5, 0, 1)
+    with pytest.raises(TypeError):
+        dense(-1, "t", x)
+    from torch._subclasses.fake_tensor import FakeTensorMode
+    with FakeTensorMode() as mode, pytest.raises((RuntimeError, ValueError)):  # without memory
+        dense(-1, "t", mode.from_tensor(x), 0, n)
