@@ -714,9 +714,21 @@ static long long work_bound(const aflex_attn_args& a, int top = 0) {
 // sizes costs more than the imbalance between units, is skipped.
 constexpr int kUnitPerWgMaxCtx = 512;
 
+// So do lists of chosen blocks, and those of up to kListPerWg blocks also where
+// the units are many: dealt out as work-groups end, they balance themselves and
+// need no merge (us with an even split / a work-group per unit, 64 / 8 heads x
+// 128: 2048 units of 32 blocks 114.6 / 95.7, 1600 of 48 124.2 / 113.9, 1024 of
+// 128 189.0 / 177.5; lognormal lengths, 2048 of up to 32 97.3 / 84.1, 1024 of up
+// to 64 73.9 / 78.2; below that many the even split is safer: 512 of up to 128
+// 53.4 / 75.4).
+constexpr int kListPerWg = 128;
+
 static bool unit_per_wg(const aflex_attn_args& a, int top = 0) {
-  return a.split_tokens == 0 && max_unit_blocks(a, top) <= kUnitPerWgMaxCtx / 16 &&
-         (long long)a.B * a.Hkv <= resident_wgs();
+  if (a.split_tokens != 0) return false;
+  const long long units = (long long)a.B * a.Hkv;
+  const int most = max_unit_blocks(a, top);
+  return (most <= kUnitPerWgMaxCtx / 16 && units <= resident_wgs()) ||
+         (top > 0 && most <= kListPerWg && 3 * units >= 4 * resident_wgs());
 }
 
 // Grid size: one work-group per unit for short contexts (above); with a fixed

@@ -416,6 +416,17 @@ def test_attention(gpu_lib, heads, top):
     _attend(a, _lists(52, a, top))
 
 
+def test_attention_of_many_units(gpu_lib):
+    """1024 and more (sequence, kv head) pairs: a work-group each; and lists too long for that."""
+    ctx = [1 + 37 * i % 700 for i in range(64)]
+    a = synth.custom_attention(62, 64, 16, 16, 64, ctx, ctx_hi=720)
+    a.context_lens[::9] = 0
+    for top in (5, 20, 45):
+        _attend(a, _lists(63 + top, a, top))
+    b = synth.custom_attention(64, 128, 8, 8, 128, [50 + 17 * i % 300 for i in range(127)] + [3000])
+    _attend(b, _lists(65, b, 150))
+
+
 def test_attention_split_over_many_work_groups(gpu_lib):
     a = synth.custom_attention(53, 1, 16, 2, 128, [9000])
     _attend(a, _lists(54, a, 500))
