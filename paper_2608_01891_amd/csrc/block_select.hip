@@ -598,21 +598,23 @@ __global__ __launch_bounds__(kPickThreads) void block_pick_kernel(aflex_block_se
   });
 }
 
-// Scores and choice of a unit in one work-group, the keys in LDS.
+// Scores and choice of a unit in one work-group, the keys in LDS (the bins of
+// the choice where the rows of the scores were: 37 KiB, four work-groups per CU).
 template <int D>
-__global__ __launch_bounds__(kSelectThreads) void block_select_kernel(aflex_block_select_args a) {
-  constexpr int NT = kSelectThreads;
+__global__ __launch_bounds__(kSelectThreads, 4) void block_select_kernel(aflex_block_select_args a) {
+  constexpr int NT = kSelectThreads, NW = NT / 64;
+  constexpr int kBytes = NW * 64 * D > (int)sizeof(PickShared) ? NW * 64 * D : (int)sizeof(PickShared);
   __shared__ __attribute__((aligned(16))) uint32_t keys[kFusedBlocks];
-  __shared__ __attribute__((aligned(16))) uint8_t rows[NT / 64][64 * D];
-  __shared__ PickShared sh;
+  __shared__ __attribute__((aligned(16))) uint8_t shared[kBytes];
   int b, g;
   unit_of(blockIdx.x, a.B, a.Hkv, b, g);
-  const int n = nblk16(clamp_len(a, b));
+  const int n = nblk16(clamp_len(a, b)), wave = threadIdx.x >> 6;
   int32_t* out = a.selected + ((size_t)b * a.Hkv + g) * a.top_blocks;
   if (trivial_row<NT>(n, a.top_blocks, out)) return;
+  score_blocks<D>(a, b, g, n, wave * 64, NT, n, shared + wave * 64 * D, keys);
+  __syncthreads();
+  PickShared& sh = *reinterpret_cast<PickShared*>(shared);
   clear_bins<NT>(sh);
-  const int wave = threadIdx.x >> 6;
-  score_blocks<D>(a, b, g, n, wave * 64, NT, n, rows[wave], keys);
   __syncthreads();
   choose<NT>(Held<NT, kFusedBlocks>(keys, n), a.top_blocks, [](int place) { return place; }, out, sh);
 }
