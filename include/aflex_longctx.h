@@ -155,13 +155,16 @@ typedef struct aflex_attn_sparse_args {
 } aflex_attn_sparse_args;
 
 /* Supported: as aflex_attn_decode, and B * Hkv * top_blocks < 2^30. The same  */
-/* result on every call with the same inputs (bitwise).                        */
+/* result on every call with the same inputs (bitwise). The softmax weights    */
+/* are rounded to bf16 for the product with the values and summed as rounded;  */
+/* scores, sums and the merge of split lists are fp32.                         */
 aflex_status aflex_attn_sparse_decode_workspace(const aflex_attn_sparse_args *a, size_t *bytes);
 aflex_status aflex_attn_sparse_decode(const aflex_attn_sparse_args *a, void *workspace, size_t workspace_bytes,
                                       aflex_stream stream);
 
 /* Kernel names for aflex_profile_start: rope_append, rope_write,              */
-/* block_summary, block_score, block_pick, attn_sparse, attn_merge.            */
+/* block_summary, block_select, block_score, block_pick, attn_sparse,         */
+/* attn_merge.                                                                */
 
 #ifdef __cplusplus
 }

@@ -630,7 +630,12 @@ def _run_own_ws(name, args, dev, ws, stream):
     graph's own memory."""
     handle = _stream(stream)
     if ws is None:
-        if torch.cuda.is_current_stream_capturing():
+        if stream is None:
+            capturing = torch.cuda.is_current_stream_capturing()
+        else:
+            with torch.cuda.stream(stream):
+                capturing = torch.cuda.is_current_stream_capturing()
+        if capturing:
             ws = Workspace()
         else:
             key = (name, dev, handle)

@@ -359,6 +359,23 @@ def test_block_select_long_with_equal_scores(gpu_lib, n, top):
         _choice(49, [16 * n - 5], (4, 1, 64), top, 1, 1, edit=edit)
 
 
+def test_block_select_long_sequences_among_many_short(gpu_lib):
+    ctx = [5] * 200
+    ctx[3], ctx[70], ctx[199] = 17000, 2100, 18000
+    _choice(53, ctx, (4, 2, 64), 20, 1, 1)
+
+
+def test_block_select_scores_too_small_for_fp32(gpu_lib):
+    """Scores of both signs that round to zero are equal."""
+    def tiny(a, s):
+        a.q *= 2.0 ** -100
+        s.exp.fill_(-118)
+        s.exp[a.block_table[0, 30:33].long()] = 0
+
+    for ctx in (900, 17000):
+        _choice(54, [ctx], (8, 2, 128), 12, 1, 1, edit=tiny)
+
+
 def test_block_select_heads_far_apart_in_size(gpu_lib):
     """Heads of one group whose scales differ by more than fp32's range, both with whole codes."""
     def far(a, s):
