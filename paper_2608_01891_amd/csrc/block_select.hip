@@ -510,6 +510,14 @@ __global__ __launch_bounds__(kPickThreads) void block_pick_kernel(aflex_block_se
   if (trivial_row<NT>(n, N, out)) return;
   const uint32_t* src = keys + (size_t)unit * stride;  // (rows are padded to a multiple of 4)
   clear_bins<NT>(sh);
+  // a short sequence among long ones, or under a loose bound (131072 tokens: 64
+  // sequences of median 20000 40.6 -> 32.7 us, of 3000 25.7 -> 15.3)
+  if (n <= kListed) {
+    const Held<NT> held(src, n);
+    __syncthreads();
+    choose<NT>(held, N, [](int place) { return place; }, out, sh);
+    return;
+  }
   const int rounds = (n + 4 * NT - 1) / (4 * NT);
   const long long base = (long long)(tid >> 6) * rounds * 256 + lane * 4;
   auto load = [&](int i) {
