@@ -12,7 +12,6 @@ import ctypes
 import gc
 import os
 import re
-import struct
 
 import torch
 
@@ -103,18 +102,6 @@ class AttnSparseArgs(ctypes.Structure):
     _fields_ = [("attn", AttnArgs), ("selected", _p), ("top_blocks", _i)]
 
 
-def _packer(cls):
-    """struct.Struct.pack of an argument block's fields, flattened (a third of a Structure's cost per call)."""
-    def codes(c):
-        return "".join({_p: "P", _i: "i", ctypes.c_float: "f"}.get(f) or codes(f) for _, f in c._fields_)
-    s = codes(cls)
-    return struct.Struct(f"{s}{ctypes.sizeof(cls) - struct.calcsize(s)}x").pack
-
-
-_pack_rope, _pack_block_summary, _pack_block_select, _pack_attn_sparse = map(
-    _packer, (RopeArgs, BlockSummaryArgs, BlockSelectArgs, AttnSparseArgs))
-
-
 class AflexError(RuntimeError):
     def __init__(self, status: int, message: str):
         super().__init__(f"aflex status {status}: {message}")
@@ -122,7 +109,7 @@ class AflexError(RuntimeError):
 
 
 _lib = None
-_dense = _rows = None  # of _tensor_args (see load)
+_call, _entry = None, {}  # of _tensor_args, and addresses of entry points (see load)
 _SZ = ctypes.POINTER(ctypes.c_size_t)
 
 
@@ -135,7 +122,7 @@ def exported_names(header=HEADER):
 
 def load():
     """Open the built library (cached). Raises if it has not been built."""
-    global _lib, _dense, _rows
+    global _lib, _call
     if _lib is not None:
         return _lib
     if not os.path.exists(LIB_PATH):
@@ -145,7 +132,7 @@ def load():
     except ImportError as e:
         raise RuntimeError(f"{_PKG}/_tensor_args.so cannot be loaded: build it with "
                            "`python -m paper_2608_01891_amd.build`") from e
-    _dense, _rows = _tensor_args.dense, _tensor_args.rows
+    _call = _tensor_args.call
     lib = ctypes.CDLL(LIB_PATH)
     AP, FP = ctypes.POINTER(AttnArgs), ctypes.POINTER(FfnArgs)
     I32P = ctypes.POINTER(ctypes.c_int32)
@@ -170,18 +157,19 @@ def load():
         "aflex_kv_write": [ctypes.POINTER(KvWriteArgs), _p],
         "aflex_pool_streams_create": [ctypes.c_int32, ctypes.POINTER(_p), ctypes.POINTER(_p)],
         "aflex_pool_streams_destroy": [_p, _p],
-        "aflex_rope_append": [_p, _p],
-        "aflex_rope_write": [_p, _p],
-        "aflex_block_summary": [_p, _p],
-        "aflex_block_select_workspace": [_p, _SZ],
-        "aflex_block_select": [_p, _p, ctypes.c_size_t, _p],
-        "aflex_attn_sparse_decode_workspace": [_p, _SZ],
-        "aflex_attn_sparse_decode": [_p, _p, ctypes.c_size_t, _p],
+        "aflex_rope_append": [ctypes.POINTER(RopeArgs), _p],
+        "aflex_rope_write": [ctypes.POINTER(RopeArgs), _p],
+        "aflex_block_summary": [ctypes.POINTER(BlockSummaryArgs), _p],
+        "aflex_block_select_workspace": [ctypes.POINTER(BlockSelectArgs), _SZ],
+        "aflex_block_select": [ctypes.POINTER(BlockSelectArgs), _p, ctypes.c_size_t, _p],
+        "aflex_attn_sparse_decode_workspace": [ctypes.POINTER(AttnSparseArgs), _SZ],
+        "aflex_attn_sparse_decode": [ctypes.POINTER(AttnSparseArgs), _p, ctypes.c_size_t, _p],
     }
     for name, args in sig.items():
         fn = getattr(lib, name)
         fn.argtypes = args
         fn.restype = ctypes.c_int
+        _entry[name] = ctypes.cast(fn, _p).value
     lib.aflex_profile_start.argtypes = [ctypes.c_char_p]
     lib.aflex_profile_start.restype = ctypes.c_int
     lib.aflex_profile_stop.argtypes = [ctypes.c_char_p, ctypes.c_size_t]
@@ -571,10 +559,11 @@ def af_layer_step(a, w, layer, k: int, mb_sizes, L: int = 1, y=None, stream_a=No
 
 # --------------------------------------------------------------------------
 # Long-context operators (include/aflex_longctx.h). These check what the C
-# interface cannot see (types, sizes, devices, strides; in _tensor_args, since
-# in Python the checks took longer than the rest of a call), run on the device
-# of their tensors, and keep a default workspace per stream; outputs that they
-# allocate belong to the stream they run on.
+# interface cannot see (types, sizes, devices, strides), run on the device of
+# their tensors, and keep a default workspace per stream; outputs that they
+# allocate belong to the stream they run on. Checks, argument block and call are
+# one native call (csrc/tensor_args.cpp): the items behind _call's first five
+# arguments are the fields of the entry point's argument block in their order.
 class BlockSummary:
     """Key summaries of a cache's blocks: ``keys`` int8 [num_blocks, Hkv, D] and
     ``exp`` int8 [num_blocks, Hkv] (mean key about keys * 2^exp)."""
@@ -598,7 +587,7 @@ def rope_table(positions: int, rotary_dim: int, base: float = 10000.0, device="c
     return torch.cat([ang.cos(), ang.sin()], 1).float().to(device)
 
 
-_BF16, _F32, _I32, _I8 = range(4)  # type codes of _tensor_args.dense
+_BF16, _F32, _I32, _I8, _ROWS = range(5)  # what the items of a call are
 
 
 def _on_device(f):
@@ -623,7 +612,7 @@ def _empty(stream, dev, *shape, dtype=torch.bfloat16):
         return torch.empty(*shape, dtype=dtype, device=f"cuda:{dev}")
 
 
-def _run_own_ws(name, args, dev, ws, stream):
+def _run_own_ws(name, dev, ws, stream, *items):
     """Call an entry point with a workspace on the current device. The default
     one belongs to the (device, stream) that the call runs on, so calls on two
     streams do not share it; while a graph is captured the call gets one of the
@@ -642,19 +631,19 @@ def _run_own_ws(name, args, dev, ws, stream):
             ws = _default_ws.get(key) or _default_ws.setdefault(key, Workspace())
     elif stream is not None and ws.buf is not None:
         ws.buf.record_stream(stream)  # (a caller's may be used on several)
-    fn = getattr(_lib, name)
-    if ws.buf is not None and ws.buf.get_device() == dev:
-        status = fn(args, ws.buf.data_ptr(), ws.buf.numel(), handle)
+    buf = ws.buf
+    if buf is not None and buf.get_device() == dev:
+        status = _call(_entry[name], dev, handle, buf.data_ptr(), buf.numel(), *items)
         if status != ERR_WORKSPACE:
             return _check(status)
-    n = ctypes.c_size_t()
-    _check(getattr(_lib, name + "_workspace")(args, ctypes.byref(n)))
+    status, need = _call(_entry[name + "_workspace"], dev, None, None, 0, *items)
+    _check(status)
     if stream is None:
-        buf = ws.get(n.value, f"cuda:{dev}")
+        buf = ws.get(need, f"cuda:{dev}")
     else:
         with torch.cuda.stream(stream):
-            buf = ws.get(n.value, f"cuda:{dev}")
-    _check(fn(args, buf.data_ptr(), buf.numel(), handle))
+            buf = ws.get(need, f"cuda:{dev}")
+    _check(_call(_entry[name], dev, handle, buf.data_ptr(), buf.numel(), *items))
 
 
 @_on_device
@@ -662,24 +651,22 @@ def _rope(dev, name, a, q, k_new, v_new, rope, cu_seqlens, max_seqlen, interleav
     B, T, Hq, Hkv, D, blocks = a.B, q.shape[0], a.Hq, a.Hkv, a.D, a.num_blocks
     if cu_seqlens is None and T != B:
         raise ValueError(f"q: expected one row for each of {B} sequences, but got {T}")
-    qp, qs = _rows(dev, "q", q, T, Hq, D)
-    kp, ks = _rows(dev, "k_new", k_new, T, Hkv, D)
-    vp, vs = _rows(dev, "v_new", v_new, T, Hkv, D)
     rows, rot = (0, 0) if rope is None else rope.shape
     keys, exp = (None, None) if summary is None else (summary.keys, summary.exp)
     if q_out is None:
         q_out = _empty(stream, dev, T, Hq, D)
-    tiles = blocks * Hkv
-    rest = _dense(dev, "rope", rope, _F32, rows * rot, "positions", positions, _I32, T,
-                  "cu_seqlens", cu_seqlens, _I32, B + 1, "q_out", q_out, _BF16, T * Hq * D,
-                  "k_cache", a.k_cache, _BF16, tiles * 16 * D, "v_cache", a.v_cache, _BF16, tiles * 16 * D,
-                  "summary keys", keys, _I8, tiles * D, "summary exponents", exp, _I8, tiles,
-                  "block_table", a.block_table, _I32, B * a.max_blocks, "context_lens", a.context_lens, _I32, B)
     if T == 0:  # (empty tensors have no address)
         return q_out
-    args = _pack_rope(qp, kp, vp, *rest, B, T, Hq, Hkv, D, rot, interleaved, rows, max_seqlen, a.block_size,
-                      a.max_blocks, blocks, qs, ks, vs)
-    _check(getattr(_lib, name)(args, _stream(stream)))
+    tiles = blocks * Hkv
+    _check(_call(_entry[name], dev, _stream(stream), None, 0,
+                 "q", q, _ROWS, T, Hq, D, "k_new", k_new, _ROWS, T, Hkv, D, "v_new", v_new, _ROWS, T, Hkv, D,
+                 "rope", rope, _F32, rows * rot, "positions", positions, _I32, T,
+                 "cu_seqlens", cu_seqlens, _I32, B + 1, "q_out", q_out, _BF16, T * Hq * D,
+                 "k_cache", a.k_cache, _BF16, tiles * 16 * D, "v_cache", a.v_cache, _BF16, tiles * 16 * D,
+                 "summary keys", keys, _I8, tiles * D, "summary exponents", exp, _I8, tiles,
+                 "block_table", a.block_table, _I32, B * a.max_blocks, "context_lens", a.context_lens, _I32, B,
+                 B, T, Hq, Hkv, D, rot, int(interleaved), rows, max_seqlen, a.block_size, a.max_blocks, blocks,
+                 None, None, None))  # the strides of q, k_new, v_new
     return q_out
 
 
@@ -713,12 +700,12 @@ def _block_summary(dev, a, summary, stream):
         else:
             with torch.cuda.stream(stream):
                 summary = BlockSummary.of(a)
-    tiles = a.num_blocks * a.Hkv
-    ptrs = _dense(dev, "k_cache", a.k_cache, _BF16, tiles * 16 * a.D, "summary keys", summary.keys, _I8, tiles * a.D,
-                  "summary exponents", summary.exp, _I8, tiles,
-                  "block_table", a.block_table, _I32, a.B * a.max_blocks, "context_lens", a.context_lens, _I32, a.B)
-    args = _pack_block_summary(*ptrs, a.B, a.Hkv, a.D, a.block_size, a.max_blocks, a.num_blocks, a.max_context_len)
-    _check(_lib.aflex_block_summary(args, _stream(stream)))
+    B, Hkv, D, tiles = a.B, a.Hkv, a.D, a.num_blocks * a.Hkv
+    _check(_call(_entry["aflex_block_summary"], dev, _stream(stream), None, 0,
+                 "k_cache", a.k_cache, _BF16, tiles * 16 * D, "summary keys", summary.keys, _I8, tiles * D,
+                 "summary exponents", summary.exp, _I8, tiles, "block_table", a.block_table, _I32, B * a.max_blocks,
+                 "context_lens", a.context_lens, _I32, B,
+                 B, Hkv, D, a.block_size, a.max_blocks, a.num_blocks, a.max_context_len))
     return summary
 
 
@@ -732,13 +719,12 @@ def _block_select(dev, a, q, summary, top_blocks, sink_blocks, recent_blocks, ou
     B, Hq, Hkv, D, tiles = a.B, a.Hq, a.Hkv, a.D, a.num_blocks * a.Hkv
     if out is None:
         out = _empty(stream, dev, B, Hkv, max(top_blocks, 0), dtype=torch.int32)
-    ptrs = _dense(dev, "q", q, _BF16, B * Hq * D, "summary keys", summary.keys, _I8, tiles * D,
-                  "summary exponents", summary.exp, _I8, tiles,
-                  "block_table", a.block_table, _I32, B * a.max_blocks, "context_lens", a.context_lens, _I32, B,
-                  "out", out, _I32, B * Hkv * max(top_blocks, 0))
-    args = _pack_block_select(*ptrs, B, Hq, Hkv, D, a.block_size, a.max_blocks, a.num_blocks, a.max_context_len,
-                              top_blocks, sink_blocks, recent_blocks)
-    _run_own_ws("aflex_block_select", args, dev, ws, stream)
+    _run_own_ws("aflex_block_select", dev, ws, stream,
+                "q", q, _BF16, B * Hq * D, "summary keys", summary.keys, _I8, tiles * D,
+                "summary exponents", summary.exp, _I8, tiles, "block_table", a.block_table, _I32, B * a.max_blocks,
+                "context_lens", a.context_lens, _I32, B, "out", out, _I32, B * Hkv * max(top_blocks, 0),
+                B, Hq, Hkv, D, a.block_size, a.max_blocks, a.num_blocks, a.max_context_len, top_blocks, sink_blocks,
+                recent_blocks)
     return out
 
 
@@ -756,13 +742,12 @@ def _attn_sparse(dev, a, selected, q, out, scale, stream, ws):
     if out is None:
         out = _empty(stream, dev, B, Hq, D)
     pool = a.num_blocks * Hkv * 16 * D
-    *ptrs, sel = _dense(dev, "q", q, _BF16, B * Hq * D, "k_cache", a.k_cache, _BF16, pool,
-                        "v_cache", a.v_cache, _BF16, pool, "block_table", a.block_table, _I32, B * a.max_blocks,
-                        "context_lens", a.context_lens, _I32, B, "out", out, _BF16, B * Hq * D,
-                        "selected", selected, _I32, B * Hkv * top)
-    args = _pack_attn_sparse(*ptrs, B, Hq, Hkv, D, a.block_size, a.max_blocks, a.num_blocks, a.max_context_len, scale,
-                             0, sel, top)
-    _run_own_ws("aflex_attn_sparse_decode", args, dev, ws, stream)
+    _run_own_ws("aflex_attn_sparse_decode", dev, ws, stream,
+                "q", q, _BF16, B * Hq * D, "k_cache", a.k_cache, _BF16, pool, "v_cache", a.v_cache, _BF16, pool,
+                "block_table", a.block_table, _I32, B * a.max_blocks, "context_lens", a.context_lens, _I32, B,
+                "out", out, _BF16, B * Hq * D,
+                B, Hq, Hkv, D, a.block_size, a.max_blocks, a.num_blocks, a.max_context_len, float(scale), 0,
+                "selected", selected, _I32, B * Hkv * top, top)
     return out
 
 

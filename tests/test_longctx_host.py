@@ -185,29 +185,106 @@ def test_host_tensors_are_refused_before_any_library_call(lib, monkeypatch, op):
     assert calls == []
 
 
+def _block_of(*items, dev=-1, call=None):
+    """The argument block that items make, zeros behind it."""
+    got = []
+    keep = ctypes.CFUNCTYPE(ctypes.c_int, ctypes.c_void_p, ctypes.c_void_p)(
+        lambda p, s: got.append((ctypes.string_at(p, 256), s)) or 7)
+    assert (call or aflex._call)(ctypes.cast(keep, ctypes.c_void_p).value, dev, 5, None, 0, *items) == 7
+    assert got[0][1] == 5
+    return got[0][0]
+
+
 def test_rows_that_the_binding_refuses(lib):
-    rows, dense = aflex._rows, aflex._dense
     x = torch.zeros(3, 12, 64, dtype=torch.bfloat16)
+
+    def rows(t, T, H, D):
+        b = _block_of("q", t, aflex._ROWS, T, H, D, None)
+        return int.from_bytes(b[:8], "little"), int.from_bytes(b[8:12], "little")
+
     y = x[:, 2:10]
-    assert rows(-1, "q", y, 3, 8, 64) == (y.data_ptr(), 12 * 64)
-    assert rows(-1, "q", x[:1, :1], 1, 1, 64) == (x.data_ptr(), 0)
-    assert rows(-1, "q", x[:0], 0, 12, 64)[1] == 0
+    assert rows(y, 3, 8, 64) == (y.data_ptr(), 12 * 64)
+    assert rows(x[:1, :1], 1, 1, 64) == (x.data_ptr(), 0)
     for bad in (x.float()[:, :8], x[:, :7], x[:, 0:8].transpose(0, 1).contiguous().transpose(0, 1),
                 x[:1, :8].expand(3, 8, 64), x[..., ::2], x[:, ::2], x[:2, :8], x[0, :8]):
         with pytest.raises(ValueError, match="q: expected bf16"):
-            rows(-1, "q", bad, 3, 8, 64)
+            rows(bad, 3, 8, 64)
+
+
+def test_dense_tensors_that_the_binding_refuses(lib):
+    x = torch.zeros(3, 12, 64, dtype=torch.bfloat16)
     n = x.numel()
-    assert dense(-1, "t", x, 0, n, "u", None, 1, 5) == (x.data_ptr(), 0)
-    for bad, code, count in ((x[:, :8], 0, 3 * 8 * 64), (x.float(), 0, n), (x, 1, n), (x, 0, n + 1), (x.to("meta"), 0, n)):
+    b = _block_of("t", x, aflex._BF16, n, 9, "u", None, aflex._F32, 5)
+    assert b[:8] == x.data_ptr().to_bytes(8, "little") and b[8:12] == bytes([9, 0, 0, 0]) and not any(b[12:])
+    for bad, code, count in ((x[:, :8], 0, 3 * 8 * 64), (x.float(), 0, n), (x, 1, n), (x, 0, n + 1), (x.to("meta"), 0, n),
+                             (x, 9, n)):
         with pytest.raises(ValueError, match="t: expected .* dense"):
-            dense(-1, "t", bad, code, count)
-    for f in (lambda: rows(0, "q", x, 3, 12, 64), lambda: dense(0, "q", x, 0, n)):  # a host tensor where cuda:0 is meant
+            _block_of("t", bad, code, count)
+    for item in (("q", x, aflex._ROWS, 3, 12, 64), ("q", x, aflex._BF16, n)):  # a host tensor where cuda:0 is meant
         with pytest.raises(ValueError, match="cuda:0"):
-            f()
-    with pytest.raises(TypeError, match="t: expected a tensor"):
-        dense(-1, "t", 5, 0, 1)
-    with pytest.raises(TypeError):
-        dense(-1, "t", x)
+            _block_of(*item, dev=0)
+    for item in (("t", 5, 0, 1), ("t", x, 0), ("t", x), (x,), (None,), ("q", None, aflex._ROWS, 3, 12, 64)):
+        with pytest.raises(TypeError):
+            _block_of(*item)
+    with pytest.raises(OverflowError):
+        _block_of(1 << 31)
+    with pytest.raises(TypeError, match="too long"):
+        _block_of(*range(65))
     from torch._subclasses.fake_tensor import FakeTensorMode
     with FakeTensorMode() as mode, pytest.raises((RuntimeError, ValueError)):  # without memory
-        dense(-1, "t", mode.from_tensor(x), 0, n)
+        _block_of("t", mode.from_tensor(x), aflex._BF16, n)
+
+
+def test_calls_lay_out_the_argument_blocks(lib, monkeypatch):
+    """Every field of the C structs from a call of the binding, on host tensors."""
+    got, real = {}, aflex._call
+
+    def call(entry, dev, stream, ws, nbytes, *items):
+        got["block"] = _block_of(*items, call=real)
+        return aflex.OK if stream is not None else (aflex.OK, 0)
+
+    monkeypatch.setattr(aflex, "_call", call)
+    monkeypatch.setattr(aflex, "_stream", lambda s: 0)
+    monkeypatch.setattr(aflex, "_default_ws", {})
+    monkeypatch.setattr(aflex, "_need_gpu", lambda d: None)
+    monkeypatch.setattr(aflex.Workspace, "get", lambda self, n, d: torch.zeros(256, dtype=torch.uint8))
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: -1)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+    a = synth.custom_attention(0, 2, 8, 2, 64, [20, 33], ctx_hi=64)
+    s = aflex.BlockSummary.of(a)
+    x = torch.zeros(2, 12, 64, dtype=torch.bfloat16)
+    q, k, v = x[:, :8], x[:, 8:10], x[:, 10:]
+    rope = aflex.rope_table(64, 32)
+    pos, cu = torch.zeros(2, dtype=torch.int32), torch.tensor([0, 1, 2], dtype=torch.int32)
+    out, sel = torch.empty_like(a.q), torch.zeros(2, 2, 3, dtype=torch.int32)
+
+    def fields(c):
+        b = c.from_buffer_copy(got["block"])
+        return {f: getattr(b, f) for f, _ in c._fields_}
+
+    P = lambda t: t.data_ptr()  # noqa: E731
+    cache = dict(k_cache=P(a.k_cache), block_table=P(a.block_table), context_lens=P(a.context_lens))
+    sizes = dict(B=2, Hkv=2, D=64, block_size=16, max_blocks_per_seq=4, num_blocks=a.num_blocks)
+    aflex.rope_write(a, q, k, v, cu, rope, max_seqlen=1, interleaved=True, positions=pos, summary=s, q_out=out)
+    assert fields(aflex.RopeArgs) == dict(
+        q=P(q), k_new=P(k), v_new=P(v), rope=P(rope), positions=P(pos), cu_seqlens=P(cu), q_out=P(out),
+        v_cache=P(a.v_cache), block_keys=P(s.keys), block_exp=P(s.exp), T=2, Hq=8, rotary_dim=32, interleaved=1,
+        rope_len=64, max_seqlen=1, q_stride=768, k_stride=768, v_stride=768, **cache, **sizes)
+    aflex.rope_append(a, q, k, v, None, q_out=out)
+    f = fields(aflex.RopeArgs)
+    assert (f["rope"], f["positions"], f["cu_seqlens"], f["block_keys"], f["block_exp"]) == (None,) * 5
+    assert (f["rotary_dim"], f["rope_len"], f["interleaved"]) == (0, 0, 0)
+    aflex.block_summary(a, s)
+    assert fields(aflex.BlockSummaryArgs) == dict(block_keys=P(s.keys), block_exp=P(s.exp), max_context_len=64, **cache,
+                                                  **sizes)
+    aflex.block_select(a, a.q, s, 3, 1, 2, out=sel)
+    del cache["k_cache"]
+    assert fields(aflex.BlockSelectArgs) == dict(
+        q=P(a.q), block_keys=P(s.keys), block_exp=P(s.exp), selected=P(sel), Hq=8, max_context_len=64, top_blocks=3,
+        sink_blocks=1, recent_blocks=2, **cache, **sizes)
+    aflex.attn_sparse_decode(a, sel, out=out, scale=0.5)
+    f = fields(aflex.AttnSparseArgs)
+    assert (f["selected"], f["top_blocks"]) == (P(sel), 3)
+    assert fields(aflex.AttnArgs) == dict(
+        q=P(a.q), k_cache=P(a.k_cache), v_cache=P(a.v_cache), out=P(out), Hq=8, max_context_len=64, scale=0.5,
+        split_tokens=0, **cache, **sizes)
