@@ -77,8 +77,8 @@ __device__ __forceinline__ float two_to(int n) { return __int_as_float((n + 127)
 // difference of the bit patterns: one instruction to round, and sums of
 // integers, the same in any order. The rows are added by halving: at each step
 // a lane gives away half of its channels, 14 (D = 128) or 15 exchanges instead
-// of 48 or 64, most of them without LDS. (With float sums, __shfl_xor and 4
-// tiles in a row per wave, 366 MB of keys took 165 us.)
+// of 48 or 64, most of them without LDS. (With float sums and __shfl_xor 366 MB of
+// keys took 165 us, so 78; about 200 vector instructions per 4 KiB tile.)
 template <int D>
 __device__ __forceinline__ void block_codes(const uint4 (&row)[D / 64][2], int d0, int d1, int lane, int8_t* keys,
                                             int8_t* exp) {
