@@ -45,6 +45,7 @@ constexpr int kPickThreads = 1024;
 constexpr int kBins = 2048;
 constexpr int kListed = 4096;       // longest list of keys that a work-group holds
 constexpr int kFusedBlocks = 1024;  // of those that it scores as well
+constexpr int kSplitUnits = 1024;
 
 // Unsigned order of the keys is the order of the floats (-0 and 0 are equal).
 __device__ __forceinline__ uint32_t order_key(float f) {
@@ -286,11 +287,12 @@ __global__ __launch_bounds__(kScoreThreads, 4) void block_score_kernel(aflex_blo
   const int heads = head_slots(a.Hkv), slots = NW / heads;
   const int workers = gridDim.x * slots, worker = blockIdx.x * slots + wave / heads;
   auto rounds_of = [&](int b) {
-    const int n = b < a.B ? nblk16(clamp_len(a, b)) : 0;
-    return n > a.top_blocks ? (n + 63) >> 6 : 0;
+    const int n = nblk16(clamp_len(a, min(b, a.B - 1)));
+    return b < a.B && n > a.top_blocks ? (n + 63) >> 6 : 0;
   };
   int total = 0;
-  for (int b = 0; b < a.B; b += 64) total += __builtin_amdgcn_readlane(wave_scan(rounds_of(b + lane)), 63);
+  for (int b = lane; b < a.B; b += 64) total += rounds_of(b);
+  total = __builtin_amdgcn_readlane(wave_scan(total), 63);
   const int per = (total + workers - 1) / workers;
   int x = worker * per;
   const int end = min(x + per, total);
@@ -476,14 +478,15 @@ __device__ __forceinline__ bool trivial_row(int n, int top, int32_t* out) {
   return true;
 }
 
-// Choice from a unit's scores in memory, at most kListed.
+// Choice from a unit's scores in memory, at most kListed (longer units are
+// another launch's).
 __global__ __launch_bounds__(kChooseThreads, 6) void block_choose_kernel(aflex_block_select_args a, int stride,
                                                                          const uint32_t* keys) {
   constexpr int NT = kChooseThreads;
   __shared__ PickShared sh;
   const int unit = blockIdx.x, n = nblk16(clamp_len(a, unit / a.Hkv));
   int32_t* out = a.selected + (size_t)unit * a.top_blocks;
-  if (trivial_row<NT>(n, a.top_blocks, out)) return;
+  if (n > kListed || trivial_row<NT>(n, a.top_blocks, out)) return;
   const Held<NT> held(keys + (size_t)unit * stride, n);  // (rows are padded to a multiple of 4)
   clear_bins<NT>(sh);
   __syncthreads();
@@ -499,7 +502,7 @@ __global__ __launch_bounds__(kChooseThreads, 6) void block_choose_kernel(aflex_b
 // keeps in registers, or 0: they are read again for every pass.
 template <int R>
 __global__ __launch_bounds__(kPickThreads) void block_pick_kernel(aflex_block_select_args a, int stride,
-                                                                  const uint32_t* keys) {
+                                                                  const uint32_t* keys, bool long_only) {
   constexpr int NT = kPickThreads;
   __shared__ PickShared sh;
   __shared__ __attribute__((aligned(16))) uint32_t list_key[kListed];
@@ -507,7 +510,7 @@ __global__ __launch_bounds__(kPickThreads) void block_pick_kernel(aflex_block_se
   const int unit = blockIdx.x, b = unit / a.Hkv, tid = threadIdx.x, lane = tid & 63;
   const int n = nblk16(clamp_len(a, b)), N = a.top_blocks;
   int32_t* out = a.selected + (size_t)unit * N;
-  if (trivial_row<NT>(n, N, out)) return;
+  if ((long_only && n <= kListed) || trivial_row<NT>(n, N, out)) return;
   const uint32_t* src = keys + (size_t)unit * stride;  // (rows are padded to a multiple of 4)
   clear_bins<NT>(sh);
   // a short sequence among long ones, or under a loose bound (131072 tokens: 64
@@ -689,12 +692,17 @@ hipError_t launch_block_select(const aflex_block_select_args& a, void* ws, hipSt
   {
     ProfScope ps("block_pick", stream);
     constexpr int kRounds = 8;
-    if (stride <= kListed)
-      block_choose_kernel<<<units, kChooseThreads, 0, stream>>>(a, stride, keys);
-    else if (stride <= kRounds * 4 * kPickThreads)
-      block_pick_kernel<kRounds><<<units, kPickThreads, 0, stream>>>(a, stride, keys);
-    else
-      block_pick_kernel<0><<<units, kPickThreads, 0, stream>>>(a, stride, keys);
+    // Where units may be long but are many, the short ones are chosen by the
+    // smaller kernel, three work-groups of which a CU holds, and a launch of its
+    // own (under a bound of 131072 tokens, one launch / two: 2048 units of median
+    // 3000 tokens 44.1 / 32.5 us, 1024 of 5000 30.1 / 25.2, 512 of 20000 32.4 / 32.0,
+    // 256 of 20000 20.2 / 21.9).
+    const bool split = stride > kListed && units >= kSplitUnits;
+    if (stride <= kListed || split) block_choose_kernel<<<units, kChooseThreads, 0, stream>>>(a, stride, keys);
+    if (stride > kRounds * 4 * kPickThreads)
+      block_pick_kernel<0><<<units, kPickThreads, 0, stream>>>(a, stride, keys, split);
+    else if (stride > kListed)
+      block_pick_kernel<kRounds><<<units, kPickThreads, 0, stream>>>(a, stride, keys, split);
   }
   return hipGetLastError();
 }

@@ -365,6 +365,13 @@ def test_block_select_long_sequences_among_many_short(gpu_lib):
     _choice(53, ctx, (4, 2, 64), 20, 1, 1)
 
 
+def test_block_select_many_units_under_a_long_bound(gpu_lib):
+    """1024 units, most of them short: long and short ones are chosen by launches of their own."""
+    ctx = [16 * (i % 40) + i % 17 for i in range(128)]
+    ctx[5], ctx[77], ctx[100] = 70000, 66000, 30000
+    _choice(55, ctx, (8, 8, 64), 20, 1, 1)
+
+
 def test_block_select_scores_too_small_for_fp32(gpu_lib):
     """Scores of both signs that round to zero are equal."""
     def tiny(a, s):
