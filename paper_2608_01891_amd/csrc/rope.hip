@@ -315,6 +315,11 @@ __global__ __launch_bounds__(256) void rope_write_kernel(aflex_rope_args a, int 
 // Tiles in a row per wave (375 MB of keys and summaries / 16 short contexts: one
 // tile 77.3 / 5.5 us, two 76.3 / 6.3, four 78.7 / 7.6, eight 82.2 / 11.9).
 constexpr int kTilesPerWave = 2;
+// Work-groups in all, at least 16 per sequence; they step on over a longer context.
+// One for every tile of the bound / at most this many: 64 sequences of median 1500
+// tokens under a bound of 131072, 114.9 / 46.6 us, 256 of 400 under 32768, 116.5 /
+// 51.7; 8 of 20000 under 65536, 76.2 / 76.5; 16 of 300 under 1024, 6.3 / 6.4.
+constexpr int kSummaryWgs = 32768;
 
 template <int D>
 __global__ __launch_bounds__(256, 6) void block_summary_kernel(aflex_block_summary_args a) {
@@ -323,12 +328,9 @@ __global__ __launch_bounds__(256, 6) void block_summary_kernel(aflex_block_summa
   const int b = blockIdx.y;
   const int ctx = min(max(a.context_lens[b], 0), a.max_context_len);
   const int tiles = ctx / 16 * a.Hkv;
-  const int t0 = (int)(blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6)) * kTilesPerWave;
-  if (t0 >= tiles) return;
   const int u = lane % U, r = lane / U;
   const int32_t* table = a.block_table + (size_t)b * a.max_blocks_per_seq;
-  int j = t0 / a.Hkv, g = t0 - j * a.Hkv;
-  const int count = min(kTilesPerWave, tiles - t0);
+  int j, g;
   // (tiles of a block one after the other in memory; the next one's loads go out first)
   auto tile_of = [&]() -> long long {
     const int blk = table[j];
@@ -341,23 +343,30 @@ __global__ __launch_bounds__(256, 6) void block_summary_kernel(aflex_block_summa
 #pragma unroll
       for (int c = 0; c < 2; ++c) row[i][c] = ld4(p + i * RS * D + c * 8);
   };
-  long long tile = tile_of();
-  uint4 row[NR][2];
-  load(tile, row);
-  for (int k = 0; k < count; ++k) {
-    uint4 next[NR][2];
-    long long next_tile = -1;
-    if (k + 1 < count) {
-      if (++g == a.Hkv) g = 0, ++j;
-      next_tile = tile_of();
-      load(next_tile, next);
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  for (long long t0 = ((long long)blockIdx.x * 4 + wave) * kTilesPerWave; t0 < tiles;
+       t0 += (long long)gridDim.x * 4 * kTilesPerWave) {
+    j = (int)t0 / a.Hkv;
+    g = (int)t0 - j * a.Hkv;
+    const int count = min(kTilesPerWave, tiles - (int)t0);
+    long long tile = tile_of();
+    uint4 row[NR][2];
+    load(tile, row);
+    for (int k = 0; k < count; ++k) {
+      uint4 next[NR][2];
+      long long next_tile = -1;
+      if (k + 1 < count) {
+        if (++g == a.Hkv) g = 0, ++j;
+        next_tile = tile_of();
+        load(next_tile, next);
+      }
+      if (tile >= 0) block_codes<D>(row, u * 16, u * 16 + 8, lane, a.block_keys + tile * D, a.block_exp + tile);
+      tile = next_tile;
+#pragma unroll
+      for (int i = 0; i < NR; ++i)
+#pragma unroll
+        for (int c = 0; c < 2; ++c) row[i][c] = next[i][c];
     }
-    if (tile >= 0) block_codes<D>(row, u * 16, u * 16 + 8, lane, a.block_keys + tile * D, a.block_exp + tile);
-    tile = next_tile;
-#pragma unroll
-    for (int i = 0; i < NR; ++i)
-#pragma unroll
-      for (int c = 0; c < 2; ++c) row[i][c] = next[i][c];
   }
 }
 
@@ -413,7 +422,11 @@ hipError_t launch_rope_write(const aflex_rope_args& in, hipStream_t stream) {
 hipError_t launch_block_summary(const aflex_block_summary_args& a, hipStream_t stream) {
   const long long tiles = (long long)(a.max_context_len / 16) * a.Hkv;
   if (tiles == 0) return hipSuccess;
-  const dim3 grid((unsigned)((tiles + 4 * kTilesPerWave - 1) / (4 * kTilesPerWave)), a.B);
+  // Work-groups for the longest context, but no more than kSummaryWgs in all: under
+  // a loose bound most would find nothing to do.
+  const long long need = (tiles + 4 * kTilesPerWave - 1) / (4 * kTilesPerWave);
+  const long long most = kSummaryWgs / a.B > 16 ? kSummaryWgs / a.B : 16;
+  const dim3 grid((unsigned)(need < most ? need : most), a.B);
   ProfScope ps("block_summary", stream);
   if (a.D == 128)
     block_summary_kernel<128><<<grid, 256, 0, stream>>>(a);

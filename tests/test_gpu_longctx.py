@@ -280,6 +280,18 @@ def test_block_summary(gpu_lib, heads):
     assert torch.equal(sd.keys.cpu(), keys) and torch.equal(sd.exp.cpu(), exp)
 
 
+def test_block_summary_more_tiles_than_work_groups(gpu_lib):
+    """2100 sequences leave each 16 work-groups, 128 tiles a pass: 200 and 136 tiles take two."""
+    ctx = [0, 16, 15] * 700
+    ctx[0], ctx[1], ctx[2099] = 405, 256, 272
+    heads = (8, 8, 64)
+    a = _odd_keys(32, synth.custom_attention(32, len(ctx), *heads, ctx, ctx_hi=416))
+    s = _summary_bytes(a)
+    sd = aflex.block_summary(a.to(DEV), aflex.BlockSummary(s.keys.to(DEV), s.exp.to(DEV)))
+    keys, exp = lc.block_summary(a.k_cache, a.block_table, a.context_lens, s.keys, s.exp)
+    assert torch.equal(sd.keys.cpu(), keys) and torch.equal(sd.exp.cpu(), exp)
+
+
 # ------------------------------------------------------------------ the choice
 def _choice(seed, ctx, heads, top, sink, recent, edit=None):
     Hq, Hkv, D = heads
