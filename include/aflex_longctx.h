@@ -15,7 +15,9 @@
  * the choice D + 1 bytes per 16 tokens and kv head, a 64th of the K and V of
  * those tokens. The conventions of aflex.h hold (device pointers, alignment,
  * streams, workspaces, validation before launch, errors); strides are counted
- * in elements.
+ * in elements. block_select and attn_sparse_decode may be several launches that
+ * communicate through the workspace: calls that share one run on one stream,
+ * and are made by one host thread at a time.
  */
 #ifndef AFLEX_LONGCTX_H
 #define AFLEX_LONGCTX_H

@@ -12,6 +12,7 @@ import ctypes
 import gc
 import os
 import re
+import threading
 
 import torch
 
@@ -263,11 +264,16 @@ def _need_gpu(device):
 
 
 class Workspace:
-    """Grow-only device scratch handed to the library (allocated by torch)."""
+    """Grow-only device scratch handed to the library (allocated by torch).
+
+    A call may be several launches that communicate through the scratch. `lock`
+    is held while one is made, so that a second host thread's call on the same
+    stream comes behind all of them, not between two."""
 
     def __init__(self, device=None):
         self.device = device
         self.buf = None
+        self.lock = threading.RLock()
 
     def fits(self, nbytes: int, device):
         return self.buf is not None and self.buf.numel() >= nbytes and self.buf.device == torch.device(device)
@@ -615,7 +621,8 @@ def _empty(stream, dev, *shape, dtype=torch.bfloat16):
 def _run_own_ws(name, dev, ws, stream, *items):
     """Call an entry point with a workspace on the current device. The default
     one belongs to the (device, stream) that the call runs on, so calls on two
-    streams do not share it; while a graph is captured the call gets one of the
+    streams do not share it, and those of two host threads on one stream take
+    turns (Workspace.lock); while a graph is captured the call gets one of the
     graph's own memory."""
     handle = _stream(stream)
     if ws is None:
@@ -631,19 +638,20 @@ def _run_own_ws(name, dev, ws, stream, *items):
             ws = _default_ws.get(key) or _default_ws.setdefault(key, Workspace())
     elif stream is not None and ws.buf is not None:
         ws.buf.record_stream(stream)  # (a caller's may be used on several)
-    buf = ws.buf
-    if buf is not None and buf.get_device() == dev:
-        status = _call(_entry[name], dev, handle, buf.data_ptr(), buf.numel(), *items)
-        if status != ERR_WORKSPACE:
-            return _check(status)
-    status, need = _call(_entry[name + "_workspace"], dev, None, None, 0, *items)
-    _check(status)
-    if stream is None:
-        buf = ws.get(need, f"cuda:{dev}")
-    else:
-        with torch.cuda.stream(stream):
+    with ws.lock:
+        buf = ws.buf
+        if buf is not None and buf.get_device() == dev:
+            status = _call(_entry[name], dev, handle, buf.data_ptr(), buf.numel(), *items)
+            if status != ERR_WORKSPACE:
+                return _check(status)
+        status, need = _call(_entry[name + "_workspace"], dev, None, None, 0, *items)
+        _check(status)
+        if stream is None:
             buf = ws.get(need, f"cuda:{dev}")
-    _check(_call(_entry[name], dev, handle, buf.data_ptr(), buf.numel(), *items))
+        else:
+            with torch.cuda.stream(stream):
+                buf = ws.get(need, f"cuda:{dev}")
+        _check(_call(_entry[name], dev, handle, buf.data_ptr(), buf.numel(), *items))
 
 
 @_on_device

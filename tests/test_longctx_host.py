@@ -2,6 +2,8 @@
 refusals before any launch, workspace sizes, and what the binding refuses."""
 import ctypes
 import os
+import threading
+import time
 
 import pytest
 import torch
@@ -288,3 +290,52 @@ def test_calls_lay_out_the_argument_blocks(lib, monkeypatch):
     assert fields(aflex.AttnArgs) == dict(
         q=P(a.q), k_cache=P(a.k_cache), v_cache=P(a.v_cache), out=P(out), Hq=8, max_context_len=64, scale=0.5,
         split_tokens=0, **cache, **sizes)
+
+
+def _no_gpu(monkeypatch):
+    """Calls of the binding run on host tensors, up to aflex._call."""
+    monkeypatch.setattr(aflex, "_stream", lambda s: 0)
+    monkeypatch.setattr(aflex, "_default_ws", {})
+    monkeypatch.setattr(aflex, "_need_gpu", lambda d: None)
+    monkeypatch.setattr(torch._C, "_cuda_getDevice", lambda: -1)
+    monkeypatch.setattr(torch.cuda, "is_current_stream_capturing", lambda: False)
+
+
+@pytest.mark.parametrize("own_ws", [False, True])
+@pytest.mark.parametrize("op", ["block_select", "attn_sparse_decode"])
+def test_a_workspace_is_in_one_host_thread_at_a_time(lib, monkeypatch, op, own_ws):
+    """The two launches of a call communicate through the workspace: a second thread's call
+    on the same stream may not launch between them."""
+    _no_gpu(monkeypatch)
+    monkeypatch.setattr(aflex.Workspace, "get", lambda self, n, d: self.__dict__.setdefault(
+        "host", torch.zeros(256, dtype=torch.uint8)))
+    inside, met, entered = {}, [], threading.Event()
+
+    def call(entry, dev, stream, ws, nbytes, *items):
+        if stream is None:
+            return aflex.OK, 256
+        inside[ws] = inside.get(ws, 0) + 1
+        if inside[ws] > 1:
+            met.append(ws)
+        if entered.is_set():
+            time.sleep(0.01)
+        else:
+            entered.set()
+            time.sleep(0.3)  # the second thread comes here meanwhile, if it can
+        inside[ws] -= 1
+        return aflex.OK
+
+    monkeypatch.setattr(aflex, "_call", call)
+    a = synth.custom_attention(0, 2, 8, 2, 64, [20, 33], ctx_hi=64)
+    s, sel = aflex.BlockSummary.of(a), torch.zeros(2, 2, 3, dtype=torch.int32)
+    kw = {"ws": aflex.Workspace()} if own_ws else {}
+    run = {"block_select": lambda: aflex.block_select(a, a.q, s, 3, out=sel, **kw),
+           "attn_sparse_decode": lambda: aflex.attn_sparse_decode(a, sel, out=torch.empty_like(a.q), **kw)}[op]
+    threads = [threading.Thread(target=run) for _ in range(2)]
+    threads[0].start()
+    assert entered.wait(10)
+    threads[1].start()
+    for t in threads:
+        t.join(20)
+        assert not t.is_alive()
+    assert not met and len(inside) >= 1
