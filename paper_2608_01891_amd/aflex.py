@@ -288,13 +288,21 @@ class Workspace:
 _default_ws = {}
 
 
-def _ws(key, nbytes, device, ws, streams=()):
+def _own(key, ws):
+    """The caller's workspace, or the default one of this kind of call (calls on
+    several streams that may overlap take a workspace each)."""
+    if ws is None:
+        ws = _default_ws.get(key)
+        if ws is None:
+            ws = _default_ws.setdefault(key, Workspace())
+    return ws
+
+
+def _ws(nbytes, device, ws, streams=()):
     """Workspace pointer and size. The buffer comes from torch's caching allocator
     on the current stream; its use on any other stream is recorded, so that a
     later growth (which frees it) cannot hand the memory out while that stream
     still reads it."""
-    if ws is None:
-        ws = _default_ws.setdefault(key, Workspace())
     buf = ws.get(nbytes, device)
     for s in streams:
         if s is not None and s != torch.cuda.current_stream(buf.device):
@@ -312,23 +320,21 @@ def _run(name, args, key, device, ws, stream):
     Tensors that are not on a GPU are refused before any library call (a kernel would
     read and write the host's addresses): no workspace is ever on another device, so
     theirs is never at hand."""
-    if ws is None:
-        ws = _default_ws.get(key)
-        if ws is None:
-            ws = _default_ws.setdefault(key, Workspace())
+    ws = _own(key, ws)
     ref = ctypes.byref(args)
     fn = getattr(_lib, name)
-    if ws.fits(0, device):
-        p, sz = _ws(key, 0, device, ws, (stream,))
-        status = fn(ref, p, sz, _stream(stream))
-        if status != ERR_WORKSPACE:
-            _check(status)
-            return
-    _need_gpu(device)
-    n = ctypes.c_size_t()
-    _check(getattr(_lib, name + "_workspace")(ref, ctypes.byref(n)))
-    p, sz = _ws(key, n.value, device, ws, (stream,))
-    _check(fn(ref, p, sz, _stream(stream)))
+    with ws.lock:
+        if ws.fits(0, device):
+            p, sz = _ws(0, device, ws, (stream,))
+            status = fn(ref, p, sz, _stream(stream))
+            if status != ERR_WORKSPACE:
+                _check(status)
+                return
+        _need_gpu(device)
+        n = ctypes.c_size_t()
+        _check(getattr(_lib, name + "_workspace")(ref, ctypes.byref(n)))
+        p, sz = _ws(n.value, device, ws, (stream,))
+        _check(fn(ref, p, sz, _stream(stream)))
 
 
 # --------------------------------------------------------------------------
@@ -506,6 +512,12 @@ def af_pipeline_step(a, w, logits, k: int, mb_sizes, L: int = 1, y=None, stream_
     for the current stream; with ``join`` the current stream then waits for
     stream_f, so the result is ordered on the caller's stream.
     """
+    ws = _own("pipe", ws)
+    with ws.lock:
+        return _af_pipeline_step(a, w, logits, k, mb_sizes, L, y, stream_a, stream_f, ws, split_tokens, join)
+
+
+def _af_pipeline_step(a, w, logits, k, mb_sizes, L, y, stream_a, stream_f, ws, split_tokens, join):
     lib = load()
     if stream_a is None or stream_f is None:
         stream_a, stream_f = pipeline_streams(a.q.device)
@@ -521,7 +533,7 @@ def af_pipeline_step(a, w, logits, k: int, mb_sizes, L: int = 1, y=None, stream_
     n = ctypes.c_size_t()
     _check(lib.aflex_af_pipeline_workspace(ctypes.byref(aa), ctypes.byref(fa), M, mb, L,
                                            ctypes.byref(n)))
-    p, sz = _ws("pipe", n.value, a.q.device, ws, (stream_a, stream_f))
+    p, sz = _ws(n.value, a.q.device, ws, (stream_a, stream_f))
     _check(lib.aflex_af_pipeline_step(ctypes.byref(aa), ctypes.byref(fa), M, mb, L, p, sz,
                                       _stream(stream_a), _stream(stream_f)))
     if join:
@@ -536,6 +548,12 @@ def af_layer_step(a, w, layer, k: int, mb_sizes, L: int = 1, y=None, stream_a=No
     MoE block (RMSNorm, router, experts, residual) on stream_f. Appends the
     new K/V into a's pools in place; returns y [B, H]. Streams as for
     af_pipeline_step."""
+    ws = _own("layer", ws)
+    with ws.lock:
+        return _af_layer_step(a, w, layer, k, mb_sizes, L, y, stream_a, stream_f, ws, join)
+
+
+def _af_layer_step(a, w, layer, k, mb_sizes, L, y, stream_a, stream_f, ws, join):
     lib = load()
     if stream_a is None or stream_f is None:
         stream_a, stream_f = pipeline_streams(a.q.device)
@@ -555,7 +573,7 @@ def af_layer_step(a, w, layer, k: int, mb_sizes, L: int = 1, y=None, stream_a=No
     n = ctypes.c_size_t()
     _check(lib.aflex_af_layer_workspace(ctypes.byref(aa), ctypes.byref(fa), ctypes.byref(la), M, mb, L,
                                         ctypes.byref(n)))
-    p, sz = _ws("layer", n.value, a.q.device, ws, (stream_a, stream_f))
+    p, sz = _ws(n.value, a.q.device, ws, (stream_a, stream_f))
     _check(lib.aflex_af_layer_step(ctypes.byref(aa), ctypes.byref(fa), ctypes.byref(la), M, mb, L, p, sz,
                                    _stream(stream_a), _stream(stream_f)))
     if join:
