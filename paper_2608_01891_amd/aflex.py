@@ -273,6 +273,7 @@ class Workspace:
     def __init__(self, device=None):
         self.device = device
         self.buf = None
+        self.home = None  # handle of the stream that torch allocated buf on
         self.lock = threading.RLock()
 
     def fits(self, nbytes: int, device):
@@ -282,7 +283,15 @@ class Workspace:
         if not self.fits(nbytes, device):
             _need_gpu(device)
             self.buf = torch.empty(max(nbytes, 256), dtype=torch.uint8, device=device)
+            self.home = torch.cuda.current_stream(device).cuda_stream
         return self.buf
+
+    def used_on(self, handle, stream):
+        """buf is used on the stream of that handle (`stream`, or the current one): a
+        later growth, which frees it, must not hand the memory out while that stream
+        still reads it."""
+        if handle != self.home:
+            self.buf.record_stream(torch.cuda.current_stream(self.buf.device) if stream is None else stream)
 
 
 _default_ws = {}
@@ -300,13 +309,10 @@ def _own(key, ws):
 
 def _ws(nbytes, device, ws, streams=()):
     """Workspace pointer and size. The buffer comes from torch's caching allocator
-    on the current stream; its use on any other stream is recorded, so that a
-    later growth (which frees it) cannot hand the memory out while that stream
-    still reads it."""
+    on the current stream; its use on any other stream is recorded."""
     buf = ws.get(nbytes, device)
     for s in streams:
-        if s is not None and s != torch.cuda.current_stream(buf.device):
-            buf.record_stream(s)
+        ws.used_on(_stream(s), s)
     return buf.data_ptr(), buf.numel()
 
 
@@ -654,11 +660,10 @@ def _run_own_ws(name, dev, ws, stream, *items):
         else:
             key = (name, dev, handle)
             ws = _default_ws.get(key) or _default_ws.setdefault(key, Workspace())
-    elif stream is not None and ws.buf is not None:
-        ws.buf.record_stream(stream)  # (a caller's may be used on several)
     with ws.lock:
         buf = ws.buf
         if buf is not None and buf.get_device() == dev:
+            ws.used_on(handle, stream)  # (a caller's may be used on several)
             status = _call(_entry[name], dev, handle, buf.data_ptr(), buf.numel(), *items)
             if status != ERR_WORKSPACE:
                 return _check(status)

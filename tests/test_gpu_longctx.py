@@ -615,3 +615,32 @@ def test_pools_of_more_than_2_to_the_31_elements(gpu_lib):
         assert torch.equal(x, y)
     assert torch.equal(res[0][3].keys, res[1][3].keys[move]) and torch.equal(res[0][3].exp, res[1][3].exp[move])
     assert torch.equal(small.k_cache, big.k_cache[move]) and torch.equal(small.v_cache, big.v_cache[move])
+
+
+@pytest.mark.parametrize("op", ["attn_sparse_decode", "attn_decode"])
+def test_workspace_grown_while_another_stream_reads_it(gpu_lib, op):
+    """A caller's workspace used on a busy stream, then grown on the one it is from: its
+    memory is not handed out before the busy stream is done."""
+    small, large = [(a.to(DEV), _lists(101, a, 70).to(DEV)) for a in (
+        synth.custom_attention(99, 2, 8, 2, 128, [2000, 1500]), synth.custom_attention(100, 64, 8, 2, 128, [600] * 64))]
+
+    def run(x, ws):
+        return aflex.attn_decode(x[0], ws=ws) if op == "attn_decode" else aflex.attn_sparse_decode(*x, ws=ws)
+
+    want = run(small, None)
+    ws, side = aflex.Workspace(), torch.cuda.Stream()
+    run(small, ws)
+    torch.cuda.synchronize()
+    at, size = ws.buf.data_ptr(), ws.buf.numel()
+    with torch.cuda.stream(side):
+        torch.cuda._sleep(100_000_000)
+        got = run(small, ws)
+    run(large, ws)
+    assert not side.query()  # still asleep
+    assert ws.buf.numel() > size
+    other = [torch.empty(size, dtype=torch.uint8, device=DEV) for _ in range(4)]
+    assert all(not t.data_ptr() <= at < t.data_ptr() + size for t in other)
+    for t in other:
+        t.fill_(255)
+    torch.cuda.synchronize()
+    assert torch.equal(got, want)

@@ -1,5 +1,6 @@
-"""A workspace is in one host thread at a time: the launches of a call
-communicate through it (no GPU needed: the library is a stub)."""
+"""Workspaces shared by host threads and by streams (no GPU needed: the library
+is a stub). One host thread at a time: the launches of a call communicate
+through it. Its use on a stream other than its own is recorded."""
 import ctypes
 import threading
 import time
@@ -70,3 +71,41 @@ def test_one_host_thread_at_a_time(monkeypatch, op, own_ws):
         t.join(20)
         assert not t.is_alive()
     assert len(lib.inside) == 1 and not lib.met
+
+
+class Buffer:
+    device = torch.device("cuda:0")
+
+    def __init__(self):
+        self.recorded = []
+
+    def record_stream(self, s):
+        self.recorded.append(s)
+
+    def get_device(self):
+        return 0
+
+    def data_ptr(self):
+        return 256
+
+    def numel(self):
+        return 1 << 20
+
+
+@pytest.mark.parametrize("stream", [None, "given"])
+@pytest.mark.parametrize("call", ["_run", "_run_own_ws"])
+def test_use_on_another_stream_is_recorded(monkeypatch, call, stream):
+    """Also where the other stream is the current one, and no stream is given."""
+    monkeypatch.setattr(aflex, "_lib", Lib())
+    monkeypatch.setattr(aflex, "_call", lambda *args: aflex.OK)
+    monkeypatch.setattr(aflex, "_entry", {"aflex_linear": 0})
+    monkeypatch.setattr(torch.cuda, "current_stream", lambda d=None: "current")
+    ws = aflex.Workspace()
+    ws.buf, ws.home = Buffer(), 7
+    for handle, want in ((7, []), (9, [stream or "current"])):
+        monkeypatch.setattr(aflex, "_stream", lambda s: handle)
+        if call == "_run":
+            aflex._run("aflex_linear", aflex.LinearArgs(), "linear", Buffer.device, ws, stream)
+        else:
+            aflex._run_own_ws("aflex_linear", 0, ws, stream)
+        assert ws.buf.recorded == want
