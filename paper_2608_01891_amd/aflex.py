@@ -110,7 +110,7 @@ class AflexError(RuntimeError):
 
 
 _lib = None
-_call, _entry = None, {}  # of _tensor_args, and addresses of entry points (see load)
+_call, _call_error, _entry = None, None, {}  # of _tensor_args, and addresses of entry points (see load)
 _SZ = ctypes.POINTER(ctypes.c_size_t)
 
 
@@ -122,18 +122,19 @@ def exported_names(header=HEADER):
 
 
 def load():
-    """Open the built library (cached). Raises if it has not been built."""
-    global _lib, _call
+    """Open the built library (cached). Raises if it has not been built. The module
+    that the long-context operators are called through is loaded with it; where it
+    cannot be, those operators raise and the others run."""
+    global _lib, _call, _call_error
     if _lib is not None:
         return _lib
     if not os.path.exists(LIB_PATH):
         raise RuntimeError(f"{LIB_PATH} is missing: build it with `python -m paper_2608_01891_amd.build`")
     try:
         from . import _tensor_args
+        _call = _tensor_args.call
     except ImportError as e:
-        raise RuntimeError(f"{_PKG}/_tensor_args.so cannot be loaded: build it with "
-                           "`python -m paper_2608_01891_amd.build`") from e
-    _call = _tensor_args.call
+        _call_error = e
     lib = ctypes.CDLL(LIB_PATH)
     AP, FP = ctypes.POINTER(AttnArgs), ctypes.POINTER(FfnArgs)
     I32P = ctypes.POINTER(ctypes.c_int32)
@@ -625,6 +626,9 @@ def _on_device(f):
     def run(t, *args):
         if _lib is None:
             load()
+        if _call is None:
+            raise RuntimeError(f"{_PKG}/_tensor_args.so cannot be loaded: build it with "
+                               "`python -m paper_2608_01891_amd.build`") from _call_error
         dev = t.get_device()
         if dev < 0:
             _need_gpu(t.device)

@@ -2,6 +2,7 @@
 refusals before any launch, workspace sizes, and what the binding refuses."""
 import ctypes
 import os
+import sys
 import threading
 import time
 
@@ -339,3 +340,18 @@ def test_a_workspace_is_in_one_host_thread_at_a_time(lib, monkeypatch, op, own_w
         t.join(20)
         assert not t.is_alive()
     assert not met and len(inside) >= 1
+
+
+def test_older_operators_load_without_the_call_module(lib, monkeypatch):
+    """The library alone serves the operators that are called through ctypes; the long-context ones say what is missing."""
+    calls = _calls()
+    import paper_2608_01891_amd as package
+    monkeypatch.delattr(package, "_tensor_args", raising=False)
+    monkeypatch.setitem(sys.modules, "paper_2608_01891_amd._tensor_args", None)  # its import fails
+    monkeypatch.setattr(aflex, "_lib", None)
+    monkeypatch.setattr(aflex, "_call", None)
+    monkeypatch.setattr(aflex.atexit, "register", lambda f: None)
+    assert aflex.load().aflex_kv_append(None, None) == INVALID
+    for op in calls.values():
+        with pytest.raises(RuntimeError, match="_tensor_args.so cannot be loaded"):
+            op()
