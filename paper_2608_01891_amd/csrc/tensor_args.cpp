@@ -77,10 +77,10 @@ bool numbers(PyObject* const* args, int n, long long* out) {
 //                                       whose rows do not overlap; their stride (elements; 0 for one
 //                                       row at most) is kept
 //   None                                the next kept stride
-//   int, float                          a number of 4 bytes
+//   int (or what stands for one, as numpy's integers do), float   a number of 4 bytes
 Py_ssize_t item(PyObject* const* args, Py_ssize_t n, long dev, Block& b) {
   PyObject* o = args[0];
-  if (PyLong_Check(o)) {
+  if (PyIndex_Check(o)) {
     long long v;
     return numbers(args, 1, &v) && b.put_int(v);
   }

@@ -6,6 +6,7 @@ import sys
 import threading
 import time
 
+import numpy as np
 import pytest
 import torch
 
@@ -355,3 +356,15 @@ def test_older_operators_load_without_the_call_module(lib, monkeypatch):
     for op in calls.values():
         with pytest.raises(RuntimeError, match="_tensor_args.so cannot be loaded"):
             op()
+
+
+def test_sizes_may_be_whole_numbers_of_other_types(lib):
+    """numpy's integers, as max() of an array of lengths gives; not strings, lists or fractions of them."""
+    b = _block_of(np.int64(640), np.int32(-3), np.uint8(7), True, 5)
+    assert [int.from_bytes(b[4 * i:4 * i + 4], "little", signed=True) for i in range(5)] == [640, -3, 7, 1, 5]
+    assert _block_of(np.float64(0.5))[:4] == _block_of(0.5)[:4]
+    with pytest.raises(OverflowError):
+        _block_of(np.int64(1 << 31))
+    for bad in (np.float32(2.0), [3], b"4", torch.ones(2)):
+        with pytest.raises(TypeError):
+            _block_of(bad)
