@@ -46,19 +46,21 @@ __device__ __forceinline__ int wave_max(int v) {
 }
 
 // Halving sum over lanes that differ in bit M of their number: lanes without
-// the bit get lo of both, lanes with it hi of both.
+// the bit get lo of both, lanes with it hi of both. (Unsigned, as all sums here:
+// bits of two's complement, which may pass 2^31 on the way.)
 template <int M>
-__device__ __forceinline__ int halve(int lo, int hi, int lane) {
+__device__ __forceinline__ uint32_t halve(uint32_t lo, uint32_t hi, int lane) {
   if constexpr (M == 32) {
-    const auto r = __builtin_amdgcn_permlane32_swap((unsigned)lo, (unsigned)hi, false, false);
-    return (int)(r[0] + r[1]);
+    const auto r = __builtin_amdgcn_permlane32_swap(lo, hi, false, false);
+    return r[0] + r[1];
   } else if constexpr (M == 16) {
-    const auto r = __builtin_amdgcn_permlane16_swap((unsigned)lo, (unsigned)hi, false, false);
-    return (int)(r[0] + r[1]);
+    const auto r = __builtin_amdgcn_permlane16_swap(lo, hi, false, false);
+    return r[0] + r[1];
   } else {
     const bool up = lane & M;
-    const int keep = up ? hi : lo, give = up ? lo : hi;
-    if constexpr (M == 8) return keep + __builtin_amdgcn_update_dpp(0, give, 0x128, 0xf, 0xf, false);  // row_ror 8
+    const uint32_t keep = up ? hi : lo, give = up ? lo : hi;
+    if constexpr (M == 8)
+      return keep + (uint32_t)__builtin_amdgcn_update_dpp(0, (int)give, 0x128, 0xf, 0xf, false);  // row_ror 8
     return keep + __shfl_xor(give, M);
   }
 }
@@ -83,7 +85,7 @@ template <int D>
 __device__ __forceinline__ void block_codes(const uint4 (&row)[D / 64][2], int d0, int d1, int lane, int8_t* keys,
                                             int8_t* exp) {
   constexpr int NR = TileLanes<D>::NR;
-  constexpr int kOne = 0x4b400000;  // bits of 1.5 2^23
+  constexpr uint32_t kOne = 0x4b400000;  // bits of 1.5 2^23
   u16x2 m2 = {0, 0};
 #pragma unroll
   for (int i = 0; i < NR; ++i)
@@ -94,23 +96,23 @@ __device__ __forceinline__ void block_codes(const uint4 (&row)[D / 64][2], int d
   const bool fine = mag < 0x7f80;
   const int e = exponent_above(mag);
   const float f = two_to(14 - e);
-  int s[16];
+  uint32_t s[16];
 #pragma unroll
   for (int c = 0; c < 2; ++c) {
 #pragma unroll
     for (int j = 0; j < 8; ++j) {
-      int t = 0;
+      uint32_t t = 0;
 #pragma unroll
       for (int i = 0; i < NR; ++i) {
         const uint4& v = row[i][c];
         const uint32_t w = j < 2 ? v.x : j < 4 ? v.y : j < 6 ? v.z : v.w;
         const float k = __uint_as_float((j & 1) ? (w & 0xffff0000u) : (w << 16));
-        t += __float_as_int(fmaf(k, f, __int_as_float(kOne)));
+        t += __float_as_uint(fmaf(k, f, __uint_as_float(kOne)));
       }
-      s[c * 8 + j] = t - (int)((unsigned)NR * kOne);
+      s[c * 8 + j] = t - NR * kOne;
     }
   }
-  int a[8], b[4], h[2];
+  uint32_t a[8], b[4], h[2];
 #pragma unroll
   for (int i = 0; i < 8; ++i) a[i] = halve<32>(s[i], s[i + 8], lane);
 #pragma unroll
@@ -118,18 +120,19 @@ __device__ __forceinline__ void block_codes(const uint4 (&row)[D / 64][2], int d
 #pragma unroll
   for (int i = 0; i < 2; ++i) h[i] = halve<8>(b[i], b[i + 2], lane);
   int d = (lane & 32 ? d1 : d0) + (lane & 16 ? 4 : 0) + (lane & 8 ? 2 : 0);
-  int big;
   if constexpr (D == 64) {
     h[0] = halve<4>(h[0], h[1], lane);
     h[1] = 0;
     d += lane & 4 ? 1 : 0;
   }
-  big = wave_max(max(abs(h[0]), abs(h[1])));
+  // (magnitudes below 2^18; of a tile that is not fine, any bits)
+  const auto size = [](uint32_t x) { return (int)(x >> 31 ? 0u - x : x); };
+  const int big = wave_max(max(size(h[0]), size(h[1])));
   const int r = max(32 - __clz(big) - 7, 0);  // (__clz(0) is 32)
   const float g = two_to(-r);
   int code[2];
 #pragma unroll
-  for (int i = 0; i < 2; ++i) code[i] = fine ? (int)fminf(fmaxf(rintf((float)h[i] * g), -127.f), 127.f) : 0;
+  for (int i = 0; i < 2; ++i) code[i] = fine ? (int)fminf(fmaxf(rintf((float)(int)h[i] * g), -127.f), 127.f) : 0;
   if constexpr (D == 128)
     *reinterpret_cast<uint16_t*>(keys + d) = (uint16_t)((code[0] & 0xff) | (code[1] << 8));
   else
