@@ -75,14 +75,17 @@ typedef struct aflex_rope_args {
                                   of at least H D; 0: dense */
 } aflex_rope_args;
 
-/* Supported: D in {64, 128}, block_size == 16, B <= 65535 for                */
-/* aflex_rope_write. No workspace. Device-side values are clamped as in        */
-/* aflex_kv_append and aflex_kv_write: sequences with context_lens outside     */
-/* [1, capacity], tokens before place 0 and, with rotary_dim > 0, tokens whose */
-/* position is outside [0, rope_len) are left alone (neither q_out nor the    */
-/* cache is written for them); for a block id outside [0, num_blocks) only     */
-/* q_out is written. A block must not appear twice among the slots written.   */
-/* Tokens beyond max_seqlen may be left alone.                                 */
+/* Supported: D in {64, 128}, block_size == 16, rows of fewer than 2^30     */
+/* elements; for aflex_rope_append B (Hq + Hkv) < 2^30 and B (Hkv + Hq D /  */
+/* 1024) < 2^26 - 4; for aflex_rope_write B <= 65535, at most 4096 heads,   */
+/* max_seqlen <= T and max_seqlen <= 2^28 - 32. No workspace. Device-side   */
+/* values are clamped as in aflex_kv_append and aflex_kv_write: sequences   */
+/* with context_lens outside [1, capacity], tokens before place 0 and, with */
+/* rotary_dim > 0, tokens whose position is outside [0, rope_len) are left  */
+/* alone (neither q_out nor the cache is written for them); for a block id  */
+/* outside [0, num_blocks) only q_out is written. A block must not appear   */
+/* twice among the slots written. Tokens beyond max_seqlen may be left      */
+/* alone.                                                                   */
 aflex_status aflex_rope_append(const aflex_rope_args *a, aflex_stream stream);
 aflex_status aflex_rope_write(const aflex_rope_args *a, aflex_stream stream);
 
@@ -137,7 +140,8 @@ typedef struct aflex_block_select_args {
 } aflex_block_select_args;
 
 /* Supported: D in {64, 128}, block_size == 16, Hq % Hkv == 0,                 */
-/* Hq / Hkv <= 16, B * Hkv * ceil(max_context_len / 16) < 2^30,                */
+/* Hq / Hkv <= 16, B * Hkv < 2^24,                                             */
+/* B * Hkv * ceil(max_context_len / 16) < 2^30,                                */
 /* B * Hkv * top_blocks < 2^30. The workspace needs no initialisation.         */
 aflex_status aflex_block_select_workspace(const aflex_block_select_args *a, size_t *bytes);
 aflex_status aflex_block_select(const aflex_block_select_args *a, void *workspace, size_t workspace_bytes,
@@ -156,10 +160,11 @@ typedef struct aflex_attn_sparse_args {
   int32_t top_blocks;          /* >= 1 */
 } aflex_attn_sparse_args;
 
-/* Supported: as aflex_attn_decode, and B * Hkv * top_blocks < 2^30. The same  */
-/* result on every call with the same inputs (bitwise). The softmax weights    */
-/* are rounded to bf16 for the product with the values and summed as rounded;  */
-/* scores, sums and the merge of split lists are fp32.                         */
+/* Supported: as aflex_attn_decode, and B * Hkv < 2^24, B * Hkv *           */
+/* top_blocks < 2^30. The same result on every call with the same inputs    */
+/* (bitwise). The softmax weights are rounded to bf16 for the product with  */
+/* the values and summed as rounded; scores, sums and the merge of split    */
+/* lists are fp32.                                                          */
 aflex_status aflex_attn_sparse_decode_workspace(const aflex_attn_sparse_args *a, size_t *bytes);
 aflex_status aflex_attn_sparse_decode(const aflex_attn_sparse_args *a, void *workspace, size_t workspace_bytes,
                                       aflex_stream stream);

@@ -11,6 +11,10 @@ using aflex::hip_status;
 
 namespace {
 
+// Threads of a launch along one dimension, which have to stay below this.
+constexpr long long kMostThreads = 1ll << 32;
+constexpr long long kMostUnits = kMostThreads / 256;  // (sequence, kv head) pairs that get a work-group of 256 each
+
 // Sizes that every entry point takes.
 aflex_status check_pools(const char* who, int B, int Hkv, int D, int block_size, int max_blocks, int num_blocks) {
   REQUIRE(B >= 1 && Hkv >= 1 && D >= 1 && num_blocks >= 1 && max_blocks >= 1, AFLEX_ERR_INVALID_ARG,
@@ -52,10 +56,14 @@ aflex_status check_rope(const aflex_rope_args* a, bool packed) {
           "%s: rows of 2^30 elements or more", who);
   REQUIRE(packed || (long long)a->B * ((long long)a->Hq + a->Hkv) < (1ll << 30), AFLEX_ERR_UNSUPPORTED,
           "%s: B * (Hq + Hkv) must stay below 2^30", who);
+  REQUIRE(packed || ((long long)a->B * a->Hkv + (long long)a->B * a->Hq * a->D / 1024 + 4) * 64 < kMostThreads,
+          AFLEX_ERR_UNSUPPORTED, "%s: B * (Hkv + Hq * D / 1024) must stay below 2^26 - 4", who);
   if (packed) {
     REQUIRE(a->T >= 0 && a->max_seqlen >= 0, AFLEX_ERR_INVALID_ARG, "%s: T and max_seqlen must not be negative", who);
     REQUIRE(a->max_seqlen <= a->T, AFLEX_ERR_INVALID_ARG, "%s: max_seqlen %d exceeds T %d", who, a->max_seqlen, a->T);
     REQUIRE(a->B <= 65535, AFLEX_ERR_UNSUPPORTED, "%s: B %d above 65535", who, a->B);
+    REQUIRE(((a->max_seqlen + 15ll) / 16 + 1) * 256 < kMostThreads, AFLEX_ERR_UNSUPPORTED,
+            "%s: max_seqlen %d above 2^28 - 32", who, a->max_seqlen);
     REQUIRE(a->Hq <= 4096 && a->Hkv <= 4096, AFLEX_ERR_UNSUPPORTED, "%s: more than 4096 heads", who);
   }
   if ((s = check_stride(who, "q_stride", a->q_stride, (long long)a->Hq * a->D)) != AFLEX_OK) return s;
@@ -88,8 +96,9 @@ aflex_status check_select(const aflex_block_select_args* a) {
           AFLEX_ERR_INVALID_ARG,
           "%s: need sink_blocks >= 0, recent_blocks >= 1 and their sum <= top_blocks (got %d, %d, %d)", who,
           a->sink_blocks, a->recent_blocks, a->top_blocks);
-  REQUIRE((long long)a->B * a->Hkv < (1ll << 30) &&
-              (long long)a->B * a->Hkv * ((a->max_context_len + 15ll) / 16) < (1ll << 30) &&
+  // (the forms with larger work-groups have more than 1024 blocks, so fewer units)
+  REQUIRE((long long)a->B * a->Hkv < kMostUnits, AFLEX_ERR_UNSUPPORTED, "%s: B * Hkv must stay below 2^24", who);
+  REQUIRE((long long)a->B * a->Hkv * ((a->max_context_len + 15ll) / 16) < (1ll << 30) &&
               (long long)a->B * a->Hkv * a->top_blocks < (1ll << 30),
           AFLEX_ERR_UNSUPPORTED,
           "%s: B * Hkv times ceil(max_context_len / 16), and times top_blocks, must stay below 2^30", who);
@@ -107,6 +116,8 @@ aflex_status check_sparse(const aflex_attn_sparse_args* a, bool need_out) {
   REQUIRE(a->selected, AFLEX_ERR_INVALID_ARG, "attn_sparse: selected is NULL");
   REQUIRE(a->top_blocks >= 1, AFLEX_ERR_INVALID_ARG, "attn_sparse: top_blocks must be positive");
   REQUIRE(a->attn.split_tokens == 0, AFLEX_ERR_UNSUPPORTED, "attn_sparse: split_tokens must be 0");
+  REQUIRE((long long)a->attn.B * a->attn.Hkv < kMostUnits, AFLEX_ERR_UNSUPPORTED,
+          "attn_sparse: B * Hkv must stay below 2^24");
   REQUIRE((long long)a->attn.B * a->attn.Hkv * a->top_blocks < (1ll << 30), AFLEX_ERR_UNSUPPORTED,
           "attn_sparse: B * Hkv * top_blocks must stay below 2^30");
   REQUIRE(aligned4(a->selected), AFLEX_ERR_ALIGNMENT, "attn_sparse: selected must be 4-byte aligned");

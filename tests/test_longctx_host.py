@@ -368,3 +368,20 @@ def test_sizes_may_be_whole_numbers_of_other_types(lib):
     for bad in (np.float32(2.0), [3], b"4", torch.ones(2)):
         with pytest.raises(TypeError):
             _block_of(bad)
+
+
+def test_more_threads_than_a_launch_takes_are_refused(lib):
+    """2^32 threads along one dimension: refused here, not left to the runtime."""
+    n = ctypes.c_size_t()
+    assert lib.aflex_rope_append(ctypes.byref(_rope(B=1 << 25, Hq=2, Hkv=2, D=64)), None) == UNSUP
+    assert lib.aflex_rope_append(ctypes.byref(_rope(B=1 << 22, Hq=128, Hkv=1, D=128)), None) == UNSUP
+    assert lib.aflex_rope_write(ctypes.byref(_rope(T=1 << 29, max_seqlen=(1 << 28) - 31)), None) == UNSUP
+    few = dict(B=1 << 23, Hkv=2, Hq=2, max_blocks_per_seq=4, max_context_len=64)
+    a = _select(top_blocks=4, sink_blocks=1, recent_blocks=1, **few)
+    assert lib.aflex_block_select_workspace(ctypes.byref(a), ctypes.byref(n)) == UNSUP
+    a.B -= 1
+    assert lib.aflex_block_select_workspace(ctypes.byref(a), ctypes.byref(n)) == aflex.OK and n.value == 0
+    a = _sparse(top_blocks=4, **few)
+    assert lib.aflex_attn_sparse_decode_workspace(ctypes.byref(a), ctypes.byref(n)) == UNSUP
+    a.attn.B -= 1
+    assert lib.aflex_attn_sparse_decode_workspace(ctypes.byref(a), ctypes.byref(n)) == aflex.OK
