@@ -162,9 +162,9 @@ typedef struct aflex_attn_sparse_args {
 
 /* Supported: as aflex_attn_decode, and B * Hkv < 2^24, B * Hkv *           */
 /* top_blocks < 2^30. The same result on every call with the same inputs    */
-/* (bitwise). The softmax weights are rounded to bf16 for the product with  */
-/* the values and summed as rounded; scores, sums and the merge of split    */
-/* lists are fp32.                                                          */
+/* (bitwise). The softmax weights keep 16 bits (two bf16 values) in the     */
+/* product with the values and are summed as rounded; scores, sums and the  */
+/* merge of split lists are fp32.                                           */
 aflex_status aflex_attn_sparse_decode_workspace(const aflex_attn_sparse_args *a, size_t *bytes);
 aflex_status aflex_attn_sparse_decode(const aflex_attn_sparse_args *a, void *workspace, size_t workspace_bytes,
                                       aflex_stream stream);

@@ -644,3 +644,21 @@ def test_workspace_grown_while_another_stream_reads_it(gpu_lib, op):
         t.fill_(255)
     torch.cuda.synchronize()
     assert torch.equal(got, want)
+
+
+@pytest.mark.parametrize("heads", [(8, 2, 64), (64, 8, 128), (28, 4, 128)])
+@pytest.mark.parametrize("top", [7, 70])
+def test_attention_carries_one_rounding(gpu_lib, heads, top):
+    """Scores that are exact (one channel of the keys, its query 1): what is left is the output's rounding,
+    2^-8 |out|, the weights' as two bf16 values, 2^-16 each above and below the line, exponents of at most 2^-19,
+    and the sums: a wave adds at most 36 pairs of blocks, of 70, in steps of 32 products twice, so 64 roundings
+    of 2^-23 for each of the 9 pairs that it has, 2^-13.8. In all less than 2^-13 sum p|v|."""
+    a = synth.custom_attention(111, 6, *heads, [1, 150, 0, 700, 1111, 33], ctx_hi=1120)
+    a.k_cache[..., 1:] = 0
+    a.k_cache[..., 0] = (a.k_cache[..., 0].float() * 2).clamp(-4, 4).bfloat16()
+    a.q[..., 0] = 1
+    sel = _lists(112, a, top)
+    got = aflex.attn_sparse_decode(a.to(DEV), sel.to(DEV), scale=1.0).cpu().double()
+    ref, mag = lc.attention_sparse(a.q, a.k_cache, a.v_cache, a.block_table, a.context_lens, sel, 1.0)
+    bad = (got - ref).abs() > 2.0 ** -8 * ref.abs() + 2.0 ** -13 * mag
+    assert not bool(bad.any()), f"{int(bad.sum())} of {bad.numel()} values"
