@@ -662,3 +662,49 @@ def test_attention_carries_one_rounding(gpu_lib, heads, top):
     ref, mag = lc.attention_sparse(a.q, a.k_cache, a.v_cache, a.block_table, a.context_lens, sel, 1.0)
     bad = (got - ref).abs() > 2.0 ** -8 * ref.abs() + 2.0 ** -13 * mag
     assert not bool(bad.any()), f"{int(bad.sum())} of {bad.numel()} values"
+
+
+@pytest.mark.parametrize("B,heads,blocks,top", [(128, (8, 8, 64), (110, 130), 100), (128, (32, 8, 128), (66, 90), 128),
+                                                (64, (8, 8, 64), (140, 200), 128), (64, (32, 8, 128), (140, 200), 128),
+                                                (3, (4, 2, 128), (400, 600), 300), (40, (8, 8, 64), (60, 100), 90)])
+def test_attention_of_long_lists_shows_every_block(gpu_lib, B, heads, blocks, top):
+    """Keys of zero, so every weight is 1, and values of whole numbers in one channel per block: a result is
+    sum / count, rounded to bf16 once, and shows each block that is lost, doubled or strange. Lists longer than
+    the 64 entries that a wave holds at a time, a work-group per list and split ones, with entries around the
+    64th that contribute nothing."""
+    Hq, Hkv, D = heads
+    g = torch.Generator().manual_seed(120 + B)
+    n = blocks[1]
+    nblk = torch.randint(blocks[0], n + 1, (B,), generator=g)
+    ctx = (nblk * 16 - torch.randint(0, 16, (B,), generator=g)).int()
+    table = torch.stack([torch.randperm(n, generator=g) for _ in range(B)]).int()
+    head = torch.arange(Hkv)
+    v = torch.zeros(n, Hkv, D, 16)
+    for blk in range(n):
+        v[blk, head, (blk + head) % D] = 1 + blk // D
+    sel = torch.full((B, Hkv, top), -1, dtype=torch.int32)
+    for b in range(B):
+        for h in range(Hkv):
+            row = torch.randperm(int(nblk[b]), generator=g)[:top].sort().values.int()
+            row[-1] = nblk[b] - 1
+            kind = (b + h) % 4
+            if kind == 1 and len(row) > 63:
+                row[63] = -1
+            elif kind == 2:
+                row[64:] = torch.cat([row[63:64], row[65:]]) if len(row) > 64 else row[64:]
+            elif kind == 3 and len(row) > 66:
+                row[65] = nblk[b] + 5  # (the next one is not greater)
+            sel[b, h, :len(row)] = row
+    a = synth.AttnInputs(q=_bf(121, B, Hq, D), k_cache=torch.zeros(n, Hkv, 16, D, dtype=torch.bfloat16),
+                         v_cache=v.bfloat16(), block_table=table, context_lens=ctx, B=B, Hq=Hq, Hkv=Hkv, D=D,
+                         block_size=16, max_blocks=n, num_blocks=n, max_context_len=16 * n)
+    got = aflex.attn_sparse_decode(a.to(DEV), sel.to(DEV)).cpu().double()
+    prev = torch.cat([torch.full((B, Hkv, 1), -1, dtype=torch.int32), sel[..., :-1]], -1)
+    valid = (sel > prev) & (sel >= 0) & (sel < nblk[:, None, None])
+    j = sel.clamp(0, n - 1).long()
+    tokens = (ctx[:, None, None] - 16 * j).clamp(max=16).double() * valid
+    blk = torch.gather(table.long()[:, None].expand(B, Hkv, n), 2, j)
+    ref = torch.zeros(B, Hkv, D, dtype=torch.float64)
+    ref.scatter_add_(2, (blk + head[:, None]) % D, tokens * (1 + blk // D))
+    ref = (ref / tokens.sum(-1, keepdim=True)).repeat_interleave(Hq // Hkv, 1)
+    assert bool(((got - ref).abs() <= 2.0 ** -8 * ref).all())
