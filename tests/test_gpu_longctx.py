@@ -10,6 +10,8 @@ carry fp32 sums of at most 128 products, of which exp2 makes less than 2^-10 of
 the weights at these magnitudes (|score| < 64: 64 * 128 * 2^-24 = 2^-11 before
 the exponential). Copies, summaries and choices are compared for equality.
 """
+import threading
+
 import numpy as np
 import pytest
 import torch
@@ -708,3 +710,68 @@ def test_attention_of_long_lists_shows_every_block(gpu_lib, B, heads, blocks, to
     ref.scatter_add_(2, (blk + head[:, None]) % D, tokens * (1 + blk // D))
     ref = (ref / tokens.sum(-1, keepdim=True)).repeat_interleave(Hq // Hkv, 1)
     assert bool(((got - ref).abs() <= 2.0 ** -8 * ref).all())
+
+
+@pytest.mark.parametrize("packed", [False, True])
+@pytest.mark.parametrize("heads,R,inter", [((16, 4, 128), 128, True), ((16, 4, 128), 64, False), ((28, 4, 128), 96, True),
+                                           ((8, 2, 64), 64, True), ((8, 2, 64), 16, False), ((5, 5, 64), 48, True)])
+def test_rotation_bits_of_both_pairings_and_of_a_part(gpu_lib, packed, heads, R, inter):
+    """As test_append_rotates_like_fp32_operations, for queries and cached keys."""
+    Hq, Hkv, D = heads
+    ctx = [40, 1, 7, 99, 16, 64]
+    a = synth.custom_attention(131, 6, *heads, ctx, ctx_hi=112).to(DEV)
+    (q, k, _), dev = _tokens(132, 6, heads, True)
+    rope = aflex.rope_table(112, R, 1000.0)
+    if packed:
+        cu = torch.arange(7, dtype=torch.int32, device=DEV)
+        out = aflex.rope_write(a, *dev, cu, rope.to(DEV), interleaved=inter)
+    else:
+        out = aflex.rope_append(a, *dev, rope.to(DEV), interleaved=inter)
+    pos = torch.tensor(ctx) - 1
+    i = torch.arange(R // 2)
+    ia, ib = (2 * i, 2 * i + 1) if inter else (i, i + R // 2)
+    c, s = rope[pos][:, None, :R // 2], rope[pos][:, None, R // 2:]
+
+    def turned(x):
+        y = x.clone()
+        f, g = x[..., ia].float(), x[..., ib].float()
+        y[..., ia], y[..., ib] = (f * c - g * s).bfloat16(), (g * c + f * s).bfloat16()
+        return y
+
+    assert torch.equal(out.cpu(), turned(q))
+    kc = a.k_cache.cpu()
+    got = torch.stack([kc[a.block_table[b, p // 16], :, p % 16] for b, p in enumerate(pos.tolist())])
+    assert torch.equal(got, turned(k))
+
+
+@pytest.mark.parametrize("n,top", [(4097, 600), (4200, 513), (4200, 1000), (8190, 1024)])
+def test_block_select_of_more_blocks_than_lanes_hold_keys(gpu_lib, n, top):
+    """Just above the short lists only some of the lanes have keys, fewer than the blocks that are wanted."""
+    _choice(57, [16 * n - 3], (4, 1, 64), top, 1, 2)
+
+
+def test_two_host_threads_on_one_stream(gpu_lib):
+    """Each thread's choice and attention are those that it gets alone."""
+    work = []
+    for seed, ctx in ((141, [17000, 300]), (142, [16500, 2000])):
+        a = synth.custom_attention(seed, 2, 8, 2, 64, ctx, ctx_hi=17000).to(DEV)
+        s = aflex.block_summary(a)
+        sel = aflex.block_select(a, a.q, s, 40)
+        work.append((a, s, sel, aflex.attn_sparse_decode(a, sel)))
+    torch.cuda.synchronize()
+    wrong = []
+
+    def run(a, s, sel, out):
+        for _ in range(200):
+            x = aflex.block_select(a, a.q, s, 40)
+            y = aflex.attn_sparse_decode(a, sel)
+            if not (torch.equal(x, sel) and torch.equal(y, out)):
+                wrong.append(1)
+
+    threads = [threading.Thread(target=run, args=w) for w in work]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join(60)
+        assert not t.is_alive()
+    assert not wrong

@@ -385,3 +385,17 @@ def test_more_threads_than_a_launch_takes_are_refused(lib):
     assert lib.aflex_attn_sparse_decode_workspace(ctypes.byref(a), ctypes.byref(n)) == UNSUP
     a.attn.B -= 1
     assert lib.aflex_attn_sparse_decode_workspace(ctypes.byref(a), ctypes.byref(n)) == aflex.OK
+
+
+def test_block_select_workspace_of_two_launches(lib):
+    """Above 1024 blocks the scores' keys are in the workspace, rows of a multiple of 4."""
+    n = ctypes.c_size_t()
+    a = _select(max_blocks_per_seq=1030, max_context_len=1025 * 16 + 1)
+    assert lib.aflex_block_select_workspace(ctypes.byref(a), ctypes.byref(n)) == aflex.OK
+    need = n.value
+    assert need >= 2 * 2 * 1028 * 4
+    assert lib.aflex_block_select(ctypes.byref(a), ctypes.c_void_p(FAKE), need - 1, None) == WS
+    assert lib.aflex_block_select(ctypes.byref(a), None, need, None) == WS
+    assert lib.aflex_block_select(ctypes.byref(a), ctypes.c_void_p(FAKE + 128), need, None) == ALIGN
+    a = _select(max_blocks_per_seq=1030, max_context_len=1024 * 16)
+    assert lib.aflex_block_select_workspace(ctypes.byref(a), ctypes.byref(n)) == aflex.OK and n.value == 0
