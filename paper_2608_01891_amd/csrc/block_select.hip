@@ -269,7 +269,13 @@ __device__ __forceinline__ int wave_scan(int v) {
 }
 
 // Wave slots along the kv heads in a work-group of the scores (the others take
-// further rounds of blocks).
+// further rounds of blocks): the next power of two, though with 3, 5, 6 or 7
+// heads some of the waves then have nothing to do. With the power below, so that
+// waves take two heads one after the other, or with one slot and every wave its
+// own rounds (us of the scores, D = 128, this / below / one slot): 3 heads, 64
+// sequences of median 20000 tokens 15.7 / 15.5 / 16.3, one of 400000 8.6 / 11.3 /
+// 14.8; 5 heads 18.1 / 21.4 / 21.9 and 10.9 / 11.8 / 20.9; 7 heads 21.2 / 24.7 /
+// 28.1 and 11.5 / 12.3 / 26.5.
 __host__ __device__ constexpr int head_slots(int Hkv) { return Hkv > 4 ? 8 : Hkv > 2 ? 4 : Hkv; }
 
 // Scores of all units whose blocks are not all taken, as rounds of 64 blocks of
@@ -497,9 +503,12 @@ __global__ __launch_bounds__(kChooseThreads, 6) void block_choose_kernel(aflex_b
 // stretch of the keys, 256 at a time, four per lane. The N-th largest of the
 // lanes' own maxima, cut to 22 bits, is a bound that at least N keys reach and
 // few others do; those go to a list in LDS and the choice is made there. Where
-// they are more than the list holds (equal scores, or N above the threads), the
-// bounds are found digit by digit over all keys. R: rounds of keys that a lane
-// keeps in registers, or 0: they are read again for every pass.
+// they are more than the list holds (equal scores, or N above the lanes that have
+// keys: all 1024 from 8192 blocks on, little more than half of them just above
+// 4096), the bounds are found digit by digit over all keys. R: rounds of keys that
+// a lane keeps in registers, or 0: they are read again for every pass (us, kept /
+// read again, 8 units of 5000 blocks 11.4 / 11.4, 16400 12.0 / 13.9, 25000 13.6 /
+// 16.8, 32500 14.0 / 18.1; 512 of median 6250 21.4 / 24.8).
 template <int R>
 __global__ __launch_bounds__(kPickThreads) void block_pick_kernel(aflex_block_select_args a, int stride,
                                                                   const uint32_t* keys, bool long_only) {
@@ -619,7 +628,7 @@ __global__ __launch_bounds__(kPickThreads) void block_pick_kernel(aflex_block_se
 }
 
 // Scores and choice of a unit in one work-group, the keys in LDS (the bins of
-// the choice where the rows of the scores were: 37 KiB, four work-groups per CU).
+// the choice where the rows of the scores were: 36 KiB, four work-groups per CU).
 template <int D>
 __global__ __launch_bounds__(kSelectThreads, 4) void block_select_kernel(aflex_block_select_args a) {
   constexpr int NT = kSelectThreads, NW = NT / 64;
@@ -691,12 +700,14 @@ hipError_t launch_block_select(const aflex_block_select_args& a, void* ws, hipSt
   }
   {
     ProfScope ps("block_pick", stream);
+    // rounds of keys in registers, 32 per lane: bounds of up to 32768 blocks (524288
+    // tokens); a kernel for longer ones cannot know that a unit is shorter
     constexpr int kRounds = 8;
     // Where units may be long but are many, the short ones are chosen by the
     // smaller kernel, three work-groups of which a CU holds, and a launch of its
-    // own (under a bound of 131072 tokens, one launch / two: 2048 units of median
-    // 3000 tokens 44.1 / 32.5 us, 1024 of 5000 30.1 / 25.2, 512 of 20000 32.4 / 32.0,
-    // 256 of 20000 20.2 / 21.9).
+    // own (under a bound of 131072 tokens, lengths lognormal with sigma 0.5, the whole
+    // choice in one launch / two: 2048 units of median 3000 tokens 42.7 / 32.2 us, 1024
+    // of 5000 30.3 / 25.6, 512 of 20000 34.8 / 38.6, 256 of 20000 20.7 / 22.2).
     const bool split = stride > kListed && units >= kSplitUnits;
     if (stride <= kListed || split) block_choose_kernel<<<units, kChooseThreads, 0, stream>>>(a, stride, keys);
     if (stride > kRounds * 4 * kPickThreads)

@@ -315,10 +315,11 @@ __global__ __launch_bounds__(256) void rope_write_kernel(aflex_rope_args a, int 
 // Tiles in a row per wave (375 MB of keys and summaries / 16 short contexts: one
 // tile 77.3 / 5.5 us, two 76.3 / 6.3, four 78.7 / 7.6, eight 82.2 / 11.9).
 constexpr int kTilesPerWave = 2;
-// Work-groups in all, at least 16 per sequence; they step on over a longer context.
-// One for every tile of the bound / at most this many: 64 sequences of median 1500
-// tokens under a bound of 131072, 114.9 / 46.6 us, 256 of 400 under 32768, 116.5 /
-// 51.7; 8 of 20000 under 65536, 76.2 / 76.5; 16 of 300 under 1024, 6.3 / 6.4.
+// Work-groups in all, but 16 per sequence where that is more; they step on over a
+// longer context. Enough for every tile of the bound / at most this many (lengths
+// lognormal with sigma 0.5): 64 sequences of median 1500 tokens under a bound of
+// 131072, 114.2 / 49.8 us, 256 of 400 under 32768, 116.6 / 56.6; 8 of 20000 under
+// 65536, 77.1 / 77.0; 16 of 300 under 1024, 6.6 / 6.6.
 constexpr int kSummaryWgs = 32768;
 
 template <int D>
@@ -422,8 +423,8 @@ hipError_t launch_rope_write(const aflex_rope_args& in, hipStream_t stream) {
 hipError_t launch_block_summary(const aflex_block_summary_args& a, hipStream_t stream) {
   const long long tiles = (long long)(a.max_context_len / 16) * a.Hkv;
   if (tiles == 0) return hipSuccess;
-  // Work-groups for the longest context, but no more than kSummaryWgs in all: under
-  // a loose bound most would find nothing to do.
+  // Work-groups for the longest context, but no more than kSummaryWgs in all (or 16
+  // per sequence): under a loose bound most would find nothing to do.
   const long long need = (tiles + 4 * kTilesPerWave - 1) / (4 * kTilesPerWave);
   const long long most = kSummaryWgs / a.B > 16 ? kSummaryWgs / a.B : 16;
   const dim3 grid((unsigned)(need < most ? need : most), a.B);
