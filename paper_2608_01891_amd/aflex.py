@@ -287,12 +287,10 @@ class Workspace:
             self.home = torch.cuda.current_stream(device).cuda_stream
         return self.buf
 
-    def used_on(self, handle, stream):
-        """buf is used on the stream of that handle (`stream`, or the current one): a
-        later growth, which frees it, must not hand the memory out while that stream
-        still reads it."""
-        if handle != self.home:
-            self.buf.record_stream(torch.cuda.current_stream(self.buf.device) if stream is None else stream)
+    def used_on(self, stream):
+        """buf is used on `stream` (None: the current one), not its home: a later growth,
+        which frees it, must not hand the memory out while that stream still reads it."""
+        self.buf.record_stream(torch.cuda.current_stream(self.buf.device) if stream is None else stream)
 
 
 _default_ws = {}
@@ -313,7 +311,8 @@ def _ws(nbytes, device, ws, streams=()):
     on the current stream; its use on any other stream is recorded."""
     buf = ws.get(nbytes, device)
     for s in streams:
-        ws.used_on(_stream(s), s)
+        if _stream(s) != ws.home:
+            ws.used_on(s)
     return buf.data_ptr(), buf.numel()
 
 
@@ -327,13 +326,17 @@ def _run(name, args, key, device, ws, stream):
     Tensors that are not on a GPU are refused before any library call (a kernel would
     read and write the host's addresses): no workspace is ever on another device, so
     theirs is never at hand."""
-    ws = _own(key, ws)
+    if ws is None:
+        ws = _own(key, ws)
     ref = ctypes.byref(args)
     fn = getattr(_lib, name)
+    handle = _stream(stream)
     with ws.lock:
-        if ws.fits(0, device):
-            p, sz = _ws(0, device, ws, (stream,))
-            status = fn(ref, p, sz, _stream(stream))
+        buf = ws.buf
+        if buf is not None and buf.device == device:
+            if handle != ws.home:
+                ws.used_on(stream)
+            status = fn(ref, buf.data_ptr(), buf.numel(), handle)
             if status != ERR_WORKSPACE:
                 _check(status)
                 return
@@ -341,7 +344,7 @@ def _run(name, args, key, device, ws, stream):
         n = ctypes.c_size_t()
         _check(getattr(_lib, name + "_workspace")(ref, ctypes.byref(n)))
         p, sz = _ws(n.value, device, ws, (stream,))
-        _check(fn(ref, p, sz, _stream(stream)))
+        _check(fn(ref, p, sz, handle))
 
 
 # --------------------------------------------------------------------------
@@ -667,7 +670,8 @@ def _run_own_ws(name, dev, ws, stream, *items):
     with ws.lock:
         buf = ws.buf
         if buf is not None and buf.get_device() == dev:
-            ws.used_on(handle, stream)  # (a caller's may be used on several)
+            if handle != ws.home:  # (a caller's may be used on several)
+                ws.used_on(stream)
             status = _call(_entry[name], dev, handle, buf.data_ptr(), buf.numel(), *items)
             if status != ERR_WORKSPACE:
                 return _check(status)
