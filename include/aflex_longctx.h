@@ -34,9 +34,10 @@ extern "C" {
 /* c = rope[p][i], s = rope[p][rotary_dim / 2 + i] at position p:             */
 /*   a' = a c - b s,   b' = b c + a s    (fp32, each operation rounded; bf16) */
 /* channels from rotary_dim on are copied. q rows are rotated into q_out, k   */
-/* rows into the K pool, v rows are copied into the V pool, at the slots of   */
-/* aflex_kv_append / aflex_kv_write: token i of sequence b's n_b new tokens   */
-/* sits at j = context_lens[b] - n_b + i. p = j unless positions is given.    */
+/* rows into the K pool (there alone), v rows are copied into the V pool, at  */
+/* the slots of aflex_kv_append / aflex_kv_write: token i of sequence b's n_b */
+/* new tokens sits at j = context_lens[b] - n_b + i. p = j unless positions   */
+/* is given.                                                                  */
 /*                                                                            */
 /* Summaries (block_keys / block_exp, both or neither): whenever a write      */
 /* fills a block's last slot, the block's summary is made from its 16 cached  */

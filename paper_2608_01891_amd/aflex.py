@@ -269,7 +269,8 @@ class Workspace:
 
     A call may be several launches that communicate through the scratch. `lock`
     is held while one is made, so that a second host thread's call on the same
-    stream comes behind all of them, not between two."""
+    stream comes behind all of them, not between two. A workspace that a captured
+    graph uses must not grow while the graph lives."""
 
     def __init__(self, device=None):
         self.device = device
@@ -714,7 +715,8 @@ def rope_append(a, q, k_new, v_new, rope, interleaved: bool = False, positions=N
     """Rotate each sequence's new query and key, and append key and value to a's paged pools in place
     (position ctx-1, or row ``positions[b]`` of ``rope``; rope=None: no rotation). q [B, Hq, D], k_new and
     v_new [B, Hkv, D] may be slices of one projection's output. With ``summary`` (BlockSummary) the blocks
-    that get full are summarised. Returns the rotated queries [B, Hq, D]."""
+    that get full are summarised. Returns the rotated queries [B, Hq, D]; the rows of sequences that are
+    left alone (no context, one above the capacity, a position outside the table) are not written."""
     return _rope(q, "aflex_rope_append", a, q, k_new, v_new, rope, None, 0, interleaved, positions,
                  summary, q_out, stream)
 

@@ -854,8 +854,8 @@ hipError_t launch_attn_decode(const aflex_attn_args& a, void* ws, hipStream_t st
 }
 
 // Attention over chosen blocks: the same work-groups over lists of at most
-// top_blocks blocks per unit (512 units of 128 blocks, 537 MB: 92 us, 5.85 TB/s,
-// and 4.6 for the merge). A list's entries name blocks of the sequence, whose
+// top_blocks blocks per unit (512 units of 128 blocks, 537 MB: 96 us a call, 5.6 TB/s,
+// the merge's 4.7 among them). A list's entries name blocks of the sequence, whose
 // pool ids are one more dependent load, made a chunk ahead like the ids alone.
 // The softmax weights keep 16 bits in the matrix product, as two bf16 values (the
 // dense form's keep 8), at no cost that shows beside the loads (the same before /

@@ -11,7 +11,7 @@
 // (four times the tag lookups of whole rows), chunks of sequences dealt to XCDs
 // by their number (the first ones, which all sequences have, on two of 8), and
 // grids over the longest context (idle work-groups; stretches of equal length
-// instead): 64 sequences of median 20000 tokens, 95 MB, 63 -> 21 us. Rows of 1 KB
+// instead): 64 sequences of median 20000 tokens, 95 MB, 63 -> 24 us. Rows of 1 KB
 // (8 heads x 128) gathered at random reach 5.0-5.3 TB/s alone: 18.4 us.
 //
 // The scores become 32-bit keys whose unsigned order is theirs, forced blocks
