@@ -20,6 +20,7 @@ _PKG = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_PKG, "libaflex.so")
 HEADER = os.path.join(os.path.dirname(_PKG), "include", "aflex.h")
 LONGCTX_HEADER = os.path.join(os.path.dirname(_PKG), "include", "aflex_longctx.h")
+DRAFT_HEADER = os.path.join(os.path.dirname(_PKG), "include", "aflex_draft.h")
 
 OK, ERR_INVALID_ARG, ERR_UNSUPPORTED, ERR_ALIGNMENT, ERR_WORKSPACE, ERR_HIP = range(6)
 
@@ -103,6 +104,36 @@ class AttnSparseArgs(ctypes.Structure):
     _fields_ = [("attn", AttnArgs), ("selected", _p), ("top_blocks", _i)]
 
 
+class RopeF8Args(ctypes.Structure):
+    _fields_ = [("q", _p), ("k_new", _p), ("v_new", _p), ("rope", _p), ("positions", _p), ("cu_seqlens", _p),
+                ("q_out", _p), ("k_cache", _p), ("v_cache", _p), ("kv_exp", _p), ("block_table", _p),
+                ("context_lens", _p),
+                ("B", _i), ("T", _i), ("Hq", _i), ("Hkv", _i), ("D", _i), ("rotary_dim", _i),
+                ("interleaved", _i), ("rope_len", _i), ("max_seqlen", _i), ("block_size", _i),
+                ("max_blocks_per_seq", _i), ("num_blocks", _i), ("q_stride", _i), ("k_stride", _i), ("v_stride", _i)]
+
+
+class AttnF8Args(ctypes.Structure):
+    _fields_ = [("q", _p), ("k_cache", _p), ("v_cache", _p), ("kv_exp", _p), ("block_table", _p),
+                ("context_lens", _p), ("out", _p),
+                ("B", _i), ("Hq", _i), ("Hkv", _i), ("D", _i), ("block_size", _i), ("max_blocks_per_seq", _i),
+                ("num_blocks", _i), ("max_context_len", _i), ("scale", ctypes.c_float)]
+
+
+class AttnTreeArgs(ctypes.Structure):
+    _fields_ = [("q", _p), ("k_cache", _p), ("v_cache", _p), ("kv_exp", _p), ("block_table", _p),
+                ("context_lens", _p), ("cu_seqlens", _p), ("masks", _p), ("out", _p),
+                ("B", _i), ("T", _i), ("Hq", _i), ("Hkv", _i), ("D", _i), ("max_drafts", _i), ("block_size", _i),
+                ("max_blocks_per_seq", _i), ("num_blocks", _i), ("max_context_len", _i), ("scale", ctypes.c_float)]
+
+
+class CacheAcceptArgs(ctypes.Structure):
+    _fields_ = [("k_cache", _p), ("v_cache", _p), ("kv_exp", _p), ("block_table", _p), ("context_lens", _p),
+                ("cu_seqlens", _p), ("accepted", _p), ("accepted_counts", _p), ("context_out", _p),
+                ("B", _i), ("Hkv", _i), ("D", _i), ("max_accepted", _i), ("block_size", _i),
+                ("max_blocks_per_seq", _i), ("num_blocks", _i)]
+
+
 class AflexError(RuntimeError):
     def __init__(self, status: int, message: str):
         super().__init__(f"aflex status {status}: {message}")
@@ -166,6 +197,13 @@ def load():
         "aflex_block_select": [ctypes.POINTER(BlockSelectArgs), _p, ctypes.c_size_t, _p],
         "aflex_attn_sparse_decode_workspace": [ctypes.POINTER(AttnSparseArgs), _SZ],
         "aflex_attn_sparse_decode": [ctypes.POINTER(AttnSparseArgs), _p, ctypes.c_size_t, _p],
+        "aflex_rope_append_f8": [ctypes.POINTER(RopeF8Args), _p],
+        "aflex_rope_write_f8": [ctypes.POINTER(RopeF8Args), _p],
+        "aflex_attn_decode_f8_workspace": [ctypes.POINTER(AttnF8Args), _SZ],
+        "aflex_attn_decode_f8": [ctypes.POINTER(AttnF8Args), _p, ctypes.c_size_t, _p],
+        "aflex_attn_tree_workspace": [ctypes.POINTER(AttnTreeArgs), _SZ],
+        "aflex_attn_tree": [ctypes.POINTER(AttnTreeArgs), _p, ctypes.c_size_t, _p],
+        "aflex_cache_accept": [ctypes.POINTER(CacheAcceptArgs), _p],
     }
     for name, args in sig.items():
         fn = getattr(lib, name)
@@ -593,8 +631,9 @@ def _af_layer_step(a, w, layer, k, mb_sizes, L, y, stream_a, stream_f, ws, join)
 
 
 # --------------------------------------------------------------------------
-# Long-context operators (include/aflex_longctx.h). These check what the C
-# interface cannot see (types, sizes, devices, strides), run on the device of
+# Long-context operators (include/aflex_longctx.h), the 8-bit cache and drafted
+# tokens (include/aflex_draft.h). These check what the C interface
+# cannot see (types, sizes, devices, strides), run on the device of
 # their tensors, and keep a default workspace per stream; outputs that they
 # allocate belong to the stream they run on. Checks, argument block and call are
 # one native call (csrc/tensor_args.cpp): the items behind _call's first five
@@ -622,7 +661,7 @@ def rope_table(positions: int, rotary_dim: int, base: float = 10000.0, device="c
     return torch.cat([ang.cos(), ang.sin()], 1).float().to(device)
 
 
-_BF16, _F32, _I32, _I8, _ROWS = range(5)  # what the items of a call are
+_BF16, _F32, _I32, _I8, _ROWS, _I64, _F8 = range(7)  # what the items of a call are
 
 
 def _on_device(f):
@@ -796,3 +835,161 @@ def attn_sparse_decode(a, selected, q=None, out=None, scale: float = 0.0, stream
     """Decode attention of q (default a.q) [B, Hq, D] over the blocks that selected [B, Hkv, top_blocks] lists."""
     q = a.q if q is None else q
     return _attn_sparse(q, a, selected, q, out, scale, stream, ws)
+
+
+# --------------------------------------------------------------------------
+# The 8-bit cache and drafted tokens (include/aflex_draft.h).
+class F8Cache:
+    """An 8-bit paged cache: ``k_cache`` float8_e4m3fn [num_blocks, Hkv, 16, D], ``v_cache`` [num_blocks, Hkv, D, 16]
+    and ``kv_exp`` int8 [num_blocks, Hkv, 2, 16] (the keys' exponents, the values'), zeroed, with the block table,
+    context lengths and sizes of ``a``, whose attributes it takes over."""
+
+    def __init__(self, a):
+        d, n = a.block_table.device, a.num_blocks
+        self.B, self.Hq, self.Hkv, self.D, self.block_size = a.B, a.Hq, a.Hkv, a.D, a.block_size
+        self.max_blocks, self.num_blocks, self.max_context_len = a.max_blocks, n, a.max_context_len
+        self.block_table, self.context_lens = a.block_table, a.context_lens
+
+        def codes(*shape):
+            return torch.zeros(n, a.Hkv, *shape, dtype=torch.uint8, device=d).view(torch.float8_e4m3fn)
+
+        self.k_cache, self.v_cache = codes(16, a.D), codes(a.D, 16)
+        self.kv_exp = torch.zeros(n, a.Hkv, 2, 16, dtype=torch.int8, device=d)
+
+
+@_on_device
+def _rope_f8(dev, name, a, q, k_new, v_new, rope, cu_seqlens, max_seqlen, interleaved, positions, q_out, stream):
+    B, T, Hq, Hkv, D, blocks = a.B, q.shape[0], a.Hq, a.Hkv, a.D, a.num_blocks
+    if cu_seqlens is None and T != B:
+        raise ValueError(f"q: expected one row for each of {B} sequences, but got {T}")
+    rows, rot = (0, 0) if rope is None else rope.shape
+    if q_out is None:
+        q_out = _empty(stream, dev, T, Hq, D)
+    if T == 0:  # (empty tensors have no address)
+        return q_out
+    tiles = blocks * Hkv
+    _check(_call(_entry[name], dev, _stream(stream), None, 0,
+                 "q", q, _ROWS, T, Hq, D, "k_new", k_new, _ROWS, T, Hkv, D, "v_new", v_new, _ROWS, T, Hkv, D,
+                 "rope", rope, _F32, rows * rot, "positions", positions, _I32, T,
+                 "cu_seqlens", cu_seqlens, _I32, B + 1, "q_out", q_out, _BF16, T * Hq * D,
+                 "k_cache", a.k_cache, _F8, tiles * 16 * D, "v_cache", a.v_cache, _F8, tiles * 16 * D,
+                 "kv_exp", a.kv_exp, _I8, tiles * 32,
+                 "block_table", a.block_table, _I32, B * a.max_blocks, "context_lens", a.context_lens, _I32, B,
+                 B, T, Hq, Hkv, D, rot, int(interleaved), rows, max_seqlen, a.block_size, a.max_blocks, blocks,
+                 None, None, None))  # the strides of q, k_new, v_new
+    return q_out
+
+
+def rope_append_f8(a, q, k_new, v_new, rope, interleaved: bool = False, positions=None, q_out=None, stream=None):
+    """rope_append into an 8-bit cache (F8Cache): the rotated key and the value of each sequence's new token as e4m3
+    codes with a power of two each. Returns the rotated queries in bf16."""
+    return _rope_f8(q, "aflex_rope_append_f8", a, q, k_new, v_new, rope, None, 0, interleaved, positions, q_out, stream)
+
+
+def rope_write_f8(a, q, k_new, v_new, cu_seqlens, rope, max_seqlen=None, interleaved: bool = False, positions=None,
+                  q_out=None, stream=None):
+    """rope_append_f8 for packed new tokens: rows cu[b] .. cu[b+1]-1 are the newest of sequence b's context (for
+    drafts ``positions`` says where each stands). ``max_seqlen`` bounds their number per sequence (None: read from
+    cu_seqlens, which waits for the device)."""
+    if max_seqlen is None:
+        _need_gpu(q.device)
+        max_seqlen = _longest(cu_seqlens)
+    return _rope_f8(q, "aflex_rope_write_f8", a, q, k_new, v_new, rope, cu_seqlens, max_seqlen, interleaved, positions,
+                    q_out, stream)
+
+
+def _longest(cu_seqlens):
+    c = cu_seqlens.cpu()
+    return int((c[1:] - c[:-1]).max()) if c.numel() > 1 else 0
+
+
+@_on_device
+def _attn_decode_f8(dev, a, q, out, scale, stream, ws):
+    B, Hq, Hkv, D = a.B, a.Hq, a.Hkv, a.D
+    if out is None:
+        out = _empty(stream, dev, B, Hq, D)
+    tiles = a.num_blocks * Hkv
+    _run_own_ws("aflex_attn_decode_f8", dev, ws, stream,
+                "q", q, _BF16, B * Hq * D, "k_cache", a.k_cache, _F8, tiles * 16 * D,
+                "v_cache", a.v_cache, _F8, tiles * 16 * D, "kv_exp", a.kv_exp, _I8, tiles * 32,
+                "block_table", a.block_table, _I32, B * a.max_blocks, "context_lens", a.context_lens, _I32, B,
+                "out", out, _BF16, B * Hq * D,
+                B, Hq, Hkv, D, a.block_size, a.max_blocks, a.num_blocks, a.max_context_len, float(scale))
+    return out
+
+
+def attn_decode_f8(a, q, out=None, scale: float = 0.0, stream=None, ws=None):
+    """Decode attention of q [B, Hq, D] over an 8-bit cache (F8Cache)."""
+    return _attn_decode_f8(q, a, q, out, scale, stream, ws)
+
+
+@_on_device
+def _attn_tree(dev, a, q, cu_seqlens, masks, max_drafts, out, scale, stream, ws):
+    B, T, Hq, Hkv, D = a.B, q.shape[0], a.Hq, a.Hkv, a.D
+    if out is None:
+        out = _empty(stream, dev, T, Hq, D)
+    if T == 0:
+        return out
+    tiles, exp = a.num_blocks * Hkv, getattr(a, "kv_exp", None)
+    kind = _BF16 if exp is None else _F8
+    _run_own_ws("aflex_attn_tree", dev, ws, stream,
+                "q", q, _BF16, T * Hq * D, "k_cache", a.k_cache, kind, tiles * 16 * D,
+                "v_cache", a.v_cache, kind, tiles * 16 * D, "kv_exp", exp, _I8, tiles * 32,
+                "block_table", a.block_table, _I32, B * a.max_blocks, "context_lens", a.context_lens, _I32, B,
+                "cu_seqlens", cu_seqlens, _I32, B + 1, "masks", masks, _I64, T, "out", out, _BF16, T * Hq * D,
+                B, T, Hq, Hkv, D, max_drafts, a.block_size, a.max_blocks, a.num_blocks, a.max_context_len,
+                float(scale))
+    return out
+
+
+def attn_tree(a, q, cu_seqlens, masks=None, max_drafts=None, out=None, scale: float = 0.0, stream=None, ws=None):
+    """Attention of drafted tokens over a cache that holds them: rows cu[b] .. cu[b+1]-1 of q [T, Hq, D] are the
+    newest tokens of sequence b's context, up to 64. Each sees the context before them and, of them, those whose
+    bits are set in its entry of ``masks`` (int64 [T], bit j: draft j of the sequence; see tree_masks; None: itself
+    and the earlier ones). ``a`` holds an 8-bit cache (kv_exp) or a bf16 one. ``max_drafts`` bounds their number per
+    sequence (None: read from cu_seqlens, which waits for the device)."""
+    if max_drafts is None:
+        _need_gpu(q.device)
+        max_drafts = _longest(cu_seqlens)
+    return _attn_tree(q, a, q, cu_seqlens, masks, max_drafts, out, scale, stream, ws)
+
+
+def tree_masks(parents, device="cpu"):
+    """Masks for attn_tree from the parents of each sequence's drafts: ``parents[b][i]`` is the draft before draft i
+    (an earlier index, or -1 for the context). A draft sees its ancestors and itself. int64, sequences behind each
+    other."""
+    rows = []
+    for tree in parents:
+        if len(tree) > 64:
+            raise ValueError(f"at most 64 drafts per sequence, but got {len(tree)}")
+        seen = []
+        for i, p in enumerate(tree):
+            if not -1 <= p < i:
+                raise ValueError(f"the parent of draft {i} must be an earlier draft or -1, but is {p}")
+            seen.append((seen[p] if p >= 0 else 0) | 1 << i)
+        rows += seen
+    return torch.tensor([m - (1 << 64) if m >> 63 else m for m in rows], dtype=torch.int64, device=device)
+
+
+@_on_device
+def _cache_accept(dev, a, cu_seqlens, accepted, counts, context_out, stream):
+    B, Hkv, D = a.B, a.Hkv, a.D
+    if context_out is None:
+        context_out = _empty(stream, dev, B, dtype=torch.int32)
+    tiles, exp, most = a.num_blocks * Hkv, getattr(a, "kv_exp", None), accepted.shape[-1]
+    kind = _BF16 if exp is None else _F8
+    _check(_call(_entry["aflex_cache_accept"], dev, _stream(stream), None, 0,
+                 "k_cache", a.k_cache, kind, tiles * 16 * D, "v_cache", a.v_cache, kind, tiles * 16 * D,
+                 "kv_exp", exp, _I8, tiles * 32, "block_table", a.block_table, _I32, B * a.max_blocks,
+                 "context_lens", a.context_lens, _I32, B, "cu_seqlens", cu_seqlens, _I32, B + 1,
+                 "accepted", accepted, _I32, B * most, "counts", counts, _I32, B,
+                 "context_out", context_out, _I32, B,
+                 B, Hkv, D, most, a.block_size, a.max_blocks, a.num_blocks))
+    return context_out
+
+
+def cache_accept(a, cu_seqlens, accepted, counts, context_out=None, stream=None):
+    """Move the accepted drafts' cache entries of each sequence together, in place: draft accepted[b, i] (int32
+    [B, most], ascending, the first counts[b] of them) to place i behind the context before the drafts. Returns the
+    new context lengths [B] (a.context_lens keeps the old ones)."""
+    return _cache_accept(a.k_cache, a, cu_seqlens, accepted, counts, context_out, stream)

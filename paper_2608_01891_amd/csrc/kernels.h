@@ -4,6 +4,7 @@
 #include <stddef.h>
 
 #include "aflex.h"
+#include "aflex_draft.h"
 #include "aflex_longctx.h"
 
 namespace aflex {
@@ -44,6 +45,34 @@ hipError_t launch_block_select(const aflex_block_select_args& a, void* ws, hipSt
 hipError_t launch_rope_append(const aflex_rope_args& a, hipStream_t stream);
 hipError_t launch_rope_write(const aflex_rope_args& a, hipStream_t stream);
 hipError_t launch_block_summary(const aflex_block_summary_args& a, hipStream_t stream);
+
+// Writes into the 8-bit cache (rope_f8.hip), and accepted drafts (cache_accept.hip).
+hipError_t launch_rope_append_f8(const aflex_rope_f8_args& a, hipStream_t stream);
+hipError_t launch_rope_write_f8(const aflex_rope_f8_args& a, hipStream_t stream);
+hipError_t launch_cache_accept(const aflex_cache_accept_args& a, hipStream_t stream);
+
+// Attention of up to max_n query tokens per sequence (attn_rows.hip).
+struct RowsShape {
+  int B, T, Hq, Hkv, D;
+  int max_n;  // bound on a sequence's tokens
+  int max_blocks, num_blocks, max_ctx;
+  float scale;  // 0: 1 / sqrt(D)
+  bool f8;
+};
+struct RowsTensors {
+  const uint16_t* q;
+  const void* k_cache;
+  const void* v_cache;
+  const int8_t* kv_exp;
+  const int32_t* block_table;
+  const int32_t* context_lens;
+  const int32_t* cu_seqlens;  // NULL: a token per sequence
+  const uint64_t* masks;      // NULL: chains
+  uint16_t* out;
+};
+bool rows_shape_fits(const RowsShape& s);
+size_t rows_workspace_bytes(const RowsShape& s);
+hipError_t launch_attn_rows(const RowsShape& s, const RowsTensors& t, void* ws, hipStream_t stream);
 
 // Dense SwiGLU FFN (ffn.hip).
 size_t swiglu_workspace_bytes(const aflex_ffn_args& f);

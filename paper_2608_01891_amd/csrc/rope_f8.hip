@@ -1,0 +1,303 @@
+// Rotation of new tokens' queries and keys on the way into an 8-bit paged KV
+// cache, gfx950: e4m3 codes and one power of two per (token, kv head, K or V).
+//
+// The rotation is that of the bf16 writes (rope.hip); a rotated key stays in fp32
+// until its one rounding to 8 bits. A row's exponent is the least that fits its
+// largest magnitude, so the row's lanes exchange that maximum (3 steps inside a
+// DPP row, no LDS), and scaling by the power of two is exact.
+#include "block_codes.h"
+#include "f8.h"
+#include "kernels.h"
+#include "profile.h"
+#include "rope_unit.h"
+
+namespace aflex {
+
+// Exponent of the row whose lanes (N neighbours) hold 16 channels each.
+template <int N>
+__device__ __forceinline__ int unit_row_exponent(const float (&v)[16]) {
+  uint32_t m = 0;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) m = max(m, finite_mag(v[i]));
+  return row_exponent(lanes_max<N>(m));
+}
+
+__device__ __forceinline__ uint2 eight_codes(const float* v, float inv) {
+  float y[8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) y[i] = scaled(v[i], inv);
+  return make_uint2(four_codes(y[0], y[1], y[2], y[3]), four_codes(y[4], y[5], y[6], y[7]));
+}
+
+// ---------------------------------------------------------------------------
+// One token per sequence: the first B Hkv waves take a (sequence, kv head) each,
+// the key by the lanes of a row and the value by all 64, which spread its codes
+// over a column of the V tile; the other waves rotate queries, a unit per lane.
+template <int D, bool INTER>
+__global__ __launch_bounds__(256) void rope_append_f8_kernel(aflex_rope_f8_args a) {
+  constexpr int U = TileLanes<D>::U, NR = TileLanes<D>::NR;
+  const int lane = threadIdx.x & 63;
+  const long long wave = (long long)blockIdx.x * 4 + (threadIdx.x >> 6);
+  const long long nkv = (long long)a.B * a.Hkv;
+  const int rot = a.rotary_dim;
+  const int cap = a.max_blocks_per_seq * 16;
+  if (wave >= nkv) {
+    const long long idx = (wave - nkv) * 64 + lane;
+    if (idx >= (long long)a.B * a.Hq * U) return;
+    const int u = (int)(idx % U);
+    const long long bh = idx / U;
+    const int b = (int)(bh / a.Hq), h = (int)(bh - (long long)b * a.Hq);
+    int d0, d1;
+    unit_channels<INTER>(u, rot, d0, d1);
+    const uint16_t* src = a.q + (size_t)b * a.q_stride + (size_t)h * D;
+    uint4 x = ld4(src + d0), y = ld4(src + d1);
+    const int ctx = a.context_lens[b];
+    if (ctx <= 0 || ctx > cap) return;
+    if (rot > 0) {
+      const int pos = a.positions ? a.positions[b] : ctx - 1;
+      if (pos < 0 || pos >= a.rope_len) return;
+      if (u * 16 < rot) rotate_unit<INTER>(x, y, load_angles(a.rope, pos, rot, u));
+    }
+    uint16_t* dst = a.q_out + (size_t)bh * D;
+    st4(dst + d0, x);
+    st4(dst + d1, y);
+    return;
+  }
+  const int b = (int)(wave / a.Hkv), g = (int)(wave - (long long)b * a.Hkv);
+  const int u = lane % U;  // (every row of lanes holds the same key)
+  int d0, d1;
+  unit_channels<INTER>(u, rot, d0, d1);
+  const uint16_t* ks = a.k_new + (size_t)b * a.k_stride + (size_t)g * D;
+  const uint4 x = ld4(ks + d0), y = ld4(ks + d1);
+  const uint16_t* vs = a.v_new + (size_t)b * a.v_stride + (size_t)g * D;
+  float vv[NR];
+#pragma unroll
+  for (int i = 0; i < NR; ++i) vv[i] = bf2f(vs[i * 64 + lane]);
+  const int ctx = a.context_lens[b];
+  if (ctx <= 0 || ctx > cap) return;
+  const int j = ctx - 1, o = j % 16;
+  const int blk = a.block_table[(size_t)b * a.max_blocks_per_seq + j / 16];
+  const int pos = rot > 0 && a.positions ? a.positions[b] : j;
+  if (rot > 0 && (pos < 0 || pos >= a.rope_len)) return;
+  if (blk < 0 || blk >= a.num_blocks) return;
+  const size_t tile = (size_t)blk * a.Hkv + g;
+  float k[16];
+  unpack_unit(x, y, k);
+  if (rot > 0 && u * 16 < rot) rotate_unit<INTER>(k, load_angles(a.rope, pos, rot, u));
+  const int ke = unit_row_exponent<U>(k);
+  const float kinv = exp2_whole(-ke);
+  if (lane < U) {
+    uint8_t* kt = a.k_cache + tile * 16 * D + o * D;
+    *reinterpret_cast<uint2*>(kt + d0) = eight_codes(k, kinv);
+    *reinterpret_cast<uint2*>(kt + d1) = eight_codes(k + 8, kinv);
+  }
+  uint32_t vm = 0;
+#pragma unroll
+  for (int i = 0; i < NR; ++i) vm = max(vm, finite_mag(vv[i]));
+  const int ve = row_exponent((uint32_t)wave_max((int)vm));
+  const float vinv = exp2_whole(-ve);
+  uint8_t* vt = a.v_cache + tile * D * 16 + o;
+#pragma unroll
+  for (int i = 0; i < NR; ++i) vt[(i * 64 + lane) * 16] = (uint8_t)two_codes<false>(scaled(vv[i], vinv), 0.f, 0);
+  if (lane < 2) a.kv_exp[tile * 32 + lane * 16 + o] = (int8_t)(lane ? ve : ke);
+}
+
+// ---------------------------------------------------------------------------
+// Packed prompts, chunks and drafts: grid (block slot, part, sequence) as in the
+// bf16 write. A wave takes up to kHeadsPerWaveF8 heads with the angles it has
+// loaded, one where that leaves few waves.
+constexpr int kHeadsPerWaveF8 = 4;
+constexpr long long kManyWavesF8 = 16384;
+
+// Codes of 16 tokens x 8 channels (`row`: a token's 8 bf16 values) to the channels'
+// rows of the V tile at vt, for the tokens of `live`.
+__device__ __forceinline__ void store_v_codes(const uint4 (&row)[16], const float (&inv)[16], uint8_t* vt,
+                                              uint32_t live) {
+#pragma unroll
+  for (int e = 0; e < 8; ++e) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      float y[4];
+#pragma unroll
+      for (int t = 0; t < 4; ++t) {
+        const uint4& r = row[4 * i + t];
+        const uint32_t c = e < 2 ? r.x : e < 4 ? r.y : e < 6 ? r.z : r.w;
+        y[t] = scaled(e & 1 ? hi_f(c) : lo_f(c), inv[4 * i + t]);
+      }
+      w[i] = four_codes(y[0], y[1], y[2], y[3]);
+    }
+    uint8_t* dst = vt + e * 16;
+    if (live == 0xffffu) {
+      *reinterpret_cast<uint4*>(dst) = make_uint4(w[0], w[1], w[2], w[3]);
+      continue;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const uint32_t here = live >> (4 * i) & 0xfu;
+      if (here == 0xfu) {
+        *reinterpret_cast<uint32_t*>(dst + 4 * i) = w[i];
+      } else {
+#pragma unroll
+        for (int t = 0; t < 4; ++t)
+          if (here >> t & 1u) dst[4 * i + t] = (uint8_t)(w[i] >> (8 * t));
+      }
+    }
+  }
+}
+
+template <int D, bool INTER>
+__global__ __launch_bounds__(256) void rope_write_f8_kernel(aflex_rope_f8_args a, int vparts, int kparts,
+                                                            int per_wave) {
+  constexpr int U = TileLanes<D>::U, NR = TileLanes<D>::NR, RS = TileLanes<D>::RS;
+  Slot s;
+  if (!find_slot(a, blockIdx.z, blockIdx.x, s)) return;
+  int part = blockIdx.y;
+  const int rot = a.rotary_dim;
+  if (part < vparts) {
+    // V: a thread per (kv head, 8 channels) with the block's rows
+    if (s.blk < 0) return;
+    constexpr int C = D / 8;
+    const int t = part * 256 + threadIdx.x;
+    const int g = t / C, c = t % C;
+    if (g >= a.Hkv) return;  // (whole heads: the lanes of a row stay together)
+    const uint16_t* src = a.v_new + (size_t)g * D + c * 8;
+    const size_t tile = (size_t)s.blk * a.Hkv + g;
+    uint4 row[16];
+    uint32_t live = 0;  // rows that are written, the same for all threads
+#pragma unroll
+    for (int o = 0; o < 16; ++o) live |= slot_pos(a, s, o) >= 0 ? 1u << o : 0u;
+    live = __builtin_amdgcn_readfirstlane(live);
+    if (live == 0) return;
+    // (rows that are not written repeat one that is)
+    const int first = __builtin_ctz(live);
+#pragma unroll
+    for (int o = 0; o < 16; ++o) row[o] = ld4(src + (size_t)(s.src + (live >> o & 1 ? o : first)) * a.v_stride);
+    float inv[16];
+    uint32_t ew[4] = {0, 0, 0, 0};
+#pragma unroll
+    for (int o = 0; o < 16; ++o) {
+      const uint32_t w[4] = {row[o].x, row[o].y, row[o].z, row[o].w};
+      uint32_t m = 0;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) m = max(m, max(finite_mag(lo_f(w[i])), finite_mag(hi_f(w[i]))));
+      const int e = row_exponent(lanes_max<C>(m));
+      inv[o] = exp2_whole(-e);
+      ew[o / 4] |= (uint32_t)(e & 0xff) << (8 * (o & 3));
+    }
+    store_v_codes(row, inv, a.v_cache + (tile * D + c * 8) * 16, live);
+    if (c == 0) {
+      int8_t* ex = a.kv_exp + tile * 32 + 16;
+      if (live == 0xffffu) {
+        *reinterpret_cast<uint4*>(ex) = make_uint4(ew[0], ew[1], ew[2], ew[3]);
+      } else {
+#pragma unroll
+        for (int o = 0; o < 16; ++o)
+          if (live >> o & 1u) ex[o] = (int8_t)(ew[o / 4] >> (8 * (o & 3)));
+      }
+    }
+    return;
+  }
+  part -= vparts;
+  const bool key = part < kparts;
+  if (!key) part -= kparts;
+  if (key && s.blk < 0) return;
+  const int heads = key ? a.Hkv : a.Hq;
+  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
+  const int h0 = (part * 4 + wave) * per_wave, h1 = min(h0 + per_wave, heads);
+  if (h0 >= h1) return;
+  const int u = lane % U, r = lane / U;
+  int d0, d1;
+  unit_channels<INTER>(u, rot, d0, d1);
+  int pos[NR];
+  Angles an[NR];
+#pragma unroll
+  for (int i = 0; i < NR; ++i) {
+    pos[i] = slot_pos(a, s, r + i * RS);
+    if (pos[i] >= 0 && u * 16 < rot) an[i] = load_angles(a.rope, pos[i], rot, u);
+  }
+  const size_t stride = key ? a.k_stride : a.q_stride;
+  const uint16_t* base = key ? a.k_new : a.q;
+  auto load = [&](int h, uint4(&row)[NR][2]) {
+#pragma unroll
+    for (int i = 0; i < NR; ++i) {
+      if (pos[i] < 0) continue;
+      const uint16_t* p = base + (size_t)(s.src + r + i * RS) * stride + (size_t)h * D;
+      row[i][0] = ld4(p + d0);
+      row[i][1] = ld4(p + d1);
+    }
+  };
+  uint4 next[NR][2] = {};
+  load(h0, next);
+  for (int h = h0; h < h1; ++h) {
+    uint4 row[NR][2];
+#pragma unroll
+    for (int i = 0; i < NR; ++i) row[i][0] = next[i][0], row[i][1] = next[i][1];
+    if (h + 1 < h1) load(h + 1, next);
+#pragma unroll
+    for (int i = 0; i < NR; ++i) {
+      const int o = r + i * RS;
+      if (!key) {
+        if (pos[i] < 0) continue;
+        if (u * 16 < rot) rotate_unit<INTER>(row[i][0], row[i][1], an[i]);
+        uint16_t* dst = a.q_out + ((size_t)(s.src + o) * a.Hq + h) * D;
+        st4(dst + d0, row[i][0]);
+        st4(dst + d1, row[i][1]);
+        continue;
+      }
+      // (a row's lanes share its position: all of them go on, or none)
+      if (pos[i] < 0) continue;
+      float k[16];
+      unpack_unit(row[i][0], row[i][1], k);
+      if (u * 16 < rot) rotate_unit<INTER>(k, an[i]);
+      const int e = unit_row_exponent<U>(k);
+      const float inv = exp2_whole(-e);
+      const size_t tile = (size_t)s.blk * a.Hkv + h;
+      uint8_t* kt = a.k_cache + (tile * 16 + o) * D;
+      *reinterpret_cast<uint2*>(kt + d0) = eight_codes(k, inv);
+      *reinterpret_cast<uint2*>(kt + d1) = eight_codes(k + 8, inv);
+      if (u == 0) a.kv_exp[tile * 32 + o] = (int8_t)e;
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Host side.
+hipError_t launch_rope_append_f8(const aflex_rope_f8_args& in, hipStream_t stream) {
+  const aflex_rope_f8_args a = with_strides(in);
+  const long long waves = (long long)a.B * a.Hkv + ((long long)a.B * a.Hq * (a.D / 16) + 63) / 64;
+  const unsigned grid = (unsigned)((waves + 3) / 4);
+  ProfScope ps("rope_append_f8", stream);
+  if (a.D == 128 && a.interleaved)
+    rope_append_f8_kernel<128, true><<<grid, 256, 0, stream>>>(a);
+  else if (a.D == 128)
+    rope_append_f8_kernel<128, false><<<grid, 256, 0, stream>>>(a);
+  else if (a.interleaved)
+    rope_append_f8_kernel<64, true><<<grid, 256, 0, stream>>>(a);
+  else
+    rope_append_f8_kernel<64, false><<<grid, 256, 0, stream>>>(a);
+  return hipGetLastError();
+}
+
+hipError_t launch_rope_write_f8(const aflex_rope_f8_args& in, hipStream_t stream) {
+  if (in.T == 0 || in.max_seqlen == 0) return hipSuccess;
+  const aflex_rope_f8_args a = with_strides(in);
+  const int vparts = (a.Hkv * (a.D / 8) + 255) / 256;
+  const int slots = (a.max_seqlen + 15) / 16 + 1;
+  const int per_wave = (long long)slots * a.B * (a.Hq + a.Hkv) >= kManyWavesF8 * kHeadsPerWaveF8 ? kHeadsPerWaveF8 : 1;
+  const int per = 4 * per_wave;
+  const int kparts = (a.Hkv + per - 1) / per, qparts = (a.Hq + per - 1) / per;
+  const dim3 grid(slots, vparts + kparts + qparts, a.B);
+  ProfScope ps("rope_write_f8", stream);
+  if (a.D == 128 && a.interleaved)
+    rope_write_f8_kernel<128, true><<<grid, 256, 0, stream>>>(a, vparts, kparts, per_wave);
+  else if (a.D == 128)
+    rope_write_f8_kernel<128, false><<<grid, 256, 0, stream>>>(a, vparts, kparts, per_wave);
+  else if (a.interleaved)
+    rope_write_f8_kernel<64, true><<<grid, 256, 0, stream>>>(a, vparts, kparts, per_wave);
+  else
+    rope_write_f8_kernel<64, false><<<grid, 256, 0, stream>>>(a, vparts, kparts, per_wave);
+  return hipGetLastError();
+}
+
+}  // namespace aflex

@@ -28,11 +28,12 @@ bool plain(const at::Tensor& t, long dev) {
   return t.layout() == at::kStrided && !t.is_neg() && (dev < 0 ? t.is_cpu() : t.is_cuda() && t.get_device() == dev);
 }
 
-constexpr long kRows = 4;  // codes 0-3: the types of dense tensors
+constexpr long kRows = 4;  // the other codes: the types of dense tensors
 
 at::ScalarType type_of(long code) {
-  constexpr at::ScalarType types[4] = {at::kBFloat16, at::kFloat, at::kInt, at::kChar};
-  return code >= 0 && code < 4 ? types[code] : at::ScalarType::Undefined;
+  constexpr at::ScalarType types[7] = {at::kBFloat16, at::kFloat, at::kInt,  at::kChar, at::ScalarType::Undefined,
+                                       at::kLong,     at::kFloat8_e4m3fn};
+  return code >= 0 && code < 7 ? types[code] : at::ScalarType::Undefined;
 }
 
 // The argument block as it is laid out: addresses of 8 bytes, numbers of 4.

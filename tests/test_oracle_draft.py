@@ -1,0 +1,129 @@
+"""Pins of the oracle of the 8-bit cache and of drafted tokens: the type's own table, closed forms, invariants."""
+import math
+
+import pytest
+import torch
+
+import oracle
+from oracle import draft, longctx as lc
+from paper_2608_01891_amd import aflex, synth
+
+F8 = torch.float8_e4m3fn
+
+
+def test_rounding_is_that_of_the_type():
+    """All e4m3 values stand; halfway points go to even codes; everything else to the nearest."""
+    codes = torch.arange(0, 0x7f, dtype=torch.uint8)
+    v = codes.view(F8).double()
+    assert float(v[-1]) == 448.0 and torch.equal(draft.round_e4m3(v), v)
+    mid = (v[1:] + v[:-1]) / 2
+    assert torch.equal(draft.round_e4m3(mid), torch.where(codes[1:] % 2 == 0, v[1:], v[:-1]))
+    for t in (0.49, 0.51):
+        x = v[:-1] + (v[1:] - v[:-1]) * t
+        assert torch.equal(draft.round_e4m3(-x), -(v[1:] if t > 0.5 else v[:-1]))
+
+
+def test_encode_closed_forms():
+    def row(*x):
+        c, e = draft.encode(torch.tensor(x, dtype=torch.float64))
+        return c.tolist(), int(e)
+
+    assert row(448.0, -1.0) == ([448.0, -1.0], 0)
+    assert row(449.0, 0.0) == ([224.0, 0.0], 1)  # 224.5 rounds to 224
+    assert row(0.0, 0.0) == ([0.0, 0.0], -100)
+    assert row(1.0, 1 + 2.0 ** -5) == ([256.0, 256.0], -8)
+    assert row(448 * 2.0 ** -100, 2.0 ** -130) == ([448.0, 0.0], -100)
+    c, e = row(math.inf, 3.0)
+    assert math.isnan(c[0]) and (c[1], e) == (384.0, -7)
+
+
+@pytest.mark.parametrize("seed", range(3))
+def test_encode_is_within_half_a_step(seed):
+    g = torch.Generator().manual_seed(seed)
+    x = torch.randn(50, 128, generator=g, dtype=torch.float64) * torch.exp2(torch.randint(-40, 40, (50, 1), generator=g))
+    c, e = draft.encode(x)
+    m = x.abs().amax(-1)
+    assert bool((m <= 448 * 2.0 ** e).all()) and bool((m > 448 * 2.0 ** (e - 1)).all())
+    err = (draft.held(c, e[:, None]) - x).abs()
+    assert bool((err <= torch.maximum(x.abs() * 2.0 ** -4, 2.0 ** (e - 10.0)[:, None])).all())
+
+
+@pytest.mark.parametrize("f8", [False, True])
+def test_one_draft_is_decode_attention(f8):
+    a = synth.custom_attention(3, 4, 8, 2, 64, [1, 16, 40, 77], ctx_hi=80)
+    kc, vc, ex = a.k_cache, a.v_cache, None
+    if f8:
+        kc, ke = draft.encode(a.k_cache)
+        v, ve = draft.encode(a.v_cache.transpose(2, 3))
+        vc, ex = v.transpose(2, 3), torch.stack([ke, ve], 2)
+    out, mag, _ = draft.attention_tree(a.q, kc, vc, ex, a.block_table, a.context_lens, list(range(5)))
+    k, v = draft.held_pools(kc, vc, ex)
+    ref = oracle.attention_decode(a.q, k, v, a.block_table, a.context_lens)
+    assert torch.allclose(out, ref, rtol=1e-12, atol=1e-13) and bool((out.abs() <= mag * (1 + 1e-12)).all())
+
+
+def test_a_chain_is_causal_attention():
+    lens = [5, 1, 17]
+    a = synth.custom_attention(4, 3, 4, 2, 64, lens, ctx_hi=32)
+    p = synth.make_prefill(5, lens, 4, 2, 64)
+    kc, vc = oracle.kv_write(a.k_cache, a.v_cache, a.block_table, a.context_lens, p.cu_seqlens, p.k, p.v)
+    out, _, _ = draft.attention_tree(p.q, kc, vc, None, a.block_table, a.context_lens, p.cu_seqlens.tolist())
+    assert torch.allclose(out, oracle.attention_prefill(p.q, p.k, p.v, p.cu_seqlens), rtol=1e-12, atol=1e-13)
+    full = torch.full((23,), -1, dtype=torch.int64)
+    one = aflex.tree_masks([list(range(-1, n - 1)) for n in lens])
+    got, _, _ = draft.attention_tree(p.q, kc, vc, None, a.block_table, a.context_lens, p.cu_seqlens.tolist(), one)
+    assert torch.equal(got, out)
+    got, _, _ = draft.attention_tree(p.q, kc, vc, None, a.block_table, a.context_lens, p.cu_seqlens.tolist(), full)
+    assert not torch.allclose(got, out)
+    none, _, size = draft.attention_tree(p.q, kc, vc, None, a.block_table, a.context_lens, p.cu_seqlens.tolist(), full * 0)
+    assert not none.any() and not size.any()
+
+
+def test_masks_from_parents():
+    m = aflex.tree_masks([[-1, 0, 0, 2, -1], [-1], []])
+    assert m.tolist() == [1, 3, 5, 13, 16, 1] and m.dtype == torch.int64
+    assert aflex.tree_masks([list(range(-1, 63))])[63] == -1
+    for bad in ([0], [-1, 1], [-2], [-1] * 65):
+        with pytest.raises(ValueError):
+            aflex.tree_masks([bad])
+
+
+def test_a_branch_sees_what_its_chain_sees():
+    """The row of a tree's draft equals the last row of the chain of its ancestors."""
+    parents = [-1, 0, 0, 1, 2, 4, -1]
+    a = synth.custom_attention(6, 1, 4, 1, 64, [30], ctx_hi=32)
+    q = torch.randn(7, 4, 64, generator=torch.Generator().manual_seed(1)).bfloat16()
+    out, _, _ = draft.attention_tree(q, a.k_cache, a.v_cache, None, a.block_table, a.context_lens, [0, 7],
+                                     aflex.tree_masks([parents]))
+    for i, path in enumerate([[0], [0, 1], [0, 2], [0, 1, 3], [0, 2, 4], [0, 2, 4, 5], [6]]):
+        kc, vc, _, ctx = draft.accept(a.k_cache, a.v_cache, None, a.block_table, a.context_lens, [0, 7],
+                                      torch.tensor([path]), torch.tensor([len(path)]))
+        n = len(path)
+        assert int(ctx[0]) == 23 + n
+        one, _, _ = draft.attention_tree(q[path], kc, vc, None, a.block_table, ctx, [0, n])
+        assert torch.allclose(one[-1], out[i], rtol=1e-12, atol=1e-13)
+
+
+def test_accept_stops_at_what_does_not_ascend():
+    a = synth.custom_attention(7, 5, 2, 1, 64, [20, 20, 20, 5, 40], ctx_hi=48)
+    acc = torch.tensor([[1, 3, 2], [4, 1, 2], [0, 1, 2], [0, 1, 2], [2, 5, 6]])
+    _, _, _, new = draft.accept(a.k_cache, a.v_cache, None, a.block_table, a.context_lens, [0, 6, 10, 13, 20, 26], acc,
+                                torch.tensor([3, 3, 9, 3, 2]))
+    assert new.tolist() == [16, 16, 20, 5, 36]
+
+
+def test_write_places_rows_and_rotation_is_exact_for_quarter_turns():
+    a = synth.custom_attention(8, 2, 2, 1, 64, [17, 3], ctx_hi=32)
+    c = aflex.F8Cache(a)
+    k = torch.randn(4, 1, 64, generator=torch.Generator().manual_seed(2))
+    ang = torch.tensor([[0.0] * 8 + [1.0] * 8] * 4)  # cosines 0, sines 1
+    turned = lc.rotate(k, ang, False)
+    assert torch.equal(turned[..., :8], -k[..., 8:16].double()) and torch.equal(turned[..., 8:16], k[..., :8].double())
+    kc, vc, ex = draft.write(c.k_cache, c.v_cache, c.kv_exp, a.block_table, a.context_lens, [0, 2, 4], turned, k)
+    for b, r, pos in ((0, 0, 15), (0, 1, 16), (1, 2, 1), (1, 3, 2)):
+        blk = int(a.block_table[b, pos // 16])
+        back = draft.held(kc[blk, 0, pos % 16], ex[blk, 0, 0, pos % 16])
+        assert float((back - turned[r, 0]).abs().max()) <= 2.0 ** -4 * float(turned[r].abs().max())
+        back = draft.held(vc[blk, 0, :, pos % 16], ex[blk, 0, 1, pos % 16])
+        assert float((back - k[r, 0]).abs().max()) <= 2.0 ** -4 * float(k[r].abs().max())
+    assert int((kc != 0).any(-1).sum()) == 4
