@@ -28,6 +28,7 @@
 #include <math.h>
 
 #include <atomic>
+#include <type_traits>
 
 #include "common.h"
 #include "f8.h"
@@ -114,9 +115,11 @@ __device__ __forceinline__ size_t part_row(const RowsParams& p, const Seq& s, in
   return (size_t)s.row0 * p.Hq + (size_t)kvh * s.take * p.G + (size_t)pass * kPassRows + (size_t)wg * p.pass_rows;
 }
 
-__device__ __forceinline__ uint4 stream16(const uint8_t* p) {
-  typedef unsigned int u32x4 __attribute__((ext_vector_type(4)));
-  return __builtin_bit_cast(uint4, __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p)));
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+
+__device__ __forceinline__ u32x4 stream16(const uint8_t* p) {
+  return __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
 }
 
 // Eight codes (two words) as bf16 times 2^scale's exponent.
@@ -129,17 +132,15 @@ __device__ __forceinline__ bf16x8 widen(uint32_t a, uint32_t b, float scale) {
   return bf16x8{w[0][0], w[0][1], w[1][0], w[1][1], w[2][0], w[2][1], w[3][0], w[3][1]};
 }
 
-// The first n of 16 bytes, zeros behind them (n may be <= 0).
-__device__ __forceinline__ uint4 keep_bytes(uint4 v, int n) {
-  const auto w = [n](uint32_t x, int at) {
-    const int k = n - at;
-    return k >= 4 ? x : k <= 0 ? 0u : x & ((1u << (8 * k)) - 1u);
-  };
-  return make_uint4(w(v.x, 0), w(v.y, 4), w(v.z, 8), w(v.w, 12));
-}
-
-__device__ __forceinline__ uint32_t word_of(const uint4& v, int i) {
-  return i == 0 ? v.x : i == 1 ? v.y : i == 2 ? v.z : v.w;
+// The first n of the bytes, zeros behind them (n may be <= 0).
+template <class V>
+__device__ __forceinline__ V keep_bytes(V v, int n) {
+#pragma unroll
+  for (int i = 0; i < (int)(sizeof(V) / 4); ++i) {
+    const int k = n - 4 * i;
+    v[i] = k >= 4 ? v[i] : k <= 0 ? 0u : v[i] & ((1u << (8 * k)) - 1u);
+  }
+  return v;
 }
 
 // How many of the TOK tokens from place `tb` on a draft with these mask bits sees,
@@ -152,23 +153,42 @@ __device__ __forceinline__ uint32_t seen_bits(uint64_t mask, int tb, int start) 
   return ((uint32_t)mask << -off) | ((1u << -off) - 1u);
 }
 
+// Largest over the four lanes that hold a row (lane % 16).
+__device__ __forceinline__ float row_max(float x) {
+  auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+}
+
+// Two weights as bf16 pairs: the rounded weights, and what the rounding left.
+__device__ __forceinline__ void split_weights(float a, float b, uint32_t& hi, uint32_t& lo) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  hi = __builtin_bit_cast(uint32_t, bf16x2{static_cast<__bf16>(a), static_cast<__bf16>(b)});
+  lo = __builtin_bit_cast(uint32_t, bf16x2{static_cast<__bf16>(a - __uint_as_float(hi << 16)),
+                                           static_cast<__bf16>(b - __uint_as_float(hi & 0xffff0000u))});
+}
+
 }  // namespace
 
-// D, 8-bit cache or bf16, row tiles of a wave.
-template <int D, bool F8, int RT>
-__global__ __launch_bounds__(64 * kRowWaves, RT == 1 ? 3 : 2) void attn_rows_kernel(RowsParams p) {
-  constexpr int NC = D / 32;          // k-chunks of the first product
-  constexpr int NMT = D / 16;         // d-tiles of the second
-  constexpr int SB = F8 ? 4 : 2;      // blocks of a step
-  constexpr int KT = SB;              // its 16-token tiles in the first product
-  constexpr int TOK = F8 ? 16 : 8;    // tokens of a lane in the second product
-  constexpr int PS = TOK / 8;         // its 32-token slices
-  constexpr int LDQ = D + 8;          // padded row of q in LDS
-  constexpr int LDO = D + 4;          // row of a partial in LDS: O, then (m, l)
-  constexpr int QROWS = RT == 4 ? kPassRows : 16 * RT;
-  constexpr int kQBytes = QROWS * LDQ * 2;
+// D, 8-bit cache or bf16, row tiles of a wave, tokens of a lane in a step.
+template <int D, bool F8, int RT, int TOK>
+__global__ __launch_bounds__(64 * kRowWaves, 2) void attn_rows_kernel(RowsParams p) {
+  constexpr int NC = D / 32;       // k-chunks of the first product
+  constexpr int NMT = D / 16;      // d-tiles of the second
+  constexpr int SB = TOK / 4;      // blocks of a step (4 TOK tokens), and its tiles in the first product
+  constexpr int NK = SB * D / (F8 ? 64 : 32);  // loads of 16 bytes of its keys
+  typedef std::conditional_t<F8 && TOK == 8, u32x2, u32x4> VLoad;  // a lane's values of a channel
+  constexpr int PS = TOK / 8;      // 32-token slices of a step
+  // Few rows: q in registers, values loaded a step ahead like the keys. Many: q in
+  // LDS, and the values take the keys' registers behind the first product.
+  constexpr bool EARLY = RT <= 2;
+  constexpr int LDQ = D + 8;       // padded row of q in LDS
+  constexpr int LDO = D + 4;       // row of a partial in LDS: O, then (m, l)
+  constexpr int kQBytes = EARLY ? 0 : kPassRows * LDQ * 2;
   constexpr int kPartBytes = 2 * 16 * RT * LDO * 4;  // partials of two waves
   __shared__ __attribute__((aligned(16))) uint8_t sm[kQBytes > kPartBytes ? kQBytes : kPartBytes];
+  __shared__ uint64_t sm_mask[EARLY ? 1 : kPassRows];
   uint16_t* sq = reinterpret_cast<uint16_t*>(sm);
   float* so = reinterpret_cast<float*>(sm);
 
@@ -177,6 +197,10 @@ __global__ __launch_bounds__(64 * kRowWaves, RT == 1 ? 3 : 2) void attn_rows_ker
   const int lane = tid & 63;
   const int r = lane & 15, qg = lane >> 4;
   const int G = p.G, wg = blockIdx.x, P = gridDim.x;
+  // places of the lane in a step: block and token of its key row (token + 4 t in tile
+  // t), block and first token of its values
+  const int kblk = TOK == 16 ? r >> 2 : r >> 3, ktok = TOK == 16 ? r & 3 : ((r >> 2) & 1) * 8 + (r & 3);
+  const int vblk = TOK == 16 ? qg : qg >> 1, vtok = TOK == 16 ? 0 : (qg & 1) * 8;
 
   // Rows of sequences without cached tokens are zeros.
   for (int b = wg; b < p.B; b += P) {
@@ -250,18 +274,118 @@ __global__ __launch_bounds__(64 * kRowWaves, RT == 1 ? 3 : 2) void attn_rows_ker
     const int turns = kRowWaves / share, turn = wave / share;
     const int row_base = pass * kPassRows;
 
-    // ---- q into LDS: row i G + h of the pass is token i, head kvh G + h ----
-    __syncthreads();
-    for (int i = tid; i < tiles * 16 * (D / 8); i += 64 * kRowWaves) {
-      const int row = i / (D / 8), c = i % (D / 8);
-      uint4 v = make_uint4(0, 0, 0, 0);
-      if (row < rows) {
-        const int tok = (row_base + row) / G, h = row_base + row - tok * G;
-        v = *reinterpret_cast<const uint4*>(p.q + ((size_t)(s.row0 + tok) * p.Hq + kvh * G + h) * D + c * 8);
+    // ---- block ids: scalar loads, a step ahead of the keys' ----
+    typedef const int32_t __attribute__((address_space(4))) * ScalarTable;
+    const ScalarTable table = (ScalarTable)(reinterpret_cast<uintptr_t>(p.bt + (size_t)b * p.max_blocks));
+    const int steps = mine > 0 ? (j1 - j0 + SB - 1) / SB : 0;
+    int raw0 = -1, raw1 = -1, raw2 = -1, raw3 = -1;  // as the table has them
+    int id0 = -1, id1 = -1, id2 = -1, id3 = -1;      // of the step at hand; -1: no such block
+    auto fetch_ids = [&](int st) __attribute__((always_inline)) {
+      const int j = j0 + st * SB;
+      raw0 = table[min(j, j1 - 1)];
+      raw1 = table[min(j + 1, j1 - 1)];
+      if constexpr (SB == 4) {
+        raw2 = table[min(j + 2, j1 - 1)];
+        raw3 = table[min(j + 3, j1 - 1)];
       }
-      *reinterpret_cast<uint4*>(sq + row * LDQ + c * 8) = v;
+    };
+    auto take_ids = [&](int st) __attribute__((always_inline)) {
+      const int j = j0 + st * SB;
+      const auto fine = [&](int id, int at) { return at < j1 && id >= 0 && id < p.num_blocks ? id : -1; };
+      id0 = fine(raw0, j);
+      id1 = fine(raw1, j + 1);
+      if constexpr (SB == 4) {
+        id2 = fine(raw2, j + 2);
+        id3 = fine(raw3, j + 3);
+      }
+    };
+    // (blocks that do not exist are read at block 0 and masked)
+    auto pick = [&](int blk) __attribute__((always_inline)) {
+      const int low = (blk & 1) ? id1 : id0;
+      if constexpr (SB == 4) return (blk & 2) ? ((blk & 1) ? id3 : id2) : low;
+      return low;
+    };
+    u32x4 kraw[NK];   // (8-bit codes come 16 channels a load, and the k-chunks take the channels in that order)
+    VLoad vraw[NMT];
+    u32x4 kx, vx;     // exponents of the lane's key block, and of its value block
+    int tb = 0, nv = 0, jb = 0;  // place of the lane's first token, how many of them are cached; first block
+    auto load_keys = [&]() __attribute__((always_inline)) {
+      const size_t tile = (size_t)max(pick(kblk), 0) * p.Hkv + kvh;
+      if constexpr (F8) {
+        kx = *reinterpret_cast<const u32x4*>(p.ke + tile * 32);
+        const uint8_t* kb = p.kc + (tile * 16 + ktok) * D + qg * 16;
+#pragma unroll
+        for (int t = 0; t < SB; ++t)
+#pragma unroll
+          for (int c = 0; c < NC / 2; ++c) kraw[t * (NC / 2) + c] = stream16(kb + 4 * t * D + c * 64);
+      } else {
+        const uint8_t* kb = p.kc + ((tile * 16 + ktok) * D + qg * 8) * 2;
+#pragma unroll
+        for (int t = 0; t < SB; ++t)
+#pragma unroll
+          for (int c = 0; c < NC; ++c) kraw[t * NC + c] = stream16(kb + (4 * t * D + c * 32) * 2);
+      }
+    };
+    auto load_values = [&](int st) __attribute__((always_inline)) {
+      const int vid = pick(vblk);
+      const size_t tile = (size_t)max(vid, 0) * p.Hkv + kvh;
+      jb = j0 + st * SB;
+      tb = (jb + vblk) * 16 + vtok;
+      nv = vid >= 0 ? s.ctx - tb : 0;
+      if constexpr (F8) {
+        vx = *reinterpret_cast<const u32x4*>(p.ke + tile * 32 + 16);
+        const uint8_t* vb = p.vc + (tile * D + r) * 16 + vtok;
+#pragma unroll
+        for (int mt = 0; mt < NMT; ++mt)
+          vraw[mt] = __builtin_nontemporal_load(reinterpret_cast<const VLoad*>(vb + mt * 256));
+      } else {
+        const uint8_t* vb = p.vc + ((tile * D + r) * 16 + vtok) * 2;
+#pragma unroll
+        for (int mt = 0; mt < NMT; ++mt) vraw[mt] = stream16(vb + mt * 512);
+      }
+    };
+
+    int st = turn;
+    if (st < steps) {
+      fetch_ids(st);
+      take_ids(st);
+      load_keys();
+      if constexpr (EARLY) load_values(st);
+      fetch_ids(min(st + turns, steps - 1));
     }
-    __syncthreads();
+
+    // ---- q: row i G + h of the pass is token i, head kvh G + h ----
+    auto q_row = [&](int row) {
+      const int tok = (row_base + row) / G, h = row_base + row - tok * G;
+      return p.q + ((size_t)(s.row0 + tok) * p.Hq + kvh * G + h) * D;
+    };
+    auto q_channel = [&](int c) { return F8 ? (c >> 1) * 64 + qg * 16 + (c & 1) * 8 : c * 32 + qg * 8; };
+    auto mask_row = [&](int row) {
+      const int tok = (row_base + row) / G;
+      return p.masks ? p.masks[s.row0 + tok] : (2ull << tok) - 1ull;
+    };
+    bf16x8 qreg[EARLY ? RT : 1][NC];
+    uint64_t mask_of[EARLY ? RT : 1];
+    if constexpr (EARLY) {
+#pragma unroll
+      for (int t = 0; t < RT; ++t) {
+        const int row = t * 16 + r;
+        mask_of[t] = mask_row(min(row, rows - 1));
+        const uint16_t* src = q_row(min(row, rows - 1));
+#pragma unroll
+        for (int c = 0; c < NC; ++c) qreg[t][c] = row < rows ? ld_bf16x8(src + q_channel(c)) : zero_bf16x8();
+      }
+    } else {
+      __syncthreads();
+      for (int i = tid; i < tiles * 16 * (D / 8); i += 64 * kRowWaves) {
+        const int row = i / (D / 8), c = i % (D / 8);
+        uint4 v = make_uint4(0, 0, 0, 0);
+        if (row < rows) v = *reinterpret_cast<const uint4*>(q_row(row) + c * 8);
+        *reinterpret_cast<uint4*>(sq + row * LDQ + c * 8) = v;
+      }
+      for (int row = tid; row < tiles * 16; row += 64 * kRowWaves) sm_mask[row] = mask_row(min(row, rows - 1));
+      __syncthreads();
+    }
 
     float m_run[RT], l_run[RT];
     f32x4 acc[RT][NMT];
@@ -273,181 +397,145 @@ __global__ __launch_bounds__(64 * kRowWaves, RT == 1 ? 3 : 2) void attn_rows_ker
       for (int mt = 0; mt < NMT; ++mt) acc[t][mt] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
 
-    const int steps = (j1 - j0 + SB - 1) / SB;
-    const int32_t* table = p.bt + (size_t)b * p.max_blocks;
-    auto load_id = [&](int j) {
-      const int id = j < j1 ? table[j] : -1;
-      return id >= 0 && id < p.num_blocks ? id : -1;
-    };
-    // Block ids, 64 per wave register, the next ones loaded a register ahead.
-    int my_id = load_id(j0 + lane), next_id = load_id(j0 + 64 + lane), chunk = 0;
-
-    for (int st = turn; st < (mine > 0 ? steps : 0); st += turns) {
-      if (st * SB / 64 != chunk) {
-        chunk = st * SB / 64;
-        my_id = next_id;
-        next_id = load_id(j0 + (chunk + 1) * 64 + lane);
-      }
-      int id[SB];
+    // The steps of this wave with N row tiles.
+    auto run_steps = [&](auto count) __attribute__((always_inline)) {
+      constexpr int N = decltype(count)::value;
+      for (; st < steps; st += turns) {
+        const int next = st + turns < steps ? st + turns : st;  // (the last step's loads are repeated, of data at hand)
+        // ---- S^T: the tiles of the step, each against all row tiles ----
+        f32x4 sc[N][SB];
 #pragma unroll
-      for (int i = 0; i < SB; ++i) id[i] = __builtin_amdgcn_readlane(my_id, (st * SB + i) & 63);
-      const int jb = j0 + st * SB;
-      // the block of the lane's key row, and that of its values
-      int pk, pv, vb;
-      if constexpr (F8) {
-        pk = (r & 8) ? ((r & 4) ? id[3] : id[2]) : ((r & 4) ? id[1] : id[0]);
-        pv = (qg & 2) ? ((qg & 1) ? id[3] : id[2]) : ((qg & 1) ? id[1] : id[0]);
-        vb = qg;
-      } else {
-        pk = (r & 8) ? id[1] : id[0];
-        pv = (qg & 2) ? id[1] : id[0];
-        vb = qg >> 1;
-      }
-      const int tb = (jb + vb) * 16 + (F8 ? 0 : (qg & 1) * 8);  // place of the lane's first token
-      const int nv = pv >= 0 ? s.ctx - tb : 0;                  // how many of them are cached
-
-      // keys: tile t holds tokens of all SB blocks; the lane's row
-      bf16x8 kf[KT][NC];
-      if constexpr (F8) {
-        float ks[KT] = {};
-        if (pk >= 0) {
-          const size_t tile = (size_t)pk * p.Hkv + kvh;
-          const uint4 ex = *reinterpret_cast<const uint4*>(p.ke + tile * 32);
-          const uint8_t* kb = p.kc + (tile * 16 + (r & 3)) * D + qg * 16;
-          uint4 raw[KT][NC / 2];
+        for (int t = 0; t < N; ++t)
 #pragma unroll
-          for (int t = 0; t < KT; ++t)
+          for (int k = 0; k < SB; ++k) sc[t][k] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int c = 0; c < NC / 2; ++c) raw[t][c] = stream16(kb + 4 * t * D + c * 64);
-#pragma unroll
-          for (int t = 0; t < KT; ++t) {
-            ks[t] = exp2_whole((int8_t)(word_of(ex, t) >> (8 * (r & 3))));
+        for (int k = 0; k < SB; ++k) {
+          bf16x8 kf[NC];
+          if constexpr (F8) {
+            const uint32_t ex = TOK == 16 ? kx[k] : (r & 4) ? kx[(2 + k) & 3] : kx[k & 1];
+            const float f = exp2_whole((int8_t)(ex >> (8 * (r & 3))));
 #pragma unroll
             for (int c = 0; c < NC / 2; ++c) {
-              kf[t][2 * c] = widen(raw[t][c].x, raw[t][c].y, ks[t]);
-              kf[t][2 * c + 1] = widen(raw[t][c].z, raw[t][c].w, ks[t]);
+              const u32x4 w = kraw[k * (NC / 2) + c];
+              kf[2 * c] = widen(w[0], w[1], f);
+              kf[2 * c + 1] = widen(w[2], w[3], f);
             }
+          } else {
+#pragma unroll
+            for (int c = 0; c < NC; ++c) kf[c] = __builtin_bit_cast(bf16x8, kraw[k * NC + c]);
           }
-        } else {
 #pragma unroll
-          for (int t = 0; t < KT; ++t)
+          for (int t = 0; t < N; ++t)
 #pragma unroll
-            for (int c = 0; c < NC; ++c) kf[t][c] = zero_bf16x8();
+            for (int c = 0; c < NC; ++c) {
+              bf16x8 qf;
+              if constexpr (EARLY)
+                qf = qreg[t][c];
+              else
+                qf = ld_bf16x8(sq + ((t0 + t) * 16 + r) * LDQ + q_channel(c));
+              sc[t][k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[c], qf, sc[t][k], 0, 0, 0);
+            }
         }
-      } else {
-        if (pk >= 0) {
-          const uint8_t* kb =
-              p.kc + ((((size_t)pk * p.Hkv + kvh) * 16 + ((r >> 2) & 1) * 8 + (r & 3)) * D + qg * 8) * 2;
-#pragma unroll
-          for (int t = 0; t < KT; ++t)
-#pragma unroll
-            for (int c = 0; c < NC; ++c)
-              kf[t][c] = __builtin_bit_cast(bf16x8, stream16(kb + (4 * t * D + c * 32) * 2));
-        } else {
-#pragma unroll
-          for (int t = 0; t < KT; ++t)
-#pragma unroll
-            for (int c = 0; c < NC; ++c) kf[t][c] = zero_bf16x8();
+        // (nothing moves across: the loads take the registers that the keys leave)
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (!EARLY) load_values(st);
+        const int tb_now = tb, nv_now = nv, jb_now = jb;
+        if constexpr (EARLY) {
+          take_ids(next);
+          load_keys();
+          fetch_ids(min(next + turns, steps - 1));
         }
-      }
-      // values: zeros behind the context, so that 0 times what lies there is 0
-      uint4 vraw[NMT];
-      int vexp[F8 ? TOK : 1];
-      if (pv >= 0) {
-        const size_t tile = (size_t)pv * p.Hkv + kvh;
-        const uint8_t* vbase = F8 ? p.vc + (tile * D + r) * 16 : p.vc + ((tile * D + r) * 16 + (qg & 1) * 8) * 2;
-#pragma unroll
-        for (int mt = 0; mt < NMT; ++mt) vraw[mt] = stream16(vbase + mt * 16 * 16 * (F8 ? 1 : 2));
-        if constexpr (F8) {
-          const uint4 ex = *reinterpret_cast<const uint4*>(p.ke + tile * 32 + 16);
-#pragma unroll
-          for (int e = 0; e < TOK; ++e) vexp[e] = (int8_t)(word_of(ex, e / 4) >> (8 * (e & 3)));
-        }
-      } else {
-#pragma unroll
-        for (int mt = 0; mt < NMT; ++mt) vraw[mt] = make_uint4(0, 0, 0, 0);
-        if constexpr (F8) {
-#pragma unroll
-          for (int e = 0; e < TOK; ++e) vexp[e] = 0;
-        }
-      }
-      if (nv < TOK) {
-#pragma unroll
-        for (int mt = 0; mt < NMT; ++mt)
-          vraw[mt] = F8 ? keep_bytes(vraw[mt], nv)
-                        : __builtin_bit_cast(uint4, keep_first(__builtin_bit_cast(bf16x8, vraw[mt]), nv));
-      }
-      bf16x8 vf[PS][NMT];
-#pragma unroll
-      for (int mt = 0; mt < NMT; ++mt) {
-        if constexpr (F8) {
-          vf[0][mt] = widen(vraw[mt].x, vraw[mt].y, 1.f);
-          vf[PS - 1][mt] = widen(vraw[mt].z, vraw[mt].w, 1.f);
-        } else {
-          vf[0][mt] = __builtin_bit_cast(bf16x8, vraw[mt]);
-        }
-      }
-      // tokens that exist, as bits; whether the step reaches the drafts
-      const uint32_t cached = nv >= TOK ? (1u << TOK) - 1u : nv <= 0 ? 0u : (1u << nv) - 1u;
-      const bool open = (jb + SB) * 16 <= start;
+        __builtin_amdgcn_sched_barrier(0);
 
+        // ---- weights ----
+        if (!((jb_now + SB) * 16 <= start && __all(nv_now >= TOK))) {  // drafts, or places that hold nothing
+          const uint32_t cached = nv_now >= TOK ? (1u << TOK) - 1u : nv_now <= 0 ? 0u : (1u << nv_now) - 1u;
 #pragma unroll
-      for (int t = 0; t < RT; ++t) {
-        if (t >= mine) break;
-        const int row = (t0 + t) * 16 + r;  // of the pass
-        f32x4 sc[KT];
+          for (int t = 0; t < N; ++t) {
+            const uint64_t mask = EARLY ? mask_of[t] : sm_mask[(t0 + t) * 16 + r];
+            const uint32_t seen = cached & seen_bits(mask, tb_now, start);
 #pragma unroll
-        for (int k = 0; k < KT; ++k) sc[k] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int c = 0; c < NC; ++c) {
-          const int d = F8 ? (c >> 1) * 64 + qg * 16 + (c & 1) * 8 : c * 32 + qg * 8;
-          const bf16x8 qf = ld_bf16x8(sq + row * LDQ + d);
-#pragma unroll
-          for (int k = 0; k < KT; ++k) sc[k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[k][c], qf, sc[k], 0, 0, 0);
-        }
-        uint32_t seen = cached;
-        if (!open) {
-          uint64_t mask = 0;
-          if (row < rows) {
-            const int tok = (row_base + row) / G;
-            mask = p.masks ? p.masks[s.row0 + tok] : (2ull << tok) - 1ull;
+            for (int e = 0; e < TOK; ++e) sc[t][e / 4][e & 3] = (seen >> e & 1u) ? sc[t][e / 4][e & 3] : kNegInf;
           }
-          seen &= seen_bits(mask, tb, start);
+          if (!__all(nv_now >= TOK)) {  // zeros behind the context, so that 0 times what lies there is 0
+#pragma unroll
+            for (int mt = 0; mt < NMT; ++mt) vraw[mt] = keep_bytes(vraw[mt], F8 ? nv_now : 2 * nv_now);
+          }
         }
-        float sv[TOK];
+        uint32_t hi[N][TOK / 2], lo[N][TOK / 2];
 #pragma unroll
-        for (int e = 0; e < TOK; ++e) sv[e] = (seen >> e & 1u) ? sc[e / 4][e & 3] * p.scale_log2 : kNegInf;
-        float mx = sv[0];
+        for (int t = 0; t < N; ++t) {
+          float mx = sc[t][0][0];
 #pragma unroll
-        for (int e = 1; e < TOK; ++e) mx = fmaxf(mx, sv[e]);
-        mx = fmaxf(mx, __shfl_xor(mx, 16));
-        mx = fmaxf(mx, __shfl_xor(mx, 32));
-        const float m_new = fmaxf(m_run[t], mx);
-        const float m_use = (m_new == kNegInf) ? 0.f : m_new;
-        const float alpha = fast_exp2(m_run[t] - m_use);
-        m_run[t] = m_new;
-        float ps = 0.f;
-        bf16x8 hi[PS], lo[PS];
+          for (int e = 1; e < TOK; ++e) mx = fmaxf(mx, sc[t][e / 4][e & 3]);
+          const float m_new = fmaxf(m_run[t], row_max(mx) * p.scale_log2);
+          const float m_use = (m_new == kNegInf) ? 0.f : m_new;
+          if (!__all(m_new == m_run[t])) {
+            const float alpha = fast_exp2(m_run[t] - m_use);
+            l_run[t] *= alpha;
 #pragma unroll
-        for (int e = 0; e < TOK; ++e) {
-          const float w = fast_exp2(sv[e] - m_use);
-          ps += w;
-          float u = w;
-          if constexpr (F8) u = __builtin_ldexpf(w, vexp[e]);
-          const __bf16 h = static_cast<__bf16>(u);
-          hi[e / 8][e & 7] = h;
-          lo[e / 8][e & 7] = static_cast<__bf16>(u - static_cast<float>(h));
+            for (int mt = 0; mt < NMT; ++mt) acc[t][mt] *= alpha;
+            m_run[t] = m_new;
+          }
+          float ps = 0.f;
+#pragma unroll
+          for (int e = 0; e < TOK; e += 2) {
+            float w[2];
+#pragma unroll
+            for (int i = 0; i < 2; ++i) {
+              const int at = e + i;
+              w[i] = fast_exp2(fmaf(sc[t][at / 4][at & 3], p.scale_log2, -m_use));
+              ps += w[i];
+              if constexpr (F8) {
+                const uint32_t ex = TOK == 16 ? vx[at / 4] : (qg & 1) ? vx[(2 + at / 4) & 3] : vx[at / 4 & 1];
+                w[i] = __builtin_ldexpf(w[i], (int8_t)(ex >> (8 * (at & 3))));
+              }
+            }
+            split_weights(w[0], w[1], hi[t][e / 2], lo[t][e / 2]);
+          }
+          l_run[t] += ps;
         }
-        l_run[t] = l_run[t] * alpha + ps;
+
+        // ---- O^T ----
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int mt = 0; mt < NMT; ++mt) {
-          acc[t][mt] *= alpha;
-#pragma unroll
-          for (int k = 0; k < PS; ++k) {
-            acc[t][mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[k][mt], hi[k], acc[t][mt], 0, 0, 0);
-            acc[t][mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[k][mt], lo[k], acc[t][mt], 0, 0, 0);
+          bf16x8 vf[PS];
+          if constexpr (F8) {
+            vf[0] = widen(vraw[mt][0], vraw[mt][1], 1.f);
+            if constexpr (PS == 2) vf[1] = widen(vraw[mt][2], vraw[mt][3], 1.f);
+          } else {
+            vf[0] = __builtin_bit_cast(bf16x8, vraw[mt]);
           }
+#pragma unroll
+          for (int t = 0; t < N; ++t)
+#pragma unroll
+            for (int k = 0; k < PS; ++k) {
+              const uint32_t *h = hi[t] + 4 * k, *l = lo[t] + 4 * k;
+              acc[t][mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                  vf[k], __builtin_bit_cast(bf16x8, u32x4{h[0], h[1], h[2], h[3]}), acc[t][mt], 0, 0, 0);
+              acc[t][mt] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                  vf[k], __builtin_bit_cast(bf16x8, u32x4{l[0], l[1], l[2], l[3]}), acc[t][mt], 0, 0, 0);
+            }
         }
+        __builtin_amdgcn_sched_barrier(0);
+        if constexpr (EARLY) {
+          load_values(next);
+        } else {
+          take_ids(next);
+          load_keys();
+          fetch_ids(min(next + turns, steps - 1));
+        }
+      }
+    };
+    if constexpr (RT == 1) {
+      run_steps(std::integral_constant<int, 1>{});
+    } else {
+      if (mine == 1) run_steps(std::integral_constant<int, 1>{});
+      if (mine == 2) run_steps(std::integral_constant<int, 2>{});
+      if constexpr (RT == 4) {
+        if (mine == 3) run_steps(std::integral_constant<int, 3>{});
+        if (mine == 4) run_steps(std::integral_constant<int, 4>{});
       }
     }
 
@@ -627,11 +715,11 @@ size_t part_rows(const RowsShape& s) { return (size_t)s.T * s.Hq + (size_t)rows_
 template <int D, bool F8>
 void launch_tiles(const RowsParams& p, int tiles, int P, hipStream_t stream) {
   if (tiles == 1)
-    attn_rows_kernel<D, F8, 1><<<P, 64 * kRowWaves, 0, stream>>>(p);
+    attn_rows_kernel<D, F8, 1, F8 ? 16 : 8><<<P, 64 * kRowWaves, 0, stream>>>(p);
   else if (tiles == 2)
-    attn_rows_kernel<D, F8, 2><<<P, 64 * kRowWaves, 0, stream>>>(p);
+    attn_rows_kernel<D, F8, 2, 8><<<P, 64 * kRowWaves, 0, stream>>>(p);
   else
-    attn_rows_kernel<D, F8, 4><<<P, 64 * kRowWaves, 0, stream>>>(p);
+    attn_rows_kernel<D, F8, 4, 8><<<P, 64 * kRowWaves, 0, stream>>>(p);
 }
 
 }  // namespace
