@@ -135,7 +135,8 @@ typedef struct aflex_attn_tree_args {
 
 /* Supported: D in {64, 128}, block_size == 16, Hq % Hkv == 0, Hq / Hkv <= 16, */
 /* max_drafts <= 64, T <= B * max_drafts, B * Hkv * (ceil(max_context_len /    */
-/* 16) + 16) * ceil(max_drafts * (Hq / Hkv) / 256) < 2^30, T * Hq < 2^30.      */
+/* 16) + 16) * ceil(max_drafts * (Hq / Hkv) / 192) < 2^30, T * Hq < 2^30,      */
+/* T < 2^24, Hkv <= 65535. */
 /* Device-side values are clamped: rows to [0, T], contexts to [0,             */
 /* max_context_len] (s_b then counts from the clamped length; places below 0   */
 /* do not exist, and the drafts there are not seen); rows of a sequence beyond */

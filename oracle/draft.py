@@ -78,15 +78,16 @@ def write(k_cache, v_cache, kv_exp, block_table, context_lens, cu, k, v):
 
 
 def attention_tree(q, k_cache, v_cache, kv_exp, block_table, context_lens, cu, masks=None, scale=None):
-    """(out, sum_j p_j |v_j|, largest sum_d |q_d k_jd| scale over the seen j), the first two [T, Hq, D], the last
-    [T, Hq], in float64."""
+    """out [T, Hq, D] and what bounds its rounding errors, in float64: sum_j p_j |v_j| [T, Hq, D]; the largest
+    sum_d |q_d k_jd| scale over the seen j [T, Hq]; for an 8-bit cache max_j (p_j 2^e_j) sum_j |c_j| [T, Hq, D], e_j
+    and c_j the exponent and codes of v_j (else zeros)."""
     T, Hq, D = q.shape
     N, Hkv = k_cache.shape[:2]
     G = Hq // Hkv
     scale = scale or 1.0 / math.sqrt(D)
     kp, vp = held_pools(k_cache, v_cache, kv_exp)
     out, mag = torch.zeros(T, Hq, D, dtype=torch.float64), torch.zeros(T, Hq, D, dtype=torch.float64)
-    size = torch.zeros(T, Hq, dtype=torch.float64)
+    size, small = torch.zeros(T, Hq, dtype=torch.float64), torch.zeros(T, Hq, D, dtype=torch.float64)
     for b in range(len(context_lens)):
         ctx, n = max(int(context_lens[b]), 0), cu[b + 1] - cu[b]
         start = ctx - n
@@ -107,7 +108,11 @@ def attention_tree(q, k_cache, v_cache, kv_exp, block_table, context_lens, cu, m
                 p = torch.softmax(x @ k.t() * scale, -1)
                 out[cu[b] + i, h], mag[cu[b] + i, h] = p @ v, p @ v.abs()
                 size[cu[b] + i, h] = (x.abs() @ k.abs().t()).amax(-1) * scale
-    return out, mag, size
+                if kv_exp is not None:
+                    e = kv_exp[blk[at], g, 1, at % 16].to(torch.int64)
+                    codes = v_cache[blk[at], g, :, at % 16].to(torch.float64).abs().sum(0)
+                    small[cu[b] + i, h] = torch.ldexp(p, e).amax(-1, keepdim=True) * codes
+    return out, mag, size, small
 
 
 def accept(k_cache, v_cache, kv_exp, block_table, context_lens, cu, accepted, counts):

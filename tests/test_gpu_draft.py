@@ -3,14 +3,18 @@
 Tolerances. Writes: queries as in the bf16 write: three fp32 roundings and one to
 bf16. Cached rows are compared for equality with codes made from the formula's fp32
 operations, which the plain expression repeats. Attention: out is rounded to bf16,
-2^-8 of |out|; a weight enters the product as two bf16 values, the second rounded
-to 2^-8 of at most 2^-8 of it: 2^-16 of the weight; the products and the sum of
-the weights are fp32 sums of n terms: at most 2 n 2^-24 of sum p |v|. A score is
-an fp32 sum of D products, its scaling and the running maximum's subtraction 4
-more roundings: (D + 4) 2^-24 of sum |q k| scale, which exp2 (itself off by
-2^-22) turns into as much of the weight, in the numerator and in the
-denominator. Hence
-  |y - r| <= 2^-8 |r| + 1.01 (2^-16 + 2^-21 + 2 n 2^-24 + 2 (D + 4) 2^-24 size) sum p |v|.
+2^-8 of |out|. Over a bf16 cache a weight enters the product as two bf16 values, the
+second rounded to 2^-8 of at most 2^-8 of it: 2^-16 of the weight. Over an 8-bit one
+it is p 2^e over the largest p 2^e of the row, rounded to fp16: 2^-11 of it, or half
+the least step, 2^-25 of the largest: on a code c, 2^-25 max(p 2^e) |c| (`small`
+sums those). The products and the sum of the weights are fp32 sums of n terms: at
+most 2 n 2^-24 of sum p |v|. A score is an fp32 sum of D products, its scaling and
+the running maximum's subtraction 4 more roundings: (D + 4) 2^-24 of sum |q k|
+scale; the exponents added to it, of magnitudes up to 16 here, 16 2^-24. exp2 (itself
+off by 2^-22) turns that into as much of the weight, in the numerator and in the
+denominator: 2 (D + 4) 2^-24 size + 2^-19 + 2^-21. Hence
+  |y - r| <= 2^-8 |r| + 1.01 ((w + 2^-18 + 2 n 2^-24 + 2 (D + 4) 2^-24 size) sum p |v| + 2^-25 small)
+with w = 2^-16 or 2^-11.
 Whatever is copied or masked is compared for equality.
 """
 import threading
@@ -246,8 +250,10 @@ def test_write_leaves_alone_what_has_no_place(gpu_lib):
 
 # ------------------------------------------------------------------ attention
 def _check_attn(got, ref, n, D, what=""):
-    out, mag, size = ref
-    most = 1.01 * (2.0 ** -16 + 2.0 ** -21 + 2 * n * 2.0 ** -24 + 2 * (D + 4) * 2.0 ** -24 * size[..., None]) * mag
+    out, mag, size, small = ref
+    w = 2.0 ** -11 if small.any() else 2.0 ** -16  # an 8-bit cache, or bf16
+    most = 1.01 * ((w + 2.0 ** -18 + 2 * n * 2.0 ** -24 + 2 * (D + 4) * 2.0 ** -24 * size[..., None]) * mag
+                   + 2.0 ** -25 * small)
     err = (got.cpu().double() - out).abs()
     bad = ~(err <= 2.0 ** -8 * out.abs() + most)
     assert not bool(bad.any()), f"{what}: {int(bad.sum())} values, first at {bad.nonzero()[0].tolist()}"

@@ -56,7 +56,7 @@ def test_one_draft_is_decode_attention(f8):
         kc, ke = draft.encode(a.k_cache)
         v, ve = draft.encode(a.v_cache.transpose(2, 3))
         vc, ex = v.transpose(2, 3), torch.stack([ke, ve], 2)
-    out, mag, _ = draft.attention_tree(a.q, kc, vc, ex, a.block_table, a.context_lens, list(range(5)))
+    out, mag, *_ = draft.attention_tree(a.q, kc, vc, ex, a.block_table, a.context_lens, list(range(5)))
     k, v = draft.held_pools(kc, vc, ex)
     ref = oracle.attention_decode(a.q, k, v, a.block_table, a.context_lens)
     assert torch.allclose(out, ref, rtol=1e-12, atol=1e-13) and bool((out.abs() <= mag * (1 + 1e-12)).all())
@@ -67,16 +67,16 @@ def test_a_chain_is_causal_attention():
     a = synth.custom_attention(4, 3, 4, 2, 64, lens, ctx_hi=32)
     p = synth.make_prefill(5, lens, 4, 2, 64)
     kc, vc = oracle.kv_write(a.k_cache, a.v_cache, a.block_table, a.context_lens, p.cu_seqlens, p.k, p.v)
-    out, _, _ = draft.attention_tree(p.q, kc, vc, None, a.block_table, a.context_lens, p.cu_seqlens.tolist())
+    out, *_ = draft.attention_tree(p.q, kc, vc, None, a.block_table, a.context_lens, p.cu_seqlens.tolist())
     assert torch.allclose(out, oracle.attention_prefill(p.q, p.k, p.v, p.cu_seqlens), rtol=1e-12, atol=1e-13)
     full = torch.full((23,), -1, dtype=torch.int64)
     one = aflex.tree_masks([list(range(-1, n - 1)) for n in lens])
-    got, _, _ = draft.attention_tree(p.q, kc, vc, None, a.block_table, a.context_lens, p.cu_seqlens.tolist(), one)
+    got, *_ = draft.attention_tree(p.q, kc, vc, None, a.block_table, a.context_lens, p.cu_seqlens.tolist(), one)
     assert torch.equal(got, out)
-    got, _, _ = draft.attention_tree(p.q, kc, vc, None, a.block_table, a.context_lens, p.cu_seqlens.tolist(), full)
+    got, *_ = draft.attention_tree(p.q, kc, vc, None, a.block_table, a.context_lens, p.cu_seqlens.tolist(), full)
     assert not torch.allclose(got, out)
-    none, _, size = draft.attention_tree(p.q, kc, vc, None, a.block_table, a.context_lens, p.cu_seqlens.tolist(), full * 0)
-    assert not none.any() and not size.any()
+    none, _, size, small = draft.attention_tree(p.q, kc, vc, None, a.block_table, a.context_lens, p.cu_seqlens.tolist(), full * 0)
+    assert not none.any() and not size.any() and not small.any()
 
 
 def test_masks_from_parents():
@@ -93,14 +93,14 @@ def test_a_branch_sees_what_its_chain_sees():
     parents = [-1, 0, 0, 1, 2, 4, -1]
     a = synth.custom_attention(6, 1, 4, 1, 64, [30], ctx_hi=32)
     q = torch.randn(7, 4, 64, generator=torch.Generator().manual_seed(1)).bfloat16()
-    out, _, _ = draft.attention_tree(q, a.k_cache, a.v_cache, None, a.block_table, a.context_lens, [0, 7],
+    out, *_ = draft.attention_tree(q, a.k_cache, a.v_cache, None, a.block_table, a.context_lens, [0, 7],
                                      aflex.tree_masks([parents]))
     for i, path in enumerate([[0], [0, 1], [0, 2], [0, 1, 3], [0, 2, 4], [0, 2, 4, 5], [6]]):
         kc, vc, _, ctx = draft.accept(a.k_cache, a.v_cache, None, a.block_table, a.context_lens, [0, 7],
                                       torch.tensor([path]), torch.tensor([len(path)]))
         n = len(path)
         assert int(ctx[0]) == 23 + n
-        one, _, _ = draft.attention_tree(q[path], kc, vc, None, a.block_table, ctx, [0, n])
+        one, *_ = draft.attention_tree(q[path], kc, vc, None, a.block_table, ctx, [0, n])
         assert torch.allclose(one[-1], out[i], rtol=1e-12, atol=1e-13)
 
 
