@@ -47,7 +47,7 @@ namespace aflex {
 namespace {
 
 constexpr int kRowWaves = 4;
-constexpr int kMostTiles = 3;  // row tiles of a wave (16 rows each)
+constexpr int kMostTiles = 2;  // row tiles of a wave (16 rows each)
 
 struct RowsParams {
   const uint16_t* q;
@@ -320,39 +320,79 @@ struct TwoWeights {
   }
 };
 
-// One row tile's softmax over NS slices of 8 tokens per lane: scores x (masked: -inf)
-// to weights, the running maximum m and sum l, and the accumulators' rescaling. F8:
-// ve and vinv are the tokens' value exponents and 2^-exponent.
-template <bool F8, int NS, int NMT, class Weights>
-__device__ __forceinline__ void softmax_step(f32x4 (&x)[2 * NS], const float (*ve)[8], const float (*vinv)[8],
-                                             float scale_log2, float& m, float& l, f32x4 (&acc)[NMT], Weights (&w)[NS]) {
+constexpr float kSlack = 8.f;
+
+// The softmax of N row tiles over NS slices of 8 tokens per lane: scores x (masked:
+// -inf) to weights, the running maxima m and sums l, and the accumulators' rescaling.
+// F8: ve holds the tokens' value exponents, a byte each with 128 added (in M' alone,
+// so it cancels), which joins a score by one conversion and its inverse the sum by one
+// shift.
+template <bool F8, int N, int NS, int NMT, class Weights>
+__device__ __forceinline__ void softmax_step(f32x4 (&x)[N][2 * NS], const u32x2 (&ve)[NS], float scale_log2,
+                                             float (&m)[N], float (&l)[N], f32x4 (&acc)[N][NMT], Weights (&w)[N][NS]) {
+  constexpr int E = 8 * NS;
+  const auto byte = [&](int e) { return ve[e / 8][(e / 4) & 1] >> (8 * (e & 3)) & 0xffu; };
   if constexpr (F8) {
 #pragma unroll
-    for (int e = 0; e < 8 * NS; ++e) x[e / 4][e & 3] = fmaf(x[e / 4][e & 3], scale_log2, ve[e / 8][e & 7]);
-  }
-  float mx = x[0][0];
+    for (int e = 0; e < E; ++e) {
+      const float v = (float)byte(e);
 #pragma unroll
-  for (int e = 1; e < 8 * NS; ++e) mx = fmaxf(mx, x[e / 4][e & 3]);
-  const float m_new = fmaxf(m, F8 ? row_max(mx) : row_max(mx) * scale_log2);
-  const float m_use = (m_new == kNegInf) ? 0.f : m_new;
-  if (!__all(m_new == m)) {
-    const float alpha = fast_exp2(m - m_use);
-    l *= alpha;
-#pragma unroll
-    for (int mt = 0; mt < NMT; ++mt) acc[mt] *= alpha;
-    m = m_new;
-  }
-#pragma unroll
-  for (int e = 0; e < 8 * NS; e += 2) {
-    float u[2];
-#pragma unroll
-    for (int i = 0; i < 2; ++i) {
-      const float s = x[(e + i) / 4][(e + i) & 3];
-      u[i] = fast_exp2(F8 ? s - m_use : fmaf(s, scale_log2, -m_use));
-      l = F8 ? fmaf(u[i], vinv[e / 8][(e + i) & 7], l) : l + u[i];
+      for (int t = 0; t < N; ++t) x[t][e / 4][e & 3] = fmaf(x[t][e / 4][e & 3], scale_log2, v);
     }
-    w[e / 8].set(e & 7, u[0], u[1]);
   }
+  // A row's reference m is its maximum when it was set last, and stays while no score
+  // is more than kSlack above it: weights are up to 2^kSlack then. So the hot path
+  // compares a lane's own scores alone, and the four lanes of a row exchange theirs
+  // where one is above.
+  bool above = false;
+  float mx[N];
+#pragma unroll
+  for (int t = 0; t < N; ++t) {
+    mx[t] = x[t][0][0];
+#pragma unroll
+    for (int e = 1; e < E; ++e) mx[t] = fmaxf(mx[t], x[t][e / 4][e & 3]);
+    if constexpr (!F8) mx[t] *= scale_log2;
+    above = above || mx[t] > m[t] + kSlack;
+  }
+  if (__any(above)) {
+#pragma unroll
+    for (int t = 0; t < N; ++t) {
+      const float m_new = fmaxf(m[t], row_max(mx[t]));
+      const float alpha = m_new == kNegInf ? 1.f : fast_exp2(m[t] - m_new);
+      l[t] *= alpha;
+#pragma unroll
+      for (int mt = 0; mt < NMT; ++mt) acc[t][mt] *= alpha;
+      m[t] = m_new;
+    }
+  }
+  float m_use[N];
+#pragma unroll
+  for (int t = 0; t < N; ++t) m_use[t] = m[t] == kNegInf ? 0.f : m[t];
+  float ps[N][2];
+#pragma unroll
+  for (int e = 0; e < E; e += 2) {
+    float inv[2];
+    if constexpr (F8) {
+#pragma unroll
+      for (int i = 0; i < 2; ++i) inv[i] = __uint_as_float((255u - byte(e + i)) << 23);  // 2^-exponent
+    }
+#pragma unroll
+    for (int t = 0; t < N; ++t) {
+      float u[2];
+#pragma unroll
+      for (int i = 0; i < 2; ++i) {
+        const float s = x[t][(e + i) / 4][(e + i) & 3];
+        u[i] = fast_exp2(F8 ? s - m_use[t] : fmaf(s, scale_log2, -m_use[t]));
+        if constexpr (F8)
+          ps[t][i] = e == 0 ? u[i] * inv[i] : fmaf(u[i], inv[i], ps[t][i]);
+        else
+          ps[t][i] = e == 0 ? u[i] : ps[t][i] + u[i];
+      }
+      w[t][e / 8].set(e & 7, u[0], u[1]);
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < N; ++t) l[t] += ps[t][0] + ps[t][1];
 }
 
 // Block ids of a piece by scalar loads: raw ones are fetched a step ahead, and become
@@ -387,6 +427,7 @@ struct BlockIds {
       id3 = fine(raw3, j + 3);
     }
   }
+  __device__ __forceinline__ bool all_fine() const { return (id0 | id1 | (NB == 4 ? id2 | id3 : 0)) >= 0; }
   __device__ __forceinline__ int pick(int i) const {
     const int low = (i & 1) ? id1 : id0;
     if constexpr (NB == 4) return (i & 2) ? ((i & 1) ? id3 : id2) : low;
@@ -394,10 +435,15 @@ struct BlockIds {
   }
 };
 
+// Waits for the global loads so far. In front of a loop whose loads run a step ahead:
+// what the loop only reads (the queries) would else be waited for inside it, each time
+// with the loads of the next step.
+__device__ __forceinline__ void wait_for_loads() { __builtin_amdgcn_s_waitcnt(0x0f70); }  // vmcnt(0)
+
 constexpr int few_per_cu(int D) { return D == 64 ? 3 : 2; }
 
-// Work-groups that a CU holds at once (by registers and LDS).
-constexpr int many_per_cu(int tiles) { return tiles == 1 ? 3 : 2; }
+// Work-groups that a CU holds at once (by registers).
+constexpr int kManyPerCu = 2;
 
 }  // namespace
 
@@ -442,7 +488,7 @@ __global__ __launch_bounds__(64 * kRowWaves, few_per_cu(D)) void attn_few_kernel
 
     u32x4 kraw[NK];  // (8-bit codes come 16 channels a load, and the k-chunks take the channels in that order)
     VLoad vraw[NMT];
-    u32x2 kx, vx;    // exponents of the 8 tokens around the lane's key rows, and of its values
+    u32x2 kx = {0, 0}, vx = {0, 0};  // exponents of the 8 tokens around the lane's key rows, and of its values
     int tb = 0, nv = 0, jb = 0;  // place of the lane's first token, how many of them are cached; first block
     // (blocks that do not exist are read at block 0 and masked)
     auto load_keys = [&]() __attribute__((always_inline)) {
@@ -491,14 +537,15 @@ __global__ __launch_bounds__(64 * kRowWaves, few_per_cu(D)) void attn_few_kernel
     for (int i = 0; i < NC; ++i)
       qf[i] = r < c.rows ? ld_bf16x8(qrow + (F8 ? (i >> 1) * 64 + qg * 16 + (i & 1) * 8 : i * 32 + qg * 8)) : zero_bf16x8();
 
-    float m_run = kNegInf, l_run = 0.f;
-    f32x4 acc[NMT];
+    float m_run[1] = {kNegInf}, l_run[1] = {0.f};
+    f32x4 acc[1][NMT];
 #pragma unroll
-    for (int mt = 0; mt < NMT; ++mt) acc[mt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int mt = 0; mt < NMT; ++mt) acc[0][mt] = f32x4{0.f, 0.f, 0.f, 0.f};
 
+    wait_for_loads();
     for (; st < steps; st += kRowWaves) {
       const int next = st + kRowWaves < steps ? st + kRowWaves : st;  // (the last step's loads are repeated)
-      f32x4 sc[2] = {f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}};
+      f32x4 sc[1][2] = {{f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}}};
 #pragma unroll
       for (int t = 0; t < 2; ++t) {
         bf16x8 kf[NC];
@@ -515,7 +562,7 @@ __global__ __launch_bounds__(64 * kRowWaves, few_per_cu(D)) void attn_few_kernel
           for (int i = 0; i < NC; ++i) kf[i] = __builtin_bit_cast(bf16x8, kraw[t * NC + i]);
         }
 #pragma unroll
-        for (int i = 0; i < NC; ++i) sc[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[i], qf[i], sc[t], 0, 0, 0);
+        for (int i = 0; i < NC; ++i) sc[0][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[i], qf[i], sc[0][t], 0, 0, 0);
       }
       // (nothing moves across: the loads take the registers that the keys leave)
       __builtin_amdgcn_sched_barrier(0);
@@ -528,64 +575,56 @@ __global__ __launch_bounds__(64 * kRowWaves, few_per_cu(D)) void attn_few_kernel
       if (!((jb_now + 2) * 16 <= start && __all(nv_now >= 8))) {  // drafts, or places that hold nothing
         const uint32_t seen = seen_bits(mask, tb_now, start, nv_now);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sc[e / 4][e & 3] = (seen >> e & 1u) ? sc[e / 4][e & 3] : kNegInf;
+        for (int e = 0; e < 8; ++e) sc[0][e / 4][e & 3] = (seen >> e & 1u) ? sc[0][e / 4][e & 3] : kNegInf;
         // zeros behind the context, so that 0 times what lies there is 0
 #pragma unroll
         for (int mt = 0; mt < NMT; ++mt) vraw[mt] = keep_bytes(vraw[mt], F8 ? nv_now : 2 * nv_now);
         if constexpr (F8) vx = keep_bytes(vx, nv_now);
       }
-      float ve[1][8], vinv[1][8];
-      if constexpr (F8) {
-#pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const int v = (int8_t)(vx[e / 4] >> (8 * (e & 3)));
-          ve[0][e] = (float)v;
-          vinv[0][e] = exp2_whole(-v);
-        }
-      }
-      Weights w[1];
-      softmax_step<F8, 1>(sc, ve, vinv, p.scale_log2, m_run, l_run, acc, w);
+      const u32x2 ve[1] = {F8 ? vx ^ 0x80808080u : vx};
+      Weights w[1][1];
+      softmax_step<F8, 1, 1>(sc, ve, p.scale_log2, m_run, l_run, acc, w);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int mt = 0; mt < NMT; ++mt) {
         if constexpr (F8)
-          acc[mt] = w[0].mul(widen_f16(vraw[mt][0], vraw[mt][1]), acc[mt]);
+          acc[0][mt] = w[0][0].mul(widen_f16(vraw[mt][0], vraw[mt][1]), acc[0][mt]);
         else
-          acc[mt] = w[0].mul(__builtin_bit_cast(bf16x8, vraw[mt]), acc[mt]);
+          acc[0][mt] = w[0][0].mul(__builtin_bit_cast(bf16x8, vraw[mt]), acc[0][mt]);
       }
       __builtin_amdgcn_sched_barrier(0);
       load_values(next);
     }
 
     // ---- merge the waves, in a fixed order: the upper half deposits, the lower adds ----
-    l_run += __shfl_xor(l_run, 16);
-    l_run += __shfl_xor(l_run, 32);
+    l_run[0] += __shfl_xor(l_run[0], 16);
+    l_run[0] += __shfl_xor(l_run[0], 32);
 #pragma unroll
     for (int half = kRowWaves / 2; half >= 1; half /= 2) {
       float* o = so + ((wave % half) * 16 + r) * LDO;
       __syncthreads();
       if (wave >= half && wave < 2 * half) {
 #pragma unroll
-        for (int mt = 0; mt < NMT; ++mt) *reinterpret_cast<f32x4*>(o + mt * 16 + 4 * qg) = acc[mt];
-        if (qg == 0) *reinterpret_cast<float2*>(o + D) = make_float2(m_run, l_run);
+        for (int mt = 0; mt < NMT; ++mt) *reinterpret_cast<f32x4*>(o + mt * 16 + 4 * qg) = acc[0][mt];
+        if (qg == 0) *reinterpret_cast<float2*>(o + D) = make_float2(m_run[0], l_run[0]);
       }
       __syncthreads();
       if (wave < half) {
         const float2 ml = *reinterpret_cast<const float2*>(o + D);
-        const float mn = fmaxf(m_run, ml.x);
+        const float mn = fmaxf(m_run[0], ml.x);
         const float mu = (mn == kNegInf) ? 0.f : mn;
-        const float wa = fast_exp2(m_run - mu), wb = fast_exp2(ml.x - mu);
-        l_run = l_run * wa + ml.y * wb;
-        m_run = mn;
+        const float wa = fast_exp2(m_run[0] - mu), wb = fast_exp2(ml.x - mu);
+        l_run[0] = l_run[0] * wa + ml.y * wb;
+        m_run[0] = mn;
 #pragma unroll
         for (int mt = 0; mt < NMT; ++mt)
-          acc[mt] = acc[mt] * wa + *reinterpret_cast<const f32x4*>(o + mt * 16 + 4 * qg) * wb;
+          acc[0][mt] = acc[0][mt] * wa + *reinterpret_cast<const f32x4*>(o + mt * 16 + 4 * qg) * wb;
       }
     }
     if (wave == 0) {
       if (lane == 0 && (int)blockIdx.x == c.first)
         p.span[((size_t)b * p.Hkv + c.kvh) * p.max_passes + c.pass] = make_int2(c.first, c.last);
-      store_rows<D>(p, s, c, c.row0 + r, qg, m_run, l_run, acc);
+      store_rows<D>(p, s, c, c.row0 + r, qg, m_run[0], l_run[0], acc[0]);
     }
   }
 }
@@ -601,19 +640,24 @@ __device__ __forceinline__ void lds_barrier() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
-template <int D, bool F8, int RT>
-__global__ __launch_bounds__(64 * kRowWaves, many_per_cu(RT)) void attn_many_kernel(RowsParams p) {
+template <int D, bool F8, int WR, int RT>
+__global__ __launch_bounds__(64 * kRowWaves, kManyPerCu) void attn_many_kernel(RowsParams p) {
   constexpr int NC = D / 32, NMT = D / 16;
   constexpr int ES = F8 ? 1 : 2;
   constexpr int CPB = D * ES;                     // 16-byte chunks of a block's K (and V) tile
   constexpr int NL = 4 * CPB / (64 * kRowWaves);  // those of a thread, 4 blocks
   constexpr int LDK = D + 8, LDV = 64 + 8;        // padded rows in LDS (16-bit elements)
-  constexpr int NS = RT == 3 ? 1 : 2;             // 32-token slices per softmax step
+  constexpr int LDO = D + 4;                      // row of a partial in LDS: O, then (m, l)
+  constexpr int TS = kRowWaves / WR;              // waves that share a step's tokens
+  constexpr int NS = 1;       // 32-token slices per softmax step
   typedef std::conditional_t<F8, HalfWeights, TwoWeights> Weights;
   typedef std::conditional_t<F8, f16x8, bf16x8> VFrag;
-  __shared__ __attribute__((aligned(16))) uint16_t sk[64 * LDK];
-  __shared__ __attribute__((aligned(16))) uint16_t sv[D * LDV];
-  __shared__ __attribute__((aligned(16))) float sx[2][F8 ? 64 : 1];  // the values' exponents, and 2^-exponent
+  constexpr int kTileBytes = (64 * LDK + D * LDV) * 2, kPartBytes = TS == 2 ? WR * RT * 16 * LDO * 4 : 0;
+  __shared__ __attribute__((aligned(16))) uint8_t sm[kTileBytes > kPartBytes ? kTileBytes : kPartBytes];
+  __shared__ __attribute__((aligned(16))) uint8_t sx[F8 ? 64 : 8];  // the values' exponents, 128 added
+  uint16_t* sk = reinterpret_cast<uint16_t*>(sm);
+  uint16_t* sv = sk + 64 * LDK;
+  float* so = reinterpret_cast<float*>(sm);
 
   const int tid = threadIdx.x;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -637,77 +681,100 @@ __global__ __launch_bounds__(64 * kRowWaves, many_per_cu(RT)) void attn_many_ker
     if (c.j1 <= c.j0) break;
     const int start = s.ctx - s.n;  // place of the first draft
     const int steps = (c.j1 - c.j0 + 3) / 4;
-    const int per_wave = (c.tiles + kRowWaves - 1) / kRowWaves;
-    const int t0 = wave * per_wave, mine = max(min(c.tiles - t0, per_wave), 0);
-    BlockIds<4> ids(p, b, c.j0, c.j1);
+    // the wave's row tiles
+    const int per_wave = (c.tiles + WR - 1) / WR;
+    const int group = wave % WR, half = wave / WR;
+    const int t0 = group * per_wave, mine = max(min(c.tiles - t0, per_wave), 0);
+    // Block ids by vector loads, 64 a register and the next 64 ahead (scalar loads share
+    // the counter of the LDS's, so that every barrier would wait for them). -1: no such
+    // block. (Plain variables: a struct of them stayed in memory.)
+    const int32_t* table = p.bt + (size_t)b * p.max_blocks;
+    auto load_id = [&](int j) __attribute__((always_inline)) { return table[min(j, c.j1 - 1)]; };
+    int ids_now = load_id(c.j0 + lane), ids_next = load_id(c.j0 + 64 + lane), chunk = 0;
+    int id0 = -1, id1 = -1, id2 = -1, id3 = -1;
+    auto take_ids = [&](int st) __attribute__((always_inline)) {
+      const int at = st * 4;
+      if (at >> 6 != chunk) {  // (steps come one by one)
+        chunk = at >> 6;
+        ids_now = ids_next;
+        ids_next = load_id(c.j0 + (chunk + 1) * 64 + lane);
+      }
+      const auto id_at = [&](int i) {
+        const int id = __builtin_amdgcn_readlane(ids_now, (at & 63) + i);
+        return (uint32_t)id < (uint32_t)p.num_blocks && c.j0 + at + i < c.j1 ? id : -1;
+      };
+      id0 = id_at(0);
+      id1 = id_at(1);
+      id2 = id_at(2);
+      id3 = id_at(3);
+    };
+    auto pick = [&](int i) __attribute__((always_inline)) {
+      const int low = (i & 1) ? id1 : id0, high = (i & 1) ? id3 : id2;
+      return (i & 2) ? high : low;
+    };
 
     // ---- a step's chunks: chunk i of the thread lies in block blk(i), the wave's ----
     u32x4 kraw[NL], vraw[NL];
     uint32_t kx[NL];
-    int vx = 0;
+    int vx[NL];
     auto blk = [&](int i) __attribute__((always_inline)) { return (i * kRowWaves + wave) * 64 / CPB; };
     auto within = [&](int i) __attribute__((always_inline)) { return (i * 64 * kRowWaves + tid) % CPB; };
+    auto heads_block = [&](int i) __attribute__((always_inline)) { return (i * kRowWaves + wave) * 64 % CPB == 0; };
     auto load = [&]() __attribute__((always_inline)) {
 #pragma unroll
       for (int i = 0; i < NL; ++i) {
-        const size_t tile = (size_t)max(ids.pick(blk(i)), 0) * p.Hkv + c.kvh;
-        const size_t at = tile * (16 * D * ES) + within(i) * 16;
-        kraw[i] = stream<u32x4>(p.kc + at);
-        vraw[i] = stream<u32x4>(p.vc + at);
-        if constexpr (F8) kx[i] = *reinterpret_cast<const uint32_t*>(p.ke + tile * 32 + (within(i) / (D / 16) & 12));
-      }
-      if constexpr (F8) {
-        if (wave == 0) {
-          const size_t tile = (size_t)max(ids.pick(lane >> 4), 0) * p.Hkv + c.kvh;
-          vx = p.ke[tile * 32 + 16 + (lane & 15)];
+        const size_t tile = (size_t)max(pick(blk(i)), 0) * p.Hkv + c.kvh;
+        // (a scalar base and an offset of 32 bits per lane)
+        const uint8_t *kb = p.kc + tile * (16 * D * ES), *vb = p.vc + tile * (16 * D * ES);
+        const uint32_t off = within(i) * 16;
+        kraw[i] = stream<u32x4>(kb + off);
+        vraw[i] = stream<u32x4>(vb + off);
+        if constexpr (F8) {
+          const int8_t* eb = p.ke + tile * 32;
+          kx[i] = *reinterpret_cast<const uint32_t*>(eb + (uint32_t)(within(i) / (D / 16) & 12));
+          if (heads_block(i)) vx[i] = eb[(uint32_t)(16 + (lane & 15))];
         }
       }
     };
     // (n0 .. n3: cached tokens of the blocks; zeros behind them, so that 0 times what lies there is 0)
-    auto store = [&](int n0, int n1, int n2, int n3) __attribute__((always_inline)) {
+    auto store = [&](bool full, int n0, int n1, int n2, int n3) __attribute__((always_inline)) {
 #pragma unroll
       for (int i = 0; i < NL; ++i) {
         const int k = blk(i), w = within(i);
-        const int nv = k == 0 ? n0 : k == 1 ? n1 : k == 2 ? n2 : n3;  // cached tokens of the block
         const int o = w / (D * ES / 16), u = (k & 1) * 16 + o;
         uint16_t* kd = sk + ((k >> 1) * 32 + ((u >> 2) & 1) * 16 + (u >> 3) * 4 + (u & 3)) * LDK +
                        (w % (D * ES / 16)) * (16 / ES);
-        u32x4 v = vraw[i];
+        if (!full) {
+          const int nv = k == 0 ? n0 : k == 1 ? n1 : k == 2 ? n2 : n3;
+          vraw[i] = keep_bytes(vraw[i], F8 ? nv : 2 * (nv - (w & 1) * 8));
+          if constexpr (F8) vx[i] = (lane & 15) < nv ? vx[i] : 0;
+        }
+        const u32x4 v = vraw[i];
         if constexpr (F8) {
-          if (nv < 16) v = keep_bytes(v, nv);
           const float f = exp2_whole((int8_t)(kx[i] >> (8 * (o & 3))));
           *reinterpret_cast<bf16x8*>(kd) = widen_bf16(kraw[i][0], kraw[i][1], f);
           *reinterpret_cast<bf16x8*>(kd + 8) = widen_bf16(kraw[i][2], kraw[i][3], f);
           uint16_t* vd = sv + w * LDV + k * 16;
           *reinterpret_cast<f16x8*>(vd) = widen_f16(v[0], v[1]);
           *reinterpret_cast<f16x8*>(vd + 8) = widen_f16(v[2], v[3]);
+          if (heads_block(i) && lane < 16) sx[k * 16 + lane] = (uint8_t)(vx[i] + 128);
         } else {
-          if (nv < 16) v = keep_bytes(v, 2 * (nv - (w & 1) * 8));
           *reinterpret_cast<u32x4*>(kd) = kraw[i];
           *reinterpret_cast<u32x4*>(sv + (w >> 1) * LDV + k * 16 + (w & 1) * 8) = v;
         }
       }
-      if constexpr (F8) {
-        if (wave == 0) {
-          const int i = lane >> 4, nv = i == 0 ? n0 : i == 1 ? n1 : i == 2 ? n2 : n3;
-          const int v = (lane & 15) < nv ? vx : 0;
-          sx[0][lane] = (float)v;
-          sx[1][lane] = exp2_whole(-v);
-        }
-      }
     };
 
-    ids.fetch(0);
-    ids.take(0);
+    take_ids(0);
     load();
-    ids.fetch(min(1, steps - 1));
 
     auto run_steps = [&](auto count) __attribute__((always_inline)) {
       constexpr int N = decltype(count)::value;
-      bf16x8 qf[N > 0 ? N : 1][NC];
-      uint64_t mask[N > 0 ? N : 1];
-      float m_run[N > 0 ? N : 1], l_run[N > 0 ? N : 1];
-      f32x4 acc[N > 0 ? N : 1][NMT];
+      constexpr int N1 = N > 0 ? N : 1;
+      bf16x8 qf[N1][NC];
+      uint64_t mask[N1];
+      float m_run[N1], l_run[N1];
+      f32x4 acc[N1][NMT];
 #pragma unroll
       for (int t = 0; t < N; ++t) {
         const int row = (t0 + t) * 16 + r;
@@ -721,36 +788,70 @@ __global__ __launch_bounds__(64 * kRowWaves, many_per_cu(RT)) void attn_many_ker
 #pragma unroll
         for (int mt = 0; mt < NMT; ++mt) acc[t][mt] = f32x4{0.f, 0.f, 0.f, 0.f};
       }
+      wait_for_loads();
       for (int st = 0; st < steps; ++st) {
         const int jb = c.j0 + st * 4;
-        const auto cached = [&](int id, int i) { return id >= 0 ? min(max(s.ctx - (jb + i) * 16, 0), 16) : 0; };
-        const int n0 = cached(ids.id0, 0), n1 = cached(ids.id1, 1), n2 = cached(ids.id2, 2), n3 = cached(ids.id3, 3);
+        const bool full = (jb + 4) * 16 <= s.ctx && (id0 | id1 | id2 | id3) >= 0;
+        int n0 = 16, n1 = 16, n2 = 16, n3 = 16;
+        if (!full) {
+          const auto cached = [&](int id, int i) { return id >= 0 ? min(max(s.ctx - (jb + i) * 16, 0), 16) : 0; };
+          n0 = cached(id0, 0), n1 = cached(id1, 1), n2 = cached(id2, 2), n3 = cached(id3, 3);
+        }
         lds_barrier();  // every wave is done with the step before
-        store(n0, n1, n2, n3);
+        store(full, n0, n1, n2, n3);
         if (st + 1 < steps) {
-          ids.take(st + 1);
+          take_ids(st + 1);
           load();
-          ids.fetch(min(st + 2, steps - 1));
         }
         lds_barrier();
         if constexpr (N > 0) {
-          const bool whole = (jb + 4) * 16 <= start && n0 + n1 + n2 + n3 == 64;
+          const bool whole = full && (jb + 4) * 16 <= start;
 #pragma unroll
-          for (int h = 0; h < 2 / NS; ++h) {
+          for (int part = 0; part < 2 / NS / TS; ++part) {
+            const int h = TS == 2 ? half : part;  // slices h NS ..
             f32x4 sc[N][2 * NS];
 #pragma unroll
             for (int t = 0; t < N; ++t)
 #pragma unroll
               for (int k = 0; k < 2 * NS; ++k) sc[t][k] = f32x4{0.f, 0.f, 0.f, 0.f};
+            // (8-bit cache: all of a product's operands are read before it starts, the values'
+            // before the softmax. A bf16 step ahead takes twice the registers and leaves none
+            // for that.)
+            u32x2 ve[NS];
+#pragma unroll
+            for (int k = 0; k < NS; ++k)
+              ve[k] = F8 ? *reinterpret_cast<const u32x2*>(sx + (h * NS + k) * 32 + qg * 8) : u32x2{0, 0};
+            auto key = [&](int k, int i) __attribute__((always_inline)) {
+              return ld_bf16x8(sk + ((h * 2 * NS + k) * 16 + r) * LDK + i * 32 + qg * 8);
+            };
+            auto value = [&](int k, int mt) __attribute__((always_inline)) {
+              return *reinterpret_cast<const VFrag*>(sv + (mt * 16 + r) * LDV + (h * NS + k) * 32 + qg * 8);
+            };
+            bf16x8 kf[2 * NS][NC];
+            VFrag vf[NS][NMT];
+            if constexpr (F8) {
+#pragma unroll
+              for (int k = 0; k < 2 * NS; ++k)
+#pragma unroll
+                for (int i = 0; i < NC; ++i) kf[k][i] = key(k, i);
+              __builtin_amdgcn_sched_barrier(0);
+            }
 #pragma unroll
             for (int k = 0; k < 2 * NS; ++k)
 #pragma unroll
               for (int i = 0; i < NC; ++i) {
-                const bf16x8 kf = ld_bf16x8(sk + ((h * 2 * NS + k) * 16 + r) * LDK + i * 32 + qg * 8);
+                if constexpr (!F8) kf[k][i] = key(k, i);
 #pragma unroll
                 for (int t = 0; t < N; ++t)
-                  sc[t][k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf, qf[t][i], sc[t][k], 0, 0, 0);
+                  sc[t][k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[k][i], qf[t][i], sc[t][k], 0, 0, 0);
               }
+            if constexpr (F8) {
+#pragma unroll
+              for (int mt = 0; mt < NMT; ++mt)
+#pragma unroll
+                for (int k = 0; k < NS; ++k) vf[k][mt] = value(k, mt);
+              __builtin_amdgcn_sched_barrier(0);
+            }
             if (!whole) {
 #pragma unroll
               for (int k = 0; k < NS; ++k) {
@@ -766,30 +867,15 @@ __global__ __launch_bounds__(64 * kRowWaves, many_per_cu(RT)) void attn_many_ker
                 }
               }
             }
-            float ve[NS][8], vinv[NS][8];
-            if constexpr (F8) {
-#pragma unroll
-              for (int k = 0; k < NS; ++k)
-#pragma unroll
-                for (int e = 0; e < 8; e += 4) {
-                  const int at = (h * NS + k) * 32 + qg * 8 + e;
-                  const f32x4 a = *reinterpret_cast<const f32x4*>(&sx[0][at]);
-                  const f32x4 d = *reinterpret_cast<const f32x4*>(&sx[1][at]);
-#pragma unroll
-                  for (int i = 0; i < 4; ++i) ve[k][e + i] = a[i], vinv[k][e + i] = d[i];
-                }
-            }
             Weights w[N][NS];
-#pragma unroll
-            for (int t = 0; t < N; ++t)
-              softmax_step<F8, NS>(sc[t], ve, vinv, p.scale_log2, m_run[t], l_run[t], acc[t], w[t]);
+            softmax_step<F8, N, NS>(sc, ve, p.scale_log2, m_run, l_run, acc, w);
 #pragma unroll
             for (int mt = 0; mt < NMT; ++mt)
 #pragma unroll
               for (int k = 0; k < NS; ++k) {
-                const VFrag vf = *reinterpret_cast<const VFrag*>(sv + (mt * 16 + r) * LDV + (h * NS + k) * 32 + qg * 8);
+                if constexpr (!F8) vf[k][mt] = value(k, mt);
 #pragma unroll
-                for (int t = 0; t < N; ++t) acc[t][mt] = w[t][k].mul(vf, acc[t][mt]);
+                for (int t = 0; t < N; ++t) acc[t][mt] = w[t][k].mul(vf[k][mt], acc[t][mt]);
               }
           }
         }
@@ -798,7 +884,39 @@ __global__ __launch_bounds__(64 * kRowWaves, many_per_cu(RT)) void attn_many_ker
       for (int t = 0; t < N; ++t) {
         l_run[t] += __shfl_xor(l_run[t], 16);
         l_run[t] += __shfl_xor(l_run[t], 32);
-        store_rows<D>(p, s, c, c.row0 + (t0 + t) * 16 + r, qg, m_run[t], l_run[t], acc[t]);
+      }
+      if constexpr (TS == 2) {  // the second half's waves deposit, the first half's add
+        lds_barrier();
+        if (half == 1) {
+#pragma unroll
+          for (int t = 0; t < N; ++t) {
+            float* o = so + ((group * RT + t) * 16 + r) * LDO;
+#pragma unroll
+            for (int mt = 0; mt < NMT; ++mt) *reinterpret_cast<f32x4*>(o + mt * 16 + 4 * qg) = acc[t][mt];
+            if (qg == 0) *reinterpret_cast<float2*>(o + D) = make_float2(m_run[t], l_run[t]);
+          }
+        }
+        lds_barrier();
+        if (half == 0) {
+#pragma unroll
+          for (int t = 0; t < N; ++t) {
+            const float* o = so + ((group * RT + t) * 16 + r) * LDO;
+            const float2 ml = *reinterpret_cast<const float2*>(o + D);
+            const float mn = fmaxf(m_run[t], ml.x);
+            const float mu = (mn == kNegInf) ? 0.f : mn;
+            const float wa = fast_exp2(m_run[t] - mu), wb = fast_exp2(ml.x - mu);
+            l_run[t] = l_run[t] * wa + ml.y * wb;
+            m_run[t] = mn;
+#pragma unroll
+            for (int mt = 0; mt < NMT; ++mt)
+              acc[t][mt] = acc[t][mt] * wa + *reinterpret_cast<const f32x4*>(o + mt * 16 + 4 * qg) * wb;
+          }
+        }
+      }
+      if (half == 0) {
+#pragma unroll
+        for (int t = 0; t < N; ++t)
+          store_rows<D>(p, s, c, c.row0 + (t0 + t) * 16 + r, qg, m_run[t], l_run[t], acc[t]);
       }
     };
     if (mine == 0) run_steps(std::integral_constant<int, 0>{});
@@ -870,7 +988,8 @@ __global__ __launch_bounds__(256) void attn_rows_merge_kernel(RowsParams p) {
 // Host side.
 namespace {
 
-// What a launch takes: row tiles of a wave (0: the kernel for up to 16 rows).
+// What a launch takes: row tiles of a wave (0: the kernel for up to 16 rows; 1: up to
+// 64 rows, two tiles of a half of the tokens).
 struct RowsPlan {
   int tiles, pass_tiles, passes, pass_rows, grid;
 };
@@ -901,7 +1020,7 @@ RowsPlan rows_plan(const RowsShape& s) {
   r.pass_tiles = r.tiles == 0 ? 1 : r.tiles * kRowWaves;
   r.passes = all > r.pass_tiles ? (all + r.pass_tiles - 1) / r.pass_tiles : 1;
   r.pass_rows = rows < r.pass_tiles * 16 ? rows : r.pass_tiles * 16;
-  const long long most = (long long)compute_units() * (r.tiles == 0 ? few_per_cu(s.D) : many_per_cu(r.tiles));
+  const long long most = (long long)compute_units() * (r.tiles == 0 ? few_per_cu(s.D) : kManyPerCu);
   const long long P = (positions_bound(s, r.passes) + 7) / 8;
   r.grid = (int)(P < 1 ? 1 : P < most ? P : most);
   return r;
@@ -915,11 +1034,11 @@ void launch_tiles(const RowsParams& p, const RowsPlan& r, hipStream_t stream) {
   if (r.tiles == 0)
     attn_few_kernel<D, F8><<<grid, block, 0, stream>>>(p);
   else if (r.tiles == 1)
-    attn_many_kernel<D, F8, 1><<<grid, block, 0, stream>>>(p);
+    attn_many_kernel<D, F8, 2, 2><<<grid, block, 0, stream>>>(p);
   else if (r.tiles == 2)
-    attn_many_kernel<D, F8, 2><<<grid, block, 0, stream>>>(p);
+    attn_many_kernel<D, F8, 4, 2><<<grid, block, 0, stream>>>(p);
   else
-    attn_many_kernel<D, F8, 3><<<grid, block, 0, stream>>>(p);
+    attn_many_kernel<D, F8, 4, 3><<<grid, block, 0, stream>>>(p);
 }
 
 }  // namespace
