@@ -67,6 +67,7 @@ struct RowsParams {
   int pass_tiles;           // row tiles that one pass takes
   int max_blocks, num_blocks, max_ctx;
   int unit_cost;
+  int whole;                // a work-group per unit: a position each
   float scale_log2;
 };
 
@@ -105,8 +106,10 @@ __device__ __forceinline__ Seq seq_of(const RowsParams& p, int b) {
 }
 
 // Positions of a unit in the flattened range: its blocks, and a charge for the
-// piece it adds.
-__device__ __forceinline__ int unit_len(const RowsParams& p, const Seq& s) { return ((s.ctx + 15) >> 4) + p.unit_cost; }
+// piece it adds; or one.
+__device__ __forceinline__ int unit_len(const RowsParams& p, const Seq& s) {
+  return p.whole ? 1 : ((s.ctx + 15) >> 4) + p.unit_cost;
+}
 
 __device__ __forceinline__ int seq_len(const RowsParams& p, int b) {
   if (b >= p.B) return 0;
@@ -136,7 +139,7 @@ __device__ __forceinline__ bool find_range(const RowsParams& p, int least, int l
   const int P = gridDim.x, wg = blockIdx.x;
   int total = 0;
   for (int c = 0; c < p.B; c += 64) total += sum64(seq_len(p, c + lane));
-  per = max((total + P - 1) / P, least);
+  per = p.whole ? 1 : max((total + P - 1) / P, least);
   const long long xs = (long long)wg * per;
   if (xs >= total) return false;
   x0 = (int)xs;
@@ -172,15 +175,22 @@ __device__ __forceinline__ Piece piece_at(const RowsParams& p, const Seq& s, int
   const int len = unit_len(p, s), unit = (x - base) / len;
   c.kvh = unit / s.passes;
   c.pass = unit - c.kvh * s.passes;
-  const int ustart = base + unit * len + p.unit_cost, nb = len - p.unit_cost;
-  c.j0 = max(x - ustart, 0);
-  c.j1 = min(nb, x1 - ustart);  // (j0 or less where the range ends inside the unit's charge)
-  c.first = ustart / per;
-  c.last = (ustart + nb - 1) / per;
+  if (p.whole) {
+    c.j0 = 0;
+    c.j1 = (s.ctx + 15) >> 4;
+    c.first = c.last = blockIdx.x;
+    xn = x1;
+  } else {
+    const int ustart = base + unit * len + p.unit_cost, nb = len - p.unit_cost;
+    c.j0 = max(x - ustart, 0);
+    c.j1 = min(nb, x1 - ustart);  // (j0 or less where the range ends inside the unit's charge)
+    c.first = ustart / per;
+    c.last = (ustart + nb - 1) / per;
+    xn = min(ustart + nb, x1);
+  }
   c.row0 = c.pass * s.tiles * 16;
   c.rows = min(s.take * p.G - c.row0, s.tiles * 16);
   c.tiles = (c.rows + 15) >> 4;
-  xn = min(ustart + nb, x1);
   return c;
 }
 
@@ -300,7 +310,8 @@ struct HalfWeights {
     w[i] = static_cast<_Float16>(a);
     w[i + 1] = static_cast<_Float16>(b);
   }
-  __device__ __forceinline__ f32x4 mul(f16x8 v, f32x4 acc) const {
+  static constexpr int kParts = 1;
+  __device__ __forceinline__ f32x4 mul(int, f16x8 v, f32x4 acc) const {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(v, w, acc, 0, 0, 0);
   }
 };
@@ -314,9 +325,9 @@ struct TwoWeights {
     lo[i / 2] = __builtin_bit_cast(uint32_t, bf16x2{static_cast<__bf16>(a - __uint_as_float(h << 16)),
                                                     static_cast<__bf16>(b - __uint_as_float(h & 0xffff0000u))});
   }
-  __device__ __forceinline__ f32x4 mul(bf16x8 v, f32x4 acc) const {
-    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, __builtin_bit_cast(bf16x8, hi), acc, 0, 0, 0);
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, __builtin_bit_cast(bf16x8, lo), acc, 0, 0, 0);
+  static constexpr int kParts = 2;
+  __device__ __forceinline__ f32x4 mul(int part, bf16x8 v, f32x4 acc) const {
+    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, __builtin_bit_cast(bf16x8, part ? lo : hi), acc, 0, 0, 0);
   }
 };
 
@@ -586,12 +597,14 @@ __global__ __launch_bounds__(64 * kRowWaves, few_per_cu(D)) void attn_few_kernel
       softmax_step<F8, 1, 1>(sc, ve, p.scale_log2, m_run, l_run, acc, w);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
-      for (int mt = 0; mt < NMT; ++mt) {
-        if constexpr (F8)
-          acc[0][mt] = w[0][0].mul(widen_f16(vraw[mt][0], vraw[mt][1]), acc[0][mt]);
-        else
-          acc[0][mt] = w[0][0].mul(__builtin_bit_cast(bf16x8, vraw[mt]), acc[0][mt]);
-      }
+      for (int part = 0; part < Weights::kParts; ++part)
+#pragma unroll
+        for (int mt = 0; mt < NMT; ++mt) {
+          if constexpr (F8)
+            acc[0][mt] = w[0][0].mul(part, widen_f16(vraw[mt][0], vraw[mt][1]), acc[0][mt]);
+          else
+            acc[0][mt] = w[0][0].mul(part, __builtin_bit_cast(bf16x8, vraw[mt]), acc[0][mt]);
+        }
       __builtin_amdgcn_sched_barrier(0);
       load_values(next);
     }
@@ -837,14 +850,17 @@ __global__ __launch_bounds__(64 * kRowWaves, kManyPerCu) void attn_many_kernel(R
               __builtin_amdgcn_sched_barrier(0);
             }
 #pragma unroll
-            for (int k = 0; k < 2 * NS; ++k)
+            for (int i = 0; i < NC; ++i) {
+              if constexpr (!F8) {
 #pragma unroll
-              for (int i = 0; i < NC; ++i) {
-                if constexpr (!F8) kf[k][i] = key(k, i);
+                for (int k = 0; k < 2 * NS; ++k) kf[k][i] = key(k, i);
+              }
+#pragma unroll
+              for (int k = 0; k < 2 * NS; ++k)
 #pragma unroll
                 for (int t = 0; t < N; ++t)
                   sc[t][k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[k][i], qf[t][i], sc[t][k], 0, 0, 0);
-              }
+            }
             if constexpr (F8) {
 #pragma unroll
               for (int mt = 0; mt < NMT; ++mt)
@@ -869,13 +885,18 @@ __global__ __launch_bounds__(64 * kRowWaves, kManyPerCu) void attn_many_kernel(R
             }
             Weights w[N][NS];
             softmax_step<F8, N, NS>(sc, ve, p.scale_log2, m_run, l_run, acc, w);
+            // (two channel tiles at a time: no product waits for the one before it)
 #pragma unroll
-            for (int mt = 0; mt < NMT; ++mt)
+            for (int mt = 0; mt < NMT; mt += 2)
 #pragma unroll
               for (int k = 0; k < NS; ++k) {
-                if constexpr (!F8) vf[k][mt] = value(k, mt);
+                if constexpr (!F8) vf[k][mt] = value(k, mt), vf[k][mt + 1] = value(k, mt + 1);
 #pragma unroll
-                for (int t = 0; t < N; ++t) acc[t][mt] = w[t][k].mul(vf[k][mt], acc[t][mt]);
+                for (int part = 0; part < Weights::kParts; ++part)
+#pragma unroll
+                  for (int i = mt; i < mt + 2; ++i)
+#pragma unroll
+                    for (int t = 0; t < N; ++t) acc[t][i] = w[t][k].mul(part, vf[k][i], acc[t][i]);
               }
           }
         }
@@ -933,24 +954,50 @@ __global__ __launch_bounds__(64 * kRowWaves, kManyPerCu) void attn_many_kernel(R
 }
 
 // ---------------------------------------------------------------------------
+// Four channels of a row, merged from its unit's partials.
+struct Merged {
+  float M = kNegInf, L = 0.f;
+  f32x4 O = {0.f, 0.f, 0.f, 0.f};
+  __device__ __forceinline__ void join(float2 ml, f32x4 o) {
+    const float mn = fmaxf(M, ml.x);
+    const float mu = (mn == kNegInf) ? 0.f : mn;
+    const float wa = fast_exp2(M - mu), wb = fast_exp2(ml.x - mu);
+    L = L * wa + ml.y * wb;
+    O = O * wa + o * wb;
+    M = mn;
+  }
+  __device__ __forceinline__ void store(uint16_t* out) const {
+    const float inv = L > 0.f ? 1.f / L : 0.f;
+    ushort4 v;
+    v.x = f2bf(O[0] * inv);
+    v.y = f2bf(O[1] * inv);
+    v.z = f2bf(O[2] * inv);
+    v.w = f2bf(O[3] * inv);
+    *reinterpret_cast<ushort4*>(out) = v;
+  }
+};
+
+// Sequence of a token row: the last one that starts at it or before it.
+__device__ __forceinline__ int seq_of_row(const RowsParams& p, int trow) {
+  if (!p.cu) return trow;
+  int lo = 0, hi = p.B - 1;
+  while (lo < hi) {
+    const int mid = (lo + hi + 1) >> 1;
+    if (p.cu[mid] <= trow)
+      lo = mid;
+    else
+      hi = mid - 1;
+  }
+  return lo;
+}
+
 // Merge launch: work-group (token row, kv head) merges the token's G rows over the
 // pieces of its unit in work-group order, a thread 4 channels of a row.
 template <int D>
 __global__ __launch_bounds__(256) void attn_rows_merge_kernel(RowsParams p) {
   constexpr int D4 = D / 4;
   const int trow = blockIdx.x, kvh = blockIdx.y;
-  int b = trow;
-  if (p.cu) {  // the last sequence that starts at trow or before it
-    int lo = 0, hi = p.B - 1;
-    while (lo < hi) {
-      const int mid = (lo + hi + 1) >> 1;
-      if (p.cu[mid] <= trow)
-        lo = mid;
-      else
-        hi = mid - 1;
-    }
-    b = lo;
-  }
+  const int b = seq_of_row(p, trow);
   const Seq s = seq_of(p, b);
   const int tok = trow - s.row0;
   if (s.ctx == 0 || tok < 0 || tok >= s.take) return;
@@ -960,28 +1007,53 @@ __global__ __launch_bounds__(256) void attn_rows_merge_kernel(RowsParams p) {
     const int row = tok * G + h, pass = row / (s.tiles * 16);
     const int2 sp = p.span[((size_t)b * p.Hkv + kvh) * p.max_passes + pass];
     if (sp.x == sp.y) continue;  // written by the first launch
-    float M = kNegInf, L = 0.f;
-    f32x4 O = {0.f, 0.f, 0.f, 0.f};
+    Merged a;
 #pragma unroll 4
     for (int w = sp.x; w <= sp.y; ++w) {
       const size_t at = part_row(p, s, kvh, row, w);
-      const float2 ml = *reinterpret_cast<const float2*>(p.part_ml + at * 2);
-      const f32x4 o = *reinterpret_cast<const f32x4*>(p.part_o + at * D + d4 * 4);
-      const float mn = fmaxf(M, ml.x);
-      const float mu = (mn == kNegInf) ? 0.f : mn;
-      const float wa = fast_exp2(M - mu), wb = fast_exp2(ml.x - mu);
-      L = L * wa + ml.y * wb;
-      O = O * wa + o * wb;
-      M = mn;
+      a.join(*reinterpret_cast<const float2*>(p.part_ml + at * 2), *reinterpret_cast<const f32x4*>(p.part_o + at * D + d4 * 4));
     }
-    const float inv = L > 0.f ? 1.f / L : 0.f;
-    ushort4 v;
-    v.x = f2bf(O[0] * inv);
-    v.y = f2bf(O[1] * inv);
-    v.z = f2bf(O[2] * inv);
-    v.w = f2bf(O[3] * inv);
-    *reinterpret_cast<ushort4*>(p.out + ((size_t)trow * p.Hq + kvh * G + h) * D + d4 * 4) = v;
+    a.store(p.out + ((size_t)trow * p.Hq + kvh * G + h) * D + d4 * 4);
   }
+}
+
+// The same for units cut into many pieces (a few long contexts): a work-group per
+// (token row, query head), whose 256 / (D / 4) groups of lanes each take a share of
+// the pieces, then the shares in order through LDS.
+template <int D>
+__global__ __launch_bounds__(256) void attn_rows_merge_many_kernel(RowsParams p) {
+  constexpr int D4 = D / 4, NG = 256 / D4;
+  __shared__ float sm_m[NG], sm_l[NG];
+  __shared__ __attribute__((aligned(16))) float sm_o[NG][D];
+  const int trow = blockIdx.x, head = blockIdx.y;
+  const int kvh = head / p.G;
+  const int b = seq_of_row(p, trow);
+  const Seq s = seq_of(p, b);
+  const int tok = trow - s.row0;
+  if (s.ctx == 0 || tok < 0 || tok >= s.take) return;
+  const int row = tok * p.G + (head - kvh * p.G), pass = row / (s.tiles * 16);
+  const int2 sp = p.span[((size_t)b * p.Hkv + kvh) * p.max_passes + pass];
+  if (sp.x == sp.y) return;
+  const int grp = threadIdx.x / D4, d4 = threadIdx.x - grp * D4;
+  const int per = (sp.y - sp.x + NG) / NG;
+  const int w0 = sp.x + grp * per, w1 = min(w0 + per, sp.y + 1);
+  Merged a;
+#pragma unroll 4
+  for (int w = w0; w < w1; ++w) {
+    const size_t at = part_row(p, s, kvh, row, w);
+    a.join(*reinterpret_cast<const float2*>(p.part_ml + at * 2), *reinterpret_cast<const f32x4*>(p.part_o + at * D + d4 * 4));
+  }
+  if (d4 == 0) {
+    sm_m[grp] = a.M;
+    sm_l[grp] = a.L;
+  }
+  *reinterpret_cast<f32x4*>(&sm_o[grp][d4 * 4]) = a.O;
+  __syncthreads();
+  if (grp != 0) return;
+#pragma unroll
+  for (int i = 1; i < NG; ++i)
+    a.join(make_float2(sm_m[i], sm_l[i]), *reinterpret_cast<const f32x4*>(&sm_o[i][d4 * 4]));
+  a.store(p.out + ((size_t)trow * p.Hq + head) * D + d4 * 4);
 }
 
 // ---------------------------------------------------------------------------
@@ -992,9 +1064,25 @@ namespace {
 // 64 rows, two tiles of a half of the tokens).
 struct RowsPlan {
   int tiles, pass_tiles, passes, pass_rows, grid;
+  bool whole;  // a work-group per unit, no merge
 };
 
 constexpr int kRowsUnitCost = 8;
+
+// Units take a work-group each, without partials and the merge's launch, where
+// contexts are at most kWholeCtx and one round of work-groups holds all units (4
+// sequences of about 80 tokens, 8 / 2 heads x 64: 6.3 us a call, 9.5 with the even
+// split), and where contexts are at most kWholeManyCtx and the units are at least
+// 3/4 of what the GPU holds at once: dealt out as work-groups end, they balance
+// themselves (256 sequences of median 500 tokens, 64 / 8 heads x 128: 79.6 us, 86.8 with
+// the even split; 128 of median 1000: 64.4 and 66.7; 128 of median 400 with up to 8
+// drafts: 61.7 and 71.4).
+constexpr int kWholeCtx = 512;
+constexpr int kWholeManyCtx = 2048;
+
+// Pieces per unit from which the merge shares a unit's pieces among lanes (8 units
+// cut into 64 pieces each: 4.9 us, 10.5 in one chain of loads).
+constexpr int kManyPieces = 8;
 
 int compute_units() {
   static std::atomic<int> cached{0};
@@ -1021,12 +1109,16 @@ RowsPlan rows_plan(const RowsShape& s) {
   r.passes = all > r.pass_tiles ? (all + r.pass_tiles - 1) / r.pass_tiles : 1;
   r.pass_rows = rows < r.pass_tiles * 16 ? rows : r.pass_tiles * 16;
   const long long most = (long long)compute_units() * (r.tiles == 0 ? few_per_cu(s.D) : kManyPerCu);
-  const long long P = (positions_bound(s, r.passes) + 7) / 8;
-  r.grid = (int)(P < 1 ? 1 : P < most ? P : most);
+  const long long units = (long long)s.B * s.Hkv * r.passes;
+  r.whole = (s.max_ctx <= kWholeCtx && units <= most) || (s.max_ctx <= kWholeManyCtx && 4 * units >= 3 * most);
+  const long long P = r.whole ? units : (positions_bound(s, r.passes) + 7) / 8;
+  r.grid = (int)(P < 1 ? 1 : P < most || r.whole ? P : most);
   return r;
 }
 
-size_t part_rows(const RowsShape& s, const RowsPlan& r) { return (size_t)s.T * s.Hq + (size_t)r.grid * r.pass_rows; }
+size_t part_rows(const RowsShape& s, const RowsPlan& r) {
+  return r.whole ? 1 : (size_t)s.T * s.Hq + (size_t)r.grid * r.pass_rows;
+}
 
 template <int D, bool F8>
 void launch_tiles(const RowsParams& p, const RowsPlan& r, hipStream_t stream) {
@@ -1088,6 +1180,7 @@ hipError_t launch_attn_rows(const RowsShape& s, const RowsTensors& t, void* ws, 
   p.num_blocks = s.num_blocks;
   p.max_ctx = s.max_ctx;
   p.unit_cost = kRowsUnitCost;
+  p.whole = r.whole;
   p.scale_log2 = (s.scale != 0.f ? s.scale : 1.0f / sqrtf((float)s.D)) * kLog2e;
   {
     ProfScope ps("attn_rows", stream);
@@ -1100,10 +1193,15 @@ hipError_t launch_attn_rows(const RowsShape& s, const RowsTensors& t, void* ws, 
     else
       launch_tiles<64, false>(p, r, stream);
   }
-  if (r.grid > 1) {  // one work-group cuts no unit
+  if (r.grid > 1 && !r.whole) {  // (else no unit is cut)
     ProfScope ps("attn_rows_merge", stream);
-    const dim3 grid(s.T, s.Hkv);
-    if (s.D == 128)
+    const bool many = r.grid >= kManyPieces * (long long)s.B * s.Hkv * r.passes;
+    const dim3 grid(s.T, many ? s.Hq : s.Hkv);
+    if (many && s.D == 128)
+      attn_rows_merge_many_kernel<128><<<grid, 256, 0, stream>>>(p);
+    else if (many)
+      attn_rows_merge_many_kernel<64><<<grid, 256, 0, stream>>>(p);
+    else if (s.D == 128)
       attn_rows_merge_kernel<128><<<grid, 256, 0, stream>>>(p);
     else
       attn_rows_merge_kernel<64><<<grid, 256, 0, stream>>>(p);

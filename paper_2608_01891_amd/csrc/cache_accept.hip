@@ -13,7 +13,7 @@
 
 namespace aflex {
 
-constexpr int kAcceptBatch = 8;
+constexpr int kAcceptBatch = 16;
 
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
@@ -26,13 +26,15 @@ struct Moves {
 
 __device__ __forceinline__ Moves find_moves(const aflex_cache_accept_args& a, int b, int lane) {
   Moves m{0, 0, -1, -1, 0, 0};
+  // (all of a sequence's numbers in one round of loads)
   const int ctx = a.context_lens[b];
   const long long n = (long long)a.cu_seqlens[b + 1] - a.cu_seqlens[b];
+  const int most = min(a.accepted_counts[b], a.max_accepted);
+  const int listed = a.accepted[(size_t)b * a.max_accepted + min(lane, a.max_accepted - 1)];
   m.ctx_out = ctx;
   if (ctx < 1 || ctx > a.max_blocks_per_seq * 16 || n < 0 || n > ctx) return m;
   const int start = ctx - (int)n;
-  const int most = min(a.accepted_counts[b], a.max_accepted);
-  const int at = lane < most ? a.accepted[(size_t)b * a.max_accepted + lane] : -1;
+  const int at = lane < most ? listed : -1;
   const int before = lane > 0 ? __shfl_up(at, 1) : -1;
   const unsigned long long bad = __ballot(!(lane < most && at > before && at < n));
   m.n = bad ? __builtin_ctzll(bad) : 64;

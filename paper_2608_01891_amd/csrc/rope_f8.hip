@@ -155,24 +155,22 @@ __global__ __launch_bounds__(256) void rope_write_f8_kernel(aflex_rope_f8_args a
   int part = blockIdx.y;
   const int rot = a.rotary_dim;
   if (part < vparts) {
-    // V: a thread per (kv head, 8 channels) with the block's rows
-    if (s.blk < 0) return;
+    // V: a thread per (kv head, 8 channels) with the block's rows. (They and the positions
+    // are loaded beside the block's id, which is looked at behind them.)
     constexpr int C = D / 8;
     const int t = part * 256 + threadIdx.x;
     const int g = t / C, c = t % C;
-    if (g >= a.Hkv) return;  // (whole heads: the lanes of a row stay together)
-    const uint16_t* src = a.v_new + (size_t)g * D + c * 8;
-    const size_t tile = (size_t)s.blk * a.Hkv + g;
+    // Rows that are written, the same for all threads: a lane looks at each (one after
+    // the other, their positions took 16 rounds to memory).
+    const int pos = slot_pos(a, s, threadIdx.x & 15);
+    const uint16_t* src = a.v_new + (size_t)min(g, a.Hkv - 1) * D + c * 8;
+    // (rows that do not exist repeat one that does)
     uint4 row[16];
-    uint32_t live = 0;  // rows that are written, the same for all threads
 #pragma unroll
-    for (int o = 0; o < 16; ++o) live |= slot_pos(a, s, o) >= 0 ? 1u << o : 0u;
-    live = __builtin_amdgcn_readfirstlane(live);
-    if (live == 0) return;
-    // (rows that are not written repeat one that is)
-    const int first = __builtin_ctz(live);
-#pragma unroll
-    for (int o = 0; o < 16; ++o) row[o] = ld4(src + (size_t)(s.src + (live >> o & 1 ? o : first)) * a.v_stride);
+    for (int o = 0; o < 16; ++o) row[o] = ld4(src + (size_t)(s.src + min(max(o, s.o0), s.o1 - 1)) * a.v_stride);
+    const uint32_t live = (uint32_t)__ballot(pos >= 0) & 0xffffu;
+    if (s.blk < 0 || g >= a.Hkv || live == 0) return;  // (whole heads: the lanes of a row stay together)
+    const size_t tile = (size_t)s.blk * a.Hkv + g;
     float inv[16];
     uint32_t ew[4] = {0, 0, 0, 0};
 #pragma unroll
@@ -201,7 +199,6 @@ __global__ __launch_bounds__(256) void rope_write_f8_kernel(aflex_rope_f8_args a
   part -= vparts;
   const bool key = part < kparts;
   if (!key) part -= kparts;
-  if (key && s.blk < 0) return;
   const int heads = key ? a.Hkv : a.Hq;
   const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
   const int h0 = (part * 4 + wave) * per_wave, h1 = min(h0 + per_wave, heads);
@@ -209,6 +206,20 @@ __global__ __launch_bounds__(256) void rope_write_f8_kernel(aflex_rope_f8_args a
   const int u = lane % U, r = lane / U;
   int d0, d1;
   unit_channels<INTER>(u, rot, d0, d1);
+  const size_t stride = key ? a.k_stride : a.q_stride;
+  const uint16_t* base = key ? a.k_new : a.q;
+  auto load = [&](int h, uint4(&row)[NR][2]) {
+#pragma unroll
+    for (int i = 0; i < NR; ++i) {
+      const int o = r + i * RS;  // (rows that exist, whether or not their position does)
+      if (o < s.o0 || o >= s.o1) continue;
+      const uint16_t* p = base + (size_t)(s.src + o) * stride + (size_t)h * D;
+      row[i][0] = ld4(p + d0);
+      row[i][1] = ld4(p + d1);
+    }
+  };
+  uint4 next[NR][2] = {};
+  load(h0, next);
   int pos[NR];
   Angles an[NR];
 #pragma unroll
@@ -216,19 +227,7 @@ __global__ __launch_bounds__(256) void rope_write_f8_kernel(aflex_rope_f8_args a
     pos[i] = slot_pos(a, s, r + i * RS);
     if (pos[i] >= 0 && u * 16 < rot) an[i] = load_angles(a.rope, pos[i], rot, u);
   }
-  const size_t stride = key ? a.k_stride : a.q_stride;
-  const uint16_t* base = key ? a.k_new : a.q;
-  auto load = [&](int h, uint4(&row)[NR][2]) {
-#pragma unroll
-    for (int i = 0; i < NR; ++i) {
-      if (pos[i] < 0) continue;
-      const uint16_t* p = base + (size_t)(s.src + r + i * RS) * stride + (size_t)h * D;
-      row[i][0] = ld4(p + d0);
-      row[i][1] = ld4(p + d1);
-    }
-  };
-  uint4 next[NR][2] = {};
-  load(h0, next);
+  if (key && s.blk < 0) return;
   for (int h = h0; h < h1; ++h) {
     uint4 row[NR][2];
 #pragma unroll
