@@ -24,7 +24,9 @@
  *   c_d = x_d 2^-e rounded to e4m3 (to nearest, ties to even); NaN for a
  *         non-finite x_d
  * and stands for c 2^e. Every step but the one rounding is exact. (A row with
- * values of 1.9375 2^127 or more may stand for an infinity.) Pools of a cache:
+ * values of 1.9375 2^127 or more may stand for an infinity.) Exponents lie in
+ * [-100, 120]; others are read for tokens that nothing attends only. Pools of a
+ * cache:
  *   k_cache [num_blocks, Hkv, 16, D] codes
  *   v_cache [num_blocks, Hkv, D, 16] codes (token fastest)
  *   kv_exp  [num_blocks, Hkv, 2, 16] exponents: the 16 keys', the 16 values'
@@ -72,6 +74,8 @@ typedef struct aflex_rope_f8_args {
 } aflex_rope_f8_args;
 
 /* Supported and clamped as aflex_rope_append and aflex_rope_write. No workspace. */
+/* aflex_rope_write_f8 may read and write back the values' codes of the other      */
+/* slots of a block that it writes: no other call writes that block meanwhile.     */
 aflex_status aflex_rope_append_f8(const aflex_rope_f8_args *a, aflex_stream stream);
 aflex_status aflex_rope_write_f8(const aflex_rope_f8_args *a, aflex_stream stream);
 
@@ -112,8 +116,9 @@ aflex_status aflex_attn_decode_f8(const aflex_attn_f8_args *a, void *workspace, 
 /*   place s_b + j for each j < n_b whose bit j of masks[cu_seqlens[b] + i] is */
 /*   set (its ancestors and itself; any set is allowed). masks NULL: j <= i    */
 /*   (a chain: the drafts follow each other, or are the tokens of a chunk).    */
-/* A row that attends nothing yields 0. One draft per sequence that sees       */
-/* itself is decode attention.                                                 */
+/* A row that attends nothing yields 0, and what a row does not attend does    */
+/* not change it, whatever its keys and values hold. One draft per sequence    */
+/* that sees itself is decode attention.                                       */
 /* ------------------------------------------------------------------------ */
 typedef struct aflex_attn_tree_args {
   const aflex_bf16 *q;         /* [T, Hq, D] */
@@ -135,7 +140,7 @@ typedef struct aflex_attn_tree_args {
 
 /* Supported: D in {64, 128}, block_size == 16, Hq % Hkv == 0, Hq / Hkv <= 16, */
 /* max_drafts <= 64, T <= B * max_drafts, B * Hkv * (ceil(max_context_len /    */
-/* 16) + 16) * ceil(max_drafts * (Hq / Hkv) / 192) < 2^30, T * Hq < 2^30,      */
+/* 16) + 16) * ceil(max_drafts * (Hq / Hkv) / 128) < 2^30, T * Hq < 2^30,      */
 /* T < 2^24, Hkv <= 65535. */
 /* Device-side values are clamped: rows to [0, T], contexts to [0,             */
 /* max_context_len] (s_b then counts from the clamped length; places below 0   */

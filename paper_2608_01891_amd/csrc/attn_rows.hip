@@ -14,13 +14,13 @@
 // the second product's operand.
 //
 // 8-bit rows are c 2^e. A key's codes become bf16 with its 2^e on the way, exactly.
-// A value's exponent joins the score: with s' = s + e the weight of the codes is
-// P' = 2^(s' - M'), M' the running maximum of s', and the row's sum is that of
-// P' 2^-e. So the largest contribution has weight 1, and P' enters the product as
-// fp16 (11 bits; below 2^-14 steps of 2^-24 of the largest) with the codes as fp16,
-// exactly. Over a bf16 cache a weight enters as two bf16 values, the rounded
-// weight and what its rounding left: 16 bits. (One bf16 value, 8 bits, would show
-// beside the output's own rounding: 2.1e-3 of the norm instead of 1.65e-3.)
+// A value's exponent joins the weight: P' = p 2^e enters the product with the codes
+// as fp16, exactly, and the row's sum is that of p. p = 2^(s - M') with M' the
+// largest s + e, to within 2^kSlack: the largest contribution has a P' of 2 to 2^9,
+// and P' is rounded to fp16 (11 bits; below 2^-14 steps of 2^-24). Over a bf16 cache
+// a weight enters as two bf16 values, the rounded weight and what its rounding left:
+// 16 bits. (One bf16 value, 8 bits, would show beside the output's own rounding:
+// 2.1e-3 of the norm instead of 1.65e-3.)
 //
 // Two kernels. Up to 16 rows (decode attention): the waves of a work-group take the
 // tokens in turns, keys and values go from memory straight into the matrix
@@ -32,6 +32,16 @@
 // end, and each work-group takes a consecutive range of them, so that long and
 // short contexts fill the GPU alike; a unit cut between work-groups leaves fp32
 // partials that a second launch merges in order.
+//
+// Bounds, and what was measured (caches that no call has read just before; 8-bit and
+// 64 / 8 heads x 128 but where it says otherwise). Decode attention: the cache's bytes.
+// 64 sequences of median 4096 tokens, 740 MB: 134.3 us, 5.5 TB/s; one of 400000, 826
+// MB: 139.2 us, 5.9 TB/s, where loads alone reach 6.4. Trees: what the vector units
+// issue, the widening of the codes and the softmax, about 215 instructions of a wave
+// beside the 32 products of a step. 32 sequences of median 4096 tokens, up to 8 drafts
+// each, 328 MB: 98.5 us, 3.3 TB/s; one context of 65536 with 64 drafts: 195 to 202 us,
+// 0.7 PFLOP/s (a large matrix product reaches 1.41); 8 sequences of median 8192, up to
+// 32 drafts, 32 / 8 heads, bf16, 301 MB: 85 to 89 us, 3.5 TB/s.
 #include <math.h>
 
 #include <atomic>
@@ -47,7 +57,11 @@ namespace aflex {
 namespace {
 
 constexpr int kRowWaves = 4;
-constexpr int kMostTiles = 2;  // row tiles of a wave (16 rows each)
+// Row tiles (16 rows each) of a wave, where there is more than one tile. (Three leave no
+// registers for the loads ahead: one context of 65536 with 64 drafts took 282 us
+// instead of 231; one, with all four waves on the same tokens, 99.9 instead of 93.3 us
+// for 32 sequences with 8 drafts.)
+constexpr int kTiles = 2;
 
 struct RowsParams {
   const uint16_t* q;
@@ -331,26 +345,108 @@ struct TwoWeights {
   }
 };
 
-constexpr float kSlack = 8.f;
+// Values that are not finite, in steps where not every row sees every token. A weight
+// of 0 does not take one out of a product, so a row would get those of drafts that it
+// does not see. The products have zeros in their place (m: one bit for each), and the
+// rows that see them get them afterwards.
+template <bool F8, class V>
+__device__ __forceinline__ V without_odd(V v, bool& odd) {
+  uint32_t any = 0;
+#pragma unroll
+  for (int i = 0; i < (int)(sizeof(V) / 4); ++i) {
+    const uint32_t m = F8 ? ((v[i] & 0x7f7f7f7fu) + 0x01010101u) >> 7 & 0x01010101u
+                          : ((v[i] & 0x7f807f80u) + 0x00800080u) >> 15 & 0x00010001u;
+    v[i] &= ~(m * (F8 ? 0xffu : 0xffffu));
+    any |= m;
+  }
+  odd = odd || any != 0;
+  return v;
+}
 
-// The softmax of N row tiles over NS slices of 8 tokens per lane: scores x (masked:
-// -inf) to weights, the running maxima m and sums l, and the accumulators' rescaling.
-// F8: ve holds the tokens' value exponents, a byte each with 128 added (in M' alone,
-// so it cancels), which joins a score by one conversion and its inverse the sum by one
-// shift.
-template <bool F8, int N, int NS, int NMT, class Weights>
-__device__ __forceinline__ void softmax_step(f32x4 (&x)[N][2 * NS], const u32x2 (&ve)[NS], float scale_log2,
-                                             float (&m)[N], float (&l)[N], f32x4 (&acc)[N][NMT], Weights (&w)[N][NS]) {
-  constexpr int E = 8 * NS;
-  const auto byte = [&](int e) { return ve[e / 8][(e / 4) & 1] >> (8 * (e & 3)) & 0xffu; };
-  if constexpr (F8) {
-#pragma unroll
-    for (int e = 0; e < E; ++e) {
-      const float v = (float)byte(e);
-#pragma unroll
-      for (int t = 0; t < N; ++t) x[t][e / 4][e & 3] = fmaf(x[t][e / 4][e & 3], scale_log2, v);
+// A work-group's pieces once more, if s_odd says so for one of its waves: the values
+// that without_odd took out of the products (of steps of BLOCKS blocks), added to what
+// store_rows has stored of the rows that see them. A pass of its own that reads the
+// kernel's arguments (a RowsParams alone) again, so that the loop of the products need
+// not keep anything for it.
+template <int D, bool F8, int BLOCKS>
+__device__ __forceinline__ void add_odd(int least, const int* s_odd) {
+  const int tid = threadIdx.x, lane = tid & 63;
+  __syncthreads();  // (and what was stored is there for the others)
+  if (!(s_odd[0] | s_odd[1] | s_odd[2] | s_odd[3])) return;
+  auto* args = __builtin_amdgcn_kernarg_segment_ptr();
+  asm volatile("" : "+s"(args));
+  RowsParams p;
+  __builtin_memcpy(&p, (const void*)args, sizeof(p));
+  int per, x, x1, b, base;
+  if (!find_range(p, least, lane, per, x, x1, b, base)) return;
+  while (x < x1) {
+    const Seq s = seq_of(p, b);
+    const int all = p.Hkv * s.passes * unit_len(p, s);
+    if (x >= base + all) {
+      base += all;
+      ++b;
+      continue;
+    }
+    int xn;
+    const Piece c = piece_at(p, s, base, x, x1, per, xn);
+    x = xn;
+    if (c.j1 <= c.j0) break;
+    const int start = s.ctx - s.n;
+    const int32_t* table = p.bt + (size_t)b * p.max_blocks;
+    for (int step = c.j0; step < c.j1; step += BLOCKS) {
+      bool whole = (step + BLOCKS) * 16 <= start && step + BLOCKS <= c.j1;
+      for (int j = step; j < min(step + BLOCKS, c.j1); ++j) whole = whole && (uint32_t)table[j] < (uint32_t)p.num_blocks;
+      if (whole) continue;
+      for (int j = step; j < min(step + BLOCKS, c.j1); ++j) {
+        const int id = table[j], cached = s.ctx - j * 16;
+        if ((uint32_t)id >= (uint32_t)p.num_blocks) continue;
+        for (int it = tid; it < c.rows * D; it += 64 * kRowWaves) {
+          const int row = c.row0 + it / D, d = it % D;
+          const uint64_t mask = mask_of_row(p, s, row);
+          const uint32_t seen =
+              seen_bits(mask, j * 16, start, cached) | seen_bits(mask, j * 16 + 8, start, cached - 8) << 8;
+          const size_t at = (((size_t)id * p.Hkv + c.kvh) * D + d) * 16;
+          float sum = 0.f;
+          for (int k = 0; k < 16; ++k) {
+            float v;
+            if constexpr (F8)
+              v = (p.vc[at + k] & 0x7f) == 0x7f ? __builtin_nanf("") : 0.f;
+            else
+              v = bf2f(reinterpret_cast<const uint16_t*>(p.vc)[at + k]);
+            sum += (seen >> k & 1u) && !(fabsf(v) < __builtin_inff()) ? v : 0.f;
+          }
+          if (sum == 0.f) continue;
+          if (c.first == c.last) {
+            uint16_t* o = p.out + row_of(p, s, c.kvh, row) * D + d;
+            *o = f2bf(bf2f(*o) + sum);
+          } else {
+            p.part_o[part_row(p, s, c.kvh, row, blockIdx.x) * D + d] += sum;
+          }
+        }
+      }
     }
   }
+}
+
+// x 2^d for d <= 0, where 2^d alone may be too small for a float.
+__device__ __forceinline__ float times_exp2(float x, float d) {
+  const float h = fast_exp2(0.5f * d);
+  return x * h * h;
+}
+
+constexpr float kSlack = 8.f;
+
+// The softmax of N row tiles over 8 tokens per lane: scores x (masked: -inf) to
+// weights, the references m and sums l, and the accumulators' rescaling.
+// F8: ve holds the tokens' value exponents, a byte each with 128 added, in the
+// references too. p = 2^(s - m) joins the sum; one shift makes 2^(e + 1) of the byte,
+// and P' = p 2^(e + 1), so the sum is doubled at the end. p is 2^-e where P' is
+// largest: it stays within floats, and what of the sum is too small for them is below
+// 2^(e - 126) of that.
+template <bool F8, int N, int NMT, class Weights>
+__device__ __forceinline__ void softmax_step(f32x4 (&x)[N][2], u32x2 ve, float scale_log2, float (&m)[N], float (&l)[N],
+                                             f32x4 (&acc)[N][NMT], Weights (&w)[N]) {
+  const auto byte = [&](int e) { return ve[e / 4] >> (8 * (e & 3)) & 0xffu; };
   // A row's reference m is its maximum when it was set last, and stays while no score
   // is more than kSlack above it: weights are up to 2^kSlack then. So the hot path
   // compares a lane's own scores alone, and the four lanes of a row exchange theirs
@@ -358,10 +454,16 @@ __device__ __forceinline__ void softmax_step(f32x4 (&x)[N][2 * NS], const u32x2 
   bool above = false;
   float mx[N];
 #pragma unroll
-  for (int t = 0; t < N; ++t) {
-    mx[t] = x[t][0][0];
+  for (int e = 0; e < 8; ++e) {
+    const float v = F8 ? (float)byte(e) : 0.f;
 #pragma unroll
-    for (int e = 1; e < E; ++e) mx[t] = fmaxf(mx[t], x[t][e / 4][e & 3]);
+    for (int t = 0; t < N; ++t) {
+      const float s = F8 ? fmaf(x[t][e / 4][e & 3], scale_log2, v) : x[t][e / 4][e & 3];
+      mx[t] = e == 0 ? s : fmaxf(mx[t], s);
+    }
+  }
+#pragma unroll
+  for (int t = 0; t < N; ++t) {
     if constexpr (!F8) mx[t] *= scale_log2;
     above = above || mx[t] > m[t] + kSlack;
   }
@@ -369,8 +471,8 @@ __device__ __forceinline__ void softmax_step(f32x4 (&x)[N][2 * NS], const u32x2 
 #pragma unroll
     for (int t = 0; t < N; ++t) {
       const float m_new = fmaxf(m[t], row_max(mx[t]));
-      const float alpha = m_new == kNegInf ? 1.f : fast_exp2(m[t] - m_new);
-      l[t] *= alpha;
+      const float d = m_new == kNegInf ? 0.f : m[t] - m_new, alpha = fast_exp2(d);
+      l[t] = F8 ? times_exp2(l[t], d) : l[t] * alpha;
 #pragma unroll
       for (int mt = 0; mt < NMT; ++mt) acc[t][mt] *= alpha;
       m[t] = m_new;
@@ -378,72 +480,61 @@ __device__ __forceinline__ void softmax_step(f32x4 (&x)[N][2 * NS], const u32x2 
   }
   float m_use[N];
 #pragma unroll
-  for (int t = 0; t < N; ++t) m_use[t] = m[t] == kNegInf ? 0.f : m[t];
+  for (int t = 0; t < N; ++t) m_use[t] = m[t] == kNegInf ? 0.f : F8 ? m[t] - 128.f : m[t];
   float ps[N][2];
 #pragma unroll
-  for (int e = 0; e < E; e += 2) {
-    float inv[2];
-    if constexpr (F8) {
+  for (int e = 0; e < 8; e += 2) {
+    float f[2];
 #pragma unroll
-      for (int i = 0; i < 2; ++i) inv[i] = __uint_as_float((255u - byte(e + i)) << 23);  // 2^-exponent
-    }
+    for (int i = 0; i < 2; ++i) f[i] = F8 ? __uint_as_float(byte(e + i) << 23) : 1.f;  // 2^(exponent + 1)
 #pragma unroll
     for (int t = 0; t < N; ++t) {
       float u[2];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
-        const float s = x[t][(e + i) / 4][(e + i) & 3];
-        u[i] = fast_exp2(F8 ? s - m_use[t] : fmaf(s, scale_log2, -m_use[t]));
-        if constexpr (F8)
-          ps[t][i] = e == 0 ? u[i] * inv[i] : fmaf(u[i], inv[i], ps[t][i]);
-        else
-          ps[t][i] = e == 0 ? u[i] : ps[t][i] + u[i];
+        u[i] = fast_exp2(fmaf(x[t][(e + i) / 4][(e + i) & 3], scale_log2, -m_use[t]));
+        ps[t][i] = e == 0 ? u[i] : ps[t][i] + u[i];
+        if constexpr (F8) u[i] *= f[i];
       }
-      w[t][e / 8].set(e & 7, u[0], u[1]);
+      w[t].set(e, u[0], u[1]);
     }
   }
 #pragma unroll
   for (int t = 0; t < N; ++t) l[t] += ps[t][0] + ps[t][1];
 }
 
-// Block ids of a piece by scalar loads: raw ones are fetched a step ahead, and become
-// ids (-1: no such block) when their step's loads are made.
-template <int NB>
+// A row's sum over the lanes that hold it.
+template <bool F8>
+__device__ __forceinline__ float row_sum(float l) {
+  l += __shfl_xor(l, 16);
+  l += __shfl_xor(l, 32);
+  return F8 ? l + l : l;
+}
+
+// Block ids of a piece's steps of two blocks by scalar loads: raw ones are fetched a
+// step ahead, and become ids (-1: no such block) when their step's loads are made.
 struct BlockIds {
   typedef const int32_t __attribute__((address_space(4))) * Table;
   Table table;
   int j0, j1, num_blocks;
-  int raw0, raw1, raw2, raw3;
-  int id0, id1, id2, id3;
+  int raw0, raw1;
+  int id0, id1;
 
   __device__ __forceinline__ BlockIds(const RowsParams& p, int b, int j0, int j1)
       : table((Table)(reinterpret_cast<uintptr_t>(p.bt + (size_t)b * p.max_blocks))), j0(j0), j1(j1),
-        num_blocks(p.num_blocks), raw0(-1), raw1(-1), raw2(-1), raw3(-1), id0(-1), id1(-1), id2(-1), id3(-1) {}
+        num_blocks(p.num_blocks), raw0(-1), raw1(-1), id0(-1), id1(-1) {}
   __device__ __forceinline__ void fetch(int st) {
-    const int j = j0 + st * NB, e = j1 - 1;
+    const int j = j0 + st * 2, e = j1 - 1;
     raw0 = table[min(j, e)];
     raw1 = table[min(j + 1, e)];
-    if constexpr (NB == 4) {
-      raw2 = table[min(j + 2, e)];
-      raw3 = table[min(j + 3, e)];
-    }
   }
   __device__ __forceinline__ int fine(int id, int j) const { return j < j1 && id >= 0 && id < num_blocks ? id : -1; }
   __device__ __forceinline__ void take(int st) {
-    const int j = j0 + st * NB;
+    const int j = j0 + st * 2;
     id0 = fine(raw0, j);
     id1 = fine(raw1, j + 1);
-    if constexpr (NB == 4) {
-      id2 = fine(raw2, j + 2);
-      id3 = fine(raw3, j + 3);
-    }
   }
-  __device__ __forceinline__ bool all_fine() const { return (id0 | id1 | (NB == 4 ? id2 | id3 : 0)) >= 0; }
-  __device__ __forceinline__ int pick(int i) const {
-    const int low = (i & 1) ? id1 : id0;
-    if constexpr (NB == 4) return (i & 2) ? ((i & 1) ? id3 : id2) : low;
-    return low;
-  }
+  __device__ __forceinline__ int pick(int i) const { return i ? id1 : id0; }
 };
 
 // Waits for the global loads so far. In front of a loop whose loads run a step ahead:
@@ -451,16 +542,24 @@ struct BlockIds {
 // with the loads of the next step.
 __device__ __forceinline__ void wait_for_loads() { __builtin_amdgcn_s_waitcnt(0x0f70); }  // vmcnt(0)
 
+// Work-groups that a CU holds at once. Few rows: two, D = 64 three (at D = 128 a third
+// costs the registers of the step ahead: 139.9 us instead of 136.8 for 64 sequences,
+// 153.7 instead of 145.8 for one of 400000).
 constexpr int few_per_cu(int D) { return D == 64 ? 3 : 2; }
 
-// Work-groups that a CU holds at once (by registers).
+// Least positions of a work-group: a step for each wave, two steps.
+constexpr int kFewLeast = 2 * kRowWaves, kManyLeast = 8;
+
+// More rows: by registers.
 constexpr int kManyPerCu = 2;
 
 }  // namespace
 
 // ---------------------------------------------------------------------------
-// Up to 16 rows: a step is 32 tokens (two blocks) of one wave.
-template <int D, bool F8>
+// Up to 16 rows: a step is 32 tokens (two blocks) of one wave. (64: 146 us instead of
+// 138 for 64 sequences, as fewer loads are on their way.) DRAFTS: rows may differ in the
+// tokens that they see.
+template <int D, bool F8, bool DRAFTS>
 __global__ __launch_bounds__(64 * kRowWaves, few_per_cu(D)) void attn_few_kernel(RowsParams p) {
   constexpr int NC = D / 32;       // k-chunks of the first product
   constexpr int NMT = D / 16;      // d-tiles of the second
@@ -469,6 +568,7 @@ __global__ __launch_bounds__(64 * kRowWaves, few_per_cu(D)) void attn_few_kernel
   typedef std::conditional_t<F8, u32x2, u32x4> VLoad;  // a lane's 8 tokens of a channel
   typedef std::conditional_t<F8, HalfWeights, TwoWeights> Weights;
   __shared__ __attribute__((aligned(16))) float so[2 * 16 * LDO];  // partials of two waves
+  __shared__ int s_odd[kRowWaves];
 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int lane = threadIdx.x & 63;
@@ -480,7 +580,8 @@ __global__ __launch_bounds__(64 * kRowWaves, few_per_cu(D)) void attn_few_kernel
 
   clear_empty<D>(p);
   int per, x, x1, b, base;
-  if (!find_range(p, 2 * kRowWaves, lane, per, x, x1, b, base)) return;
+  if (!find_range(p, kFewLeast, lane, per, x, x1, b, base)) return;
+  if (lane == 0) s_odd[wave] = 0;
   while (x < x1) {
     const Seq s = seq_of(p, b);
     const int all = p.Hkv * s.passes * unit_len(p, s);
@@ -495,7 +596,7 @@ __global__ __launch_bounds__(64 * kRowWaves, few_per_cu(D)) void attn_few_kernel
     if (c.j1 <= c.j0) break;
     const int start = s.ctx - s.n;  // place of the first draft
     const int steps = (c.j1 - c.j0 + 1) / 2;
-    BlockIds<2> ids(p, b, c.j0, c.j1);
+    BlockIds ids(p, b, c.j0, c.j1);
 
     u32x4 kraw[NK];  // (8-bit codes come 16 channels a load, and the k-chunks take the channels in that order)
     VLoad vraw[NMT];
@@ -542,7 +643,7 @@ __global__ __launch_bounds__(64 * kRowWaves, few_per_cu(D)) void attn_few_kernel
 
     const int row = min(r, c.rows - 1);
     const uint16_t* qrow = p.q + row_of(p, s, c.kvh, row) * D;
-    const uint64_t mask = mask_of_row(p, s, row);
+    const uint64_t mask = DRAFTS ? mask_of_row(p, s, row) : 0;
     bf16x8 qf[NC];
 #pragma unroll
     for (int i = 0; i < NC; ++i)
@@ -583,35 +684,40 @@ __global__ __launch_bounds__(64 * kRowWaves, few_per_cu(D)) void attn_few_kernel
       ids.fetch(min(next + kRowWaves, steps - 1));
       __builtin_amdgcn_sched_barrier(0);
 
-      if (!((jb_now + 2) * 16 <= start && __all(nv_now >= 8))) {  // drafts, or places that hold nothing
-        const uint32_t seen = seen_bits(mask, tb_now, start, nv_now);
+      if (!((!DRAFTS || (jb_now + 2) * 16 <= start) && __all(nv_now >= 8))) {  // drafts, or places that hold nothing
+        const uint32_t seen = DRAFTS ? seen_bits(mask, tb_now, start, nv_now) : seen_bits(0, tb_now, tb_now + 8, nv_now);
 #pragma unroll
         for (int e = 0; e < 8; ++e) sc[0][e / 4][e & 3] = (seen >> e & 1u) ? sc[0][e / 4][e & 3] : kNegInf;
         // zeros behind the context, so that 0 times what lies there is 0
 #pragma unroll
         for (int mt = 0; mt < NMT; ++mt) vraw[mt] = keep_bytes(vraw[mt], F8 ? nv_now : 2 * nv_now);
+        if constexpr (DRAFTS) {
+          bool odd = false;
+#pragma unroll
+          for (int mt = 0; mt < NMT; ++mt) vraw[mt] = without_odd<F8>(vraw[mt], odd);
+          if (odd) s_odd[wave] = 1;
+        }
         if constexpr (F8) vx = keep_bytes(vx, nv_now);
       }
-      const u32x2 ve[1] = {F8 ? vx ^ 0x80808080u : vx};
-      Weights w[1][1];
-      softmax_step<F8, 1, 1>(sc, ve, p.scale_log2, m_run, l_run, acc, w);
+      const u32x2 ve = F8 ? vx ^ 0x80808080u : vx;
+      Weights w[1];
+      softmax_step<F8>(sc, ve, p.scale_log2, m_run, l_run, acc, w);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int part = 0; part < Weights::kParts; ++part)
 #pragma unroll
         for (int mt = 0; mt < NMT; ++mt) {
           if constexpr (F8)
-            acc[0][mt] = w[0][0].mul(part, widen_f16(vraw[mt][0], vraw[mt][1]), acc[0][mt]);
+            acc[0][mt] = w[0].mul(part, widen_f16(vraw[mt][0], vraw[mt][1]), acc[0][mt]);
           else
-            acc[0][mt] = w[0][0].mul(part, __builtin_bit_cast(bf16x8, vraw[mt]), acc[0][mt]);
+            acc[0][mt] = w[0].mul(part, __builtin_bit_cast(bf16x8, vraw[mt]), acc[0][mt]);
         }
       __builtin_amdgcn_sched_barrier(0);
       load_values(next);
     }
 
     // ---- merge the waves, in a fixed order: the upper half deposits, the lower adds ----
-    l_run[0] += __shfl_xor(l_run[0], 16);
-    l_run[0] += __shfl_xor(l_run[0], 32);
+    l_run[0] = row_sum<F8>(l_run[0]);
 #pragma unroll
     for (int half = kRowWaves / 2; half >= 1; half /= 2) {
       float* o = so + ((wave % half) * 16 + r) * LDO;
@@ -627,7 +733,7 @@ __global__ __launch_bounds__(64 * kRowWaves, few_per_cu(D)) void attn_few_kernel
         const float mn = fmaxf(m_run[0], ml.x);
         const float mu = (mn == kNegInf) ? 0.f : mn;
         const float wa = fast_exp2(m_run[0] - mu), wb = fast_exp2(ml.x - mu);
-        l_run[0] = l_run[0] * wa + ml.y * wb;
+        l_run[0] = times_exp2(l_run[0], m_run[0] - mu) + times_exp2(ml.y, ml.x - mu);
         m_run[0] = mn;
 #pragma unroll
         for (int mt = 0; mt < NMT; ++mt)
@@ -640,10 +746,13 @@ __global__ __launch_bounds__(64 * kRowWaves, few_per_cu(D)) void attn_few_kernel
       store_rows<D>(p, s, c, c.row0 + r, qg, m_run[0], l_run[0], acc[0]);
     }
   }
+  if constexpr (DRAFTS) add_odd<D, F8, 2>(kFewLeast, s_odd);
 }
 
 // ---------------------------------------------------------------------------
-// More rows: a step is 64 tokens (four blocks) of the work-group. Its threads load
+// More rows, WR waves on row tiles of their own, and 4 / WR on halves of a step's
+// tokens: up to 64 rows WR = 2 (two tiles a wave share what it reads from LDS), else 4.
+// A step is 64 tokens (four blocks) of the work-group. Its threads load
 // the tiles as they lie (16 bytes each, whole 128-byte lines), a step ahead, and put
 // them into LDS as 16-bit operands: K [token][D] with the tokens in the order of the
 // first product's tiles, V^T [D][token], padded rows.
@@ -653,7 +762,7 @@ __device__ __forceinline__ void lds_barrier() {
   __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
 }
 
-template <int D, bool F8, int WR, int RT>
+template <int D, bool F8, int WR>
 __global__ __launch_bounds__(64 * kRowWaves, kManyPerCu) void attn_many_kernel(RowsParams p) {
   constexpr int NC = D / 32, NMT = D / 16;
   constexpr int ES = F8 ? 1 : 2;
@@ -662,12 +771,12 @@ __global__ __launch_bounds__(64 * kRowWaves, kManyPerCu) void attn_many_kernel(R
   constexpr int LDK = D + 8, LDV = 64 + 8;        // padded rows in LDS (16-bit elements)
   constexpr int LDO = D + 4;                      // row of a partial in LDS: O, then (m, l)
   constexpr int TS = kRowWaves / WR;              // waves that share a step's tokens
-  constexpr int NS = 1;       // 32-token slices per softmax step
   typedef std::conditional_t<F8, HalfWeights, TwoWeights> Weights;
   typedef std::conditional_t<F8, f16x8, bf16x8> VFrag;
-  constexpr int kTileBytes = (64 * LDK + D * LDV) * 2, kPartBytes = TS == 2 ? WR * RT * 16 * LDO * 4 : 0;
+  constexpr int kTileBytes = (64 * LDK + D * LDV) * 2, kPartBytes = TS == 2 ? WR * kTiles * 16 * LDO * 4 : 0;
   __shared__ __attribute__((aligned(16))) uint8_t sm[kTileBytes > kPartBytes ? kTileBytes : kPartBytes];
   __shared__ __attribute__((aligned(16))) uint8_t sx[F8 ? 64 : 8];  // the values' exponents, 128 added
+  __shared__ int s_odd[kRowWaves];
   uint16_t* sk = reinterpret_cast<uint16_t*>(sm);
   uint16_t* sv = sk + 64 * LDK;
   float* so = reinterpret_cast<float*>(sm);
@@ -679,7 +788,8 @@ __global__ __launch_bounds__(64 * kRowWaves, kManyPerCu) void attn_many_kernel(R
 
   clear_empty<D>(p);
   int per, x, x1, b, base;
-  if (!find_range(p, 8, lane, per, x, x1, b, base)) return;
+  if (!find_range(p, kManyLeast, lane, per, x, x1, b, base)) return;
+  if (lane == 0) s_odd[wave] = 0;
   while (x < x1) {
     const Seq s = seq_of(p, b);
     const int all = p.Hkv * s.passes * unit_len(p, s);
@@ -698,9 +808,8 @@ __global__ __launch_bounds__(64 * kRowWaves, kManyPerCu) void attn_many_kernel(R
     const int per_wave = (c.tiles + WR - 1) / WR;
     const int group = wave % WR, half = wave / WR;
     const int t0 = group * per_wave, mine = max(min(c.tiles - t0, per_wave), 0);
-    // Block ids by vector loads, 64 a register and the next 64 ahead (scalar loads share
-    // the counter of the LDS's, so that every barrier would wait for them). -1: no such
-    // block. (Plain variables: a struct of them stayed in memory.)
+    // Block ids by vector loads, 64 a register and the next 64 ahead. -1: no such block.
+    // (Plain variables: a struct of them stayed in memory.)
     const int32_t* table = p.bt + (size_t)b * p.max_blocks;
     auto load_id = [&](int j) __attribute__((always_inline)) { return table[min(j, c.j1 - 1)]; };
     int ids_now = load_id(c.j0 + lane), ids_next = load_id(c.j0 + 64 + lane), chunk = 0;
@@ -750,18 +859,23 @@ __global__ __launch_bounds__(64 * kRowWaves, kManyPerCu) void attn_many_kernel(R
       }
     };
     // (n0 .. n3: cached tokens of the blocks; zeros behind them, so that 0 times what lies there is 0)
-    auto store = [&](bool full, int n0, int n1, int n2, int n3) __attribute__((always_inline)) {
+    auto store = [&](bool whole, int n0, int n1, int n2, int n3) __attribute__((always_inline)) {
+      if (!whole) {
+        bool odd = false;
+#pragma unroll
+        for (int i = 0; i < NL; ++i) {
+          const int k = blk(i), nv = k == 0 ? n0 : k == 1 ? n1 : k == 2 ? n2 : n3;
+          vraw[i] = without_odd<F8>(keep_bytes(vraw[i], F8 ? nv : 2 * (nv - (within(i) & 1) * 8)), odd);
+          if constexpr (F8) vx[i] = (lane & 15) < nv ? vx[i] : 0;
+        }
+        if (odd) s_odd[wave] = 1;
+      }
 #pragma unroll
       for (int i = 0; i < NL; ++i) {
         const int k = blk(i), w = within(i);
         const int o = w / (D * ES / 16), u = (k & 1) * 16 + o;
         uint16_t* kd = sk + ((k >> 1) * 32 + ((u >> 2) & 1) * 16 + (u >> 3) * 4 + (u & 3)) * LDK +
                        (w % (D * ES / 16)) * (16 / ES);
-        if (!full) {
-          const int nv = k == 0 ? n0 : k == 1 ? n1 : k == 2 ? n2 : n3;
-          vraw[i] = keep_bytes(vraw[i], F8 ? nv : 2 * (nv - (w & 1) * 8));
-          if constexpr (F8) vx[i] = (lane & 15) < nv ? vx[i] : 0;
-        }
         const u32x4 v = vraw[i];
         if constexpr (F8) {
           const float f = exp2_whole((int8_t)(kx[i] >> (8 * (o & 3))));
@@ -804,114 +918,94 @@ __global__ __launch_bounds__(64 * kRowWaves, kManyPerCu) void attn_many_kernel(R
       wait_for_loads();
       for (int st = 0; st < steps; ++st) {
         const int jb = c.j0 + st * 4;
-        const bool full = (jb + 4) * 16 <= s.ctx && (id0 | id1 | id2 | id3) >= 0;
+        const bool whole = (jb + 4) * 16 <= start && (id0 | id1 | id2 | id3) >= 0;  // every row sees every token
         int n0 = 16, n1 = 16, n2 = 16, n3 = 16;
-        if (!full) {
+        if (!whole) {
           const auto cached = [&](int id, int i) { return id >= 0 ? min(max(s.ctx - (jb + i) * 16, 0), 16) : 0; };
           n0 = cached(id0, 0), n1 = cached(id1, 1), n2 = cached(id2, 2), n3 = cached(id3, 3);
         }
         lds_barrier();  // every wave is done with the step before
-        store(full, n0, n1, n2, n3);
+        store(whole, n0, n1, n2, n3);
         if (st + 1 < steps) {
           take_ids(st + 1);
           load();
         }
         lds_barrier();
         if constexpr (N > 0) {
-          const bool whole = full && (jb + 4) * 16 <= start;
 #pragma unroll
-          for (int part = 0; part < 2 / NS / TS; ++part) {
-            const int h = TS == 2 ? half : part;  // slices h NS ..
-            f32x4 sc[N][2 * NS];
+          for (int part = 0; part < 2 / TS; ++part) {
+            const int h = TS == 2 ? half : part;  // the slice of 32 tokens
+            const u32x2 ve = F8 ? *reinterpret_cast<const u32x2*>(sx + h * 32 + qg * 8) : u32x2{0, 0};
+            f32x4 sc[N][2];
 #pragma unroll
-            for (int t = 0; t < N; ++t)
-#pragma unroll
-              for (int k = 0; k < 2 * NS; ++k) sc[t][k] = f32x4{0.f, 0.f, 0.f, 0.f};
+            for (int t = 0; t < N; ++t) sc[t][0] = sc[t][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+            auto key = [&](int k, int i) __attribute__((always_inline)) {
+              return ld_bf16x8(sk + ((h * 2 + k) * 16 + r) * LDK + i * 32 + qg * 8);
+            };
+            auto value = [&](int mt) __attribute__((always_inline)) {
+              return *reinterpret_cast<const VFrag*>(sv + (mt * 16 + r) * LDV + h * 32 + qg * 8);
+            };
             // (8-bit cache: all of a product's operands are read before it starts, the values'
             // before the softmax. A bf16 step ahead takes twice the registers and leaves none
             // for that.)
-            u32x2 ve[NS];
-#pragma unroll
-            for (int k = 0; k < NS; ++k)
-              ve[k] = F8 ? *reinterpret_cast<const u32x2*>(sx + (h * NS + k) * 32 + qg * 8) : u32x2{0, 0};
-            auto key = [&](int k, int i) __attribute__((always_inline)) {
-              return ld_bf16x8(sk + ((h * 2 * NS + k) * 16 + r) * LDK + i * 32 + qg * 8);
-            };
-            auto value = [&](int k, int mt) __attribute__((always_inline)) {
-              return *reinterpret_cast<const VFrag*>(sv + (mt * 16 + r) * LDV + (h * NS + k) * 32 + qg * 8);
-            };
-            bf16x8 kf[2 * NS][NC];
-            VFrag vf[NS][NMT];
+            bf16x8 kf[2][NC];
+            VFrag vf[NMT];
             if constexpr (F8) {
 #pragma unroll
-              for (int k = 0; k < 2 * NS; ++k)
+              for (int k = 0; k < 2; ++k)
 #pragma unroll
                 for (int i = 0; i < NC; ++i) kf[k][i] = key(k, i);
               __builtin_amdgcn_sched_barrier(0);
             }
 #pragma unroll
             for (int i = 0; i < NC; ++i) {
-              if constexpr (!F8) {
+              if constexpr (!F8) kf[0][i] = key(0, i), kf[1][i] = key(1, i);
 #pragma unroll
-                for (int k = 0; k < 2 * NS; ++k) kf[k][i] = key(k, i);
-              }
-#pragma unroll
-              for (int k = 0; k < 2 * NS; ++k)
+              for (int k = 0; k < 2; ++k)
 #pragma unroll
                 for (int t = 0; t < N; ++t)
                   sc[t][k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[k][i], qf[t][i], sc[t][k], 0, 0, 0);
             }
             if constexpr (F8) {
 #pragma unroll
-              for (int mt = 0; mt < NMT; ++mt)
-#pragma unroll
-                for (int k = 0; k < NS; ++k) vf[k][mt] = value(k, mt);
+              for (int mt = 0; mt < NMT; ++mt) vf[mt] = value(mt);
               __builtin_amdgcn_sched_barrier(0);
             }
             if (!whole) {
+              // the lane's 8 tokens lie in block 2 h + (qg >> 1)
+              const int tb = jb * 16 + h * 32 + qg * 8;
+              const int nv = (h == 0 ? ((qg & 2) ? n1 : n0) : ((qg & 2) ? n3 : n2)) - (qg & 1) * 8;
 #pragma unroll
-              for (int k = 0; k < NS; ++k) {
-                const int sl = h * NS + k;  // 32-token slice: the lane's 8 tokens lie in its block 2 sl + (qg >> 1)
-                const int in = sl == 0 ? ((qg & 2) ? n1 : n0) : ((qg & 2) ? n3 : n2);
-                const int tb = jb * 16 + sl * 32 + qg * 8;
+              for (int t = 0; t < N; ++t) {
+                const uint32_t seen = seen_bits(mask[t], tb, start, nv);
 #pragma unroll
-                for (int t = 0; t < N; ++t) {
-                  const uint32_t seen = seen_bits(mask[t], tb, start, in - (qg & 1) * 8);
-#pragma unroll
-                  for (int e = 0; e < 8; ++e)
-                    sc[t][2 * k + e / 4][e & 3] = (seen >> e & 1u) ? sc[t][2 * k + e / 4][e & 3] : kNegInf;
-                }
+                for (int e = 0; e < 8; ++e) sc[t][e / 4][e & 3] = (seen >> e & 1u) ? sc[t][e / 4][e & 3] : kNegInf;
               }
             }
-            Weights w[N][NS];
-            softmax_step<F8, N, NS>(sc, ve, p.scale_log2, m_run, l_run, acc, w);
+            Weights w[N];
+            softmax_step<F8>(sc, ve, p.scale_log2, m_run, l_run, acc, w);
             // (two channel tiles at a time: no product waits for the one before it)
 #pragma unroll
-            for (int mt = 0; mt < NMT; mt += 2)
+            for (int mt = 0; mt < NMT; mt += 2) {
+              if constexpr (!F8) vf[mt] = value(mt), vf[mt + 1] = value(mt + 1);
 #pragma unroll
-              for (int k = 0; k < NS; ++k) {
-                if constexpr (!F8) vf[k][mt] = value(k, mt), vf[k][mt + 1] = value(k, mt + 1);
+              for (int part = 0; part < Weights::kParts; ++part)
 #pragma unroll
-                for (int part = 0; part < Weights::kParts; ++part)
+                for (int i = mt; i < mt + 2; ++i)
 #pragma unroll
-                  for (int i = mt; i < mt + 2; ++i)
-#pragma unroll
-                    for (int t = 0; t < N; ++t) acc[t][i] = w[t][k].mul(part, vf[k][i], acc[t][i]);
-              }
+                  for (int t = 0; t < N; ++t) acc[t][i] = w[t].mul(part, vf[i], acc[t][i]);
+            }
           }
         }
       }
 #pragma unroll
-      for (int t = 0; t < N; ++t) {
-        l_run[t] += __shfl_xor(l_run[t], 16);
-        l_run[t] += __shfl_xor(l_run[t], 32);
-      }
+      for (int t = 0; t < N; ++t) l_run[t] = row_sum<F8>(l_run[t]);
       if constexpr (TS == 2) {  // the second half's waves deposit, the first half's add
         lds_barrier();
         if (half == 1) {
 #pragma unroll
           for (int t = 0; t < N; ++t) {
-            float* o = so + ((group * RT + t) * 16 + r) * LDO;
+            float* o = so + ((group * kTiles + t) * 16 + r) * LDO;
 #pragma unroll
             for (int mt = 0; mt < NMT; ++mt) *reinterpret_cast<f32x4*>(o + mt * 16 + 4 * qg) = acc[t][mt];
             if (qg == 0) *reinterpret_cast<float2*>(o + D) = make_float2(m_run[t], l_run[t]);
@@ -921,12 +1015,12 @@ __global__ __launch_bounds__(64 * kRowWaves, kManyPerCu) void attn_many_kernel(R
         if (half == 0) {
 #pragma unroll
           for (int t = 0; t < N; ++t) {
-            const float* o = so + ((group * RT + t) * 16 + r) * LDO;
+            const float* o = so + ((group * kTiles + t) * 16 + r) * LDO;
             const float2 ml = *reinterpret_cast<const float2*>(o + D);
             const float mn = fmaxf(m_run[t], ml.x);
             const float mu = (mn == kNegInf) ? 0.f : mn;
             const float wa = fast_exp2(m_run[t] - mu), wb = fast_exp2(ml.x - mu);
-            l_run[t] = l_run[t] * wa + ml.y * wb;
+            l_run[t] = times_exp2(l_run[t], m_run[t] - mu) + times_exp2(ml.y, ml.x - mu);
             m_run[t] = mn;
 #pragma unroll
             for (int mt = 0; mt < NMT; ++mt)
@@ -942,15 +1036,11 @@ __global__ __launch_bounds__(64 * kRowWaves, kManyPerCu) void attn_many_kernel(R
     };
     if (mine == 0) run_steps(std::integral_constant<int, 0>{});
     if (mine == 1) run_steps(std::integral_constant<int, 1>{});
-    if constexpr (RT >= 2) {
-      if (mine == 2) run_steps(std::integral_constant<int, 2>{});
-    }
-    if constexpr (RT >= 3) {
-      if (mine == 3) run_steps(std::integral_constant<int, 3>{});
-    }
+    if (mine == 2) run_steps(std::integral_constant<int, 2>{});
     if (tid == 0 && (int)blockIdx.x == c.first)
       p.span[((size_t)b * p.Hkv + c.kvh) * p.max_passes + c.pass] = make_int2(c.first, c.last);
   }
+  add_odd<D, F8, 4>(kManyLeast, s_odd);
 }
 
 // ---------------------------------------------------------------------------
@@ -962,7 +1052,7 @@ struct Merged {
     const float mn = fmaxf(M, ml.x);
     const float mu = (mn == kNegInf) ? 0.f : mn;
     const float wa = fast_exp2(M - mu), wb = fast_exp2(ml.x - mu);
-    L = L * wa + ml.y * wb;
+    L = times_exp2(L, M - mu) + times_exp2(ml.y, ml.x - mu);
     O = O * wa + o * wb;
     M = mn;
   }
@@ -1060,8 +1150,8 @@ __global__ __launch_bounds__(256) void attn_rows_merge_many_kernel(RowsParams p)
 // Host side.
 namespace {
 
-// What a launch takes: row tiles of a wave (0: the kernel for up to 16 rows; 1: up to
-// 64 rows, two tiles of a half of the tokens).
+// What a launch takes: tiles 0 is the kernel for up to 16 rows, 1 that for up to 64, 2
+// that for more.
 struct RowsPlan {
   int tiles, pass_tiles, passes, pass_rows, grid;
   bool whole;  // a work-group per unit, no merge
@@ -1104,7 +1194,7 @@ long long positions_bound(const RowsShape& s, int passes) {
 RowsPlan rows_plan(const RowsShape& s) {
   RowsPlan r;
   const int rows = s.max_n * (s.Hq / s.Hkv), all = (rows + 15) / 16;
-  r.tiles = all <= 1 ? 0 : all <= kRowWaves ? 1 : all <= 2 * kRowWaves ? 2 : kMostTiles;
+  r.tiles = all <= 1 ? 0 : all <= kRowWaves ? 1 : kTiles;
   r.pass_tiles = r.tiles == 0 ? 1 : r.tiles * kRowWaves;
   r.passes = all > r.pass_tiles ? (all + r.pass_tiles - 1) / r.pass_tiles : 1;
   r.pass_rows = rows < r.pass_tiles * 16 ? rows : r.pass_tiles * 16;
@@ -1123,20 +1213,20 @@ size_t part_rows(const RowsShape& s, const RowsPlan& r) {
 template <int D, bool F8>
 void launch_tiles(const RowsParams& p, const RowsPlan& r, hipStream_t stream) {
   const dim3 grid(r.grid), block(64 * kRowWaves);
-  if (r.tiles == 0)
-    attn_few_kernel<D, F8><<<grid, block, 0, stream>>>(p);
+  if (!p.cu)
+    attn_few_kernel<D, true, false><<<grid, block, 0, stream>>>(p);
+  else if (r.tiles == 0)
+    attn_few_kernel<D, F8, true><<<grid, block, 0, stream>>>(p);
   else if (r.tiles == 1)
-    attn_many_kernel<D, F8, 2, 2><<<grid, block, 0, stream>>>(p);
-  else if (r.tiles == 2)
-    attn_many_kernel<D, F8, 4, 2><<<grid, block, 0, stream>>>(p);
+    attn_many_kernel<D, F8, 2><<<grid, block, 0, stream>>>(p);
   else
-    attn_many_kernel<D, F8, 4, 3><<<grid, block, 0, stream>>>(p);
+    attn_many_kernel<D, F8, 4><<<grid, block, 0, stream>>>(p);
 }
 
 }  // namespace
 
 bool rows_shape_fits(const RowsShape& s) {
-  const int rows = s.max_n * (s.Hq / s.Hkv), most = kMostTiles * kRowWaves * 16;
+  const int rows = s.max_n * (s.Hq / s.Hkv), most = kTiles * kRowWaves * 16;
   const long long passes = rows > most ? (rows + most - 1) / most : 1;
   return (long long)s.B * s.Hkv * passes * ((s.max_ctx + 15) / 16 + 16) < (1ll << 30) &&
          (long long)s.T * s.Hq < (1ll << 30);

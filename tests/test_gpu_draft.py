@@ -5,16 +5,18 @@ bf16. Cached rows are compared for equality with codes made from the formula's f
 operations, which the plain expression repeats. Attention: out is rounded to bf16,
 2^-8 of |out|. Over a bf16 cache a weight enters the product as two bf16 values, the
 second rounded to 2^-8 of at most 2^-8 of it: 2^-16 of the weight. Over an 8-bit one
-it is p 2^e over the largest p 2^e of the row, rounded to fp16: 2^-11 of it, or half
-the least step, 2^-25 of the largest: on a code c, 2^-25 max(p 2^e) |c| (`small`
-sums those). The products and the sum of the weights are fp32 sums of n terms: at
-most 2 n 2^-24 of sum p |v|. A score is an fp32 sum of D products, its scaling and
-the running maximum's subtraction 4 more roundings: (D + 4) 2^-24 of sum |q k|
-scale; the exponents added to it, of magnitudes up to 16 here, 16 2^-24. exp2 (itself
-off by 2^-22) turns that into as much of the weight, in the numerator and in the
-denominator: 2 (D + 4) 2^-24 size + 2^-19 + 2^-21. Hence
-  |y - r| <= 2^-8 |r| + 1.01 ((w + 2^-18 + 2 n 2^-24 + 2 (D + 4) 2^-24 size) sum p |v| + 2^-25 small)
-with w = 2^-16 or 2^-11.
+it is p 2^e over a reference of at most the largest p 2^e of the row, rounded to fp16:
+2^-11 of it, or half the least step, 2^-25 of the largest: on a code c, 2^-25 max(p
+2^e) |c| (`small` sums those). The products and the sum of the weights are fp32 sums
+of n terms: at most 2 n 2^-24 of sum p |v|. A score is an fp32 sum of D products, its
+scaling and the reference's subtraction 4 more roundings: (D + 4) 2^-24 of sum |q k|
+scale; the exponent in the reference, of a magnitude up to E, adds E 2^-24. exp2
+(itself off by 2^-22) turns that into as much of the weight, in the numerator and in
+the denominator: 2 (D + 4) 2^-24 size + 2 E 2^-24 + 2^-21. Where the reference grows,
+what came before is scaled by an exp2 of at most 2^-8: once 2^-22 in the sum and in the
+product, the times before by 2^-8 less each: 2^-21. Hence
+  |y - r| <= 2^-8 |r| + 1.01 ((w + 2 E 2^-24 + 2^-20 + 2 n 2^-24 + 2 (D + 4) 2^-24 size) sum p |v| + 2^-25 small)
+with w = 2^-16 or 2^-11, and E = 16 where a test does not say otherwise.
 Whatever is copied or masked is compared for equality.
 """
 import threading
@@ -249,10 +251,10 @@ def test_write_leaves_alone_what_has_no_place(gpu_lib):
 
 
 # ------------------------------------------------------------------ attention
-def _check_attn(got, ref, n, D, what=""):
+def _check_attn(got, ref, n, D, what="", exps=16):
     out, mag, size, small = ref
     w = 2.0 ** -11 if small.any() else 2.0 ** -16  # an 8-bit cache, or bf16
-    most = 1.01 * ((w + 2.0 ** -18 + 2 * n * 2.0 ** -24 + 2 * (D + 4) * 2.0 ** -24 * size[..., None]) * mag
+    most = 1.01 * ((w + 2 * exps * 2.0 ** -24 + 2.0 ** -20 + 2 * n * 2.0 ** -24 + 2 * (D + 4) * 2.0 ** -24 * size[..., None]) * mag
                    + 2.0 ** -25 * small)
     err = (got.cpu().double() - out).abs()
     bad = ~(err <= 2.0 ** -8 * out.abs() + most)
@@ -391,6 +393,88 @@ def test_masked_places_do_not_matter(gpu_lib, f8):
     kb[blk, :, o] = nan
     got, _ = _tree(b, counts, 58, masks)
     assert torch.equal(got, clean)
+
+
+@pytest.mark.parametrize("f8", [False, True])
+@pytest.mark.parametrize("heads,ctx", [((2, 1, 64), 90), ((4, 1, 128), 90), ((8, 1, 64), 200), ((8, 1, 128), 6000),
+                                       ((14, 1, 128), 200), ((16, 1, 64), 6000), ((12, 3, 128), 2500)])
+@pytest.mark.parametrize("chain", [False, True])
+def test_values_that_are_not_finite_reach_the_rows_that_see_them(gpu_lib, heads, ctx, f8, chain):
+    """Infinities and NaN in the values of drafts, and of tokens beside a block that does not exist."""
+    Hq, Hkv, D = heads
+    counts, lens = [6, 3], [ctx, 35]
+    a, b = (_cache(105, heads, lens, f8, ctx_hi=ctx + 40) for _ in range(2))
+    masks = None if chain else _trees(106, counts) & ~(1 << 4) | 1
+    bad = [0, 2, 4]  # drafts of the first sequence
+    full = torch.tensor([(2 << i) - 1 for n in counts for i in range(n)]) if chain else masks
+    for c in (a, b):
+        c.block_table[0, 1] = -1
+        kv = (c.k_cache.view(torch.uint8), c.v_cache.view(torch.uint8)) if f8 else (c.k_cache, c.v_cache)
+        for place in [lens[0] - 6 + j for j in bad] + [3]:
+            blk, o = int(c.block_table[0, place // 16]), place % 16
+            if f8:
+                kv[1][blk, :, 5:9, o] = 0x7f if c is b else 0
+            else:
+                kv[1][blk, :, 5:9, o] = 0.0
+                if c is b:
+                    kv[1][blk, :, 5, o] = float("inf")
+                    kv[1][blk, :, 6, o] = float("inf") if place % 2 else float("-inf")
+                    kv[1][blk, :, 7, o] = float("nan")
+    seen = torch.tensor([[bool(int(m) >> j & 1) for j in bad] for m in full[:6]])
+    assert bool(seen.any(-1).all())  # (draft 0 is seen by all; place 3 too)
+    q = _rand(107, 9, Hq, D).bfloat16()
+    clean, _ = _tree(a, counts, 0, masks, q=q)
+    got, ref = _tree(b, counts, 0, masks, q=q)
+    keep = [d for d in range(D) if not 5 <= d < 9]
+    assert torch.equal(got[:, :, keep], clean[:, :, keep]) and torch.equal(got[6:], clean[6:])
+    assert torch.equal(got[:6, :, 8], clean[:6, :, 8]) or f8
+    assert _same(got.cpu()[:6, :, 5:8], ref[0][:6, :, 5:8])
+    # without the tokens that all rows see: rows that see no such draft are as if there were none
+    for c in (a, b):
+        kv = (c.k_cache.view(torch.uint8), c.v_cache.view(torch.uint8)) if f8 else (c.k_cache, c.v_cache)
+        for place in (lens[0] - 6, 3):
+            kv[1][int(c.block_table[0, place // 16]), :, 5:9, place % 16] = 0
+    clean, _ = _tree(a, counts, 0, masks, q=q)
+    got, ref = _tree(b, counts, 0, masks, q=q)
+    none = ~seen[:, 1:].any(-1)
+    assert bool(none.any()) and torch.equal(got[:6][none.to(DEV)], clean[:6][none.to(DEV)])
+    assert _same(got.cpu()[:6, :, 5:8][~none], ref[0][:6, :, 5:8][~none])
+
+
+@pytest.mark.parametrize("heads,counts", [((8, 2, 64), [1, 1, 1]), ((16, 1, 128), [1, 1, 1]), ((8, 2, 128), [5, 16, 7]),
+                                          ((16, 2, 64), [7, 3, 16])])
+@pytest.mark.parametrize("order", ["mixed", "small first", "large first"])
+def test_values_of_any_size(gpu_lib, heads, counts, order):
+    """Value rows of 2^-100 and zero beside ones of 2^60: the weights and their sum span more than a float does."""
+    lens = [700, 40, 6000]
+    c = _cache(108, heads, lens, True)
+    e = c.kv_exp[:, :, 1]
+    g = torch.Generator().manual_seed(109)
+    e.copy_(torch.randint(-100, 61, e.shape, generator=g))
+    if order != "mixed":  # by the place in the context
+        for s, n in enumerate(lens):
+            for j in range(-(-n // 16)):
+                late = j >= (n // 16) // 2
+                e[int(c.block_table[s, j])] = 60 if late == (order == "small first") else -100
+    zero = torch.randint(0, 3, e.shape, generator=g) == 0
+    c.v_cache.view(torch.uint8).masked_fill_(zero[:, :, None, :], 0)
+    e.masked_fill_(zero, -100)
+    got, ref = _tree(c, counts, 110, None)
+    _check_attn(got, ref, 6000, heads[2], exps=128)
+    e.masked_fill_(e > -60, -100)  # nothing but tiny rows
+    c.v_cache.view(torch.uint8).masked_fill_((e == -100)[:, :, None, :], 0x34)
+    got, ref = _tree(c, counts, 110, None)
+    _check_attn(got, ref, 6000, heads[2], exps=128)
+
+
+@pytest.mark.parametrize("f8", [False, True])
+@pytest.mark.parametrize("heads,most", [((8, 8, 64), 1), ((64, 8, 128), 2), ((64, 8, 128), 6), ((32, 4, 64), 16)])
+def test_units_that_share_work_groups(gpu_lib, f8, heads, most):
+    """Contexts of a large bound: several units a work-group, and units cut between two of them."""
+    counts = [1 + i % most for i in range(40)]
+    a = _cache(111, heads, [(613 * i) % 900 + most for i in range(40)], f8, ctx_hi=6400)
+    got, ref = _tree(a, counts, 112, None)
+    _check_attn(got, ref, 920, heads[2])
 
 
 @pytest.mark.parametrize("f8", [False, True])
