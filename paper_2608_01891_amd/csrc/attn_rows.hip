@@ -36,12 +36,13 @@
 // Bounds, and what was measured (caches that no call has read just before; 8-bit and
 // 64 / 8 heads x 128 but where it says otherwise). Decode attention: the cache's bytes.
 // 64 sequences of median 4096 tokens, 740 MB: 134.3 us, 5.5 TB/s; one of 400000, 826
-// MB: 139.2 us, 5.9 TB/s, where loads alone reach 6.4. Trees: what the vector units
-// issue, the widening of the codes and the softmax, about 215 instructions of a wave
-// beside the 32 products of a step. 32 sequences of median 4096 tokens, up to 8 drafts
-// each, 328 MB: 98.5 us, 3.3 TB/s; one context of 65536 with 64 drafts: 195 to 202 us,
-// 0.7 PFLOP/s (a large matrix product reaches 1.41); 8 sequences of median 8192, up to
-// 32 drafts, 32 / 8 heads, bf16, 301 MB: 85 to 89 us, 3.5 TB/s.
+// MB: 139.2 us, 5.9 TB/s, where loads alone reach 6.4. Trees: the chain of a step
+// (barrier, widening into LDS, barrier, operands, products, softmax, products) with two
+// waves on a SIMD. 32 sequences of median 4096 tokens, up to 8 drafts each, 328 MB: 96
+// us, 3.4 TB/s, the vector units busy for 41% of it, the matrix units 18%, LDS 39%; one
+// context of 65536 with 64 drafts: 194 us, 0.71 PFLOP/s (a large matrix product reaches
+// 1.41), 52%, 31% and 44%; 8 sequences of median 8192, up to 32 drafts, 32 / 8 heads,
+// bf16, 301 MB: 84 us, 3.6 TB/s.
 #include <math.h>
 
 #include <atomic>
@@ -768,7 +769,7 @@ __global__ __launch_bounds__(64 * kRowWaves, kManyPerCu) void attn_many_kernel(R
   constexpr int ES = F8 ? 1 : 2;
   constexpr int CPB = D * ES;                     // 16-byte chunks of a block's K (and V) tile
   constexpr int NL = 4 * CPB / (64 * kRowWaves);  // those of a thread, 4 blocks
-  constexpr int LDK = D + 8, LDV = 64 + 8;        // padded rows in LDS (16-bit elements)
+  constexpr int LDK = D + 16, LDV = 64 + 16;      // padded rows in LDS (16-bit elements; 8: 0.7% slower)
   constexpr int LDO = D + 4;                      // row of a partial in LDS: O, then (m, l)
   constexpr int TS = kRowWaves / WR;              // waves that share a step's tokens
   typedef std::conditional_t<F8, HalfWeights, TwoWeights> Weights;
@@ -1170,9 +1171,12 @@ constexpr int kRowsUnitCost = 8;
 constexpr int kWholeCtx = 512;
 constexpr int kWholeManyCtx = 2048;
 
-// Pieces per unit from which the merge shares a unit's pieces among lanes (8 units
-// cut into 64 pieces each: 4.9 us, 10.5 in one chain of loads).
+// Pieces per unit from which the merge shares a unit's pieces among lanes, if there are
+// few rows: at most kFewRows a CU (one row of 64 heads in 64 pieces: 139.6 us in all, 148.5
+// in one chain of loads; 8 rows: 200 and 204; 64 rows in 16 pieces: 199.8 and 197.8; 200
+// of 32 heads in 8 pieces: 87.6 and 83.7).
 constexpr int kManyPieces = 8;
+constexpr int kFewRows = 8;
 
 int compute_units() {
   static std::atomic<int> cached{0};
@@ -1285,7 +1289,8 @@ hipError_t launch_attn_rows(const RowsShape& s, const RowsTensors& t, void* ws, 
   }
   if (r.grid > 1 && !r.whole) {  // (else no unit is cut)
     ProfScope ps("attn_rows_merge", stream);
-    const bool many = r.grid >= kManyPieces * (long long)s.B * s.Hkv * r.passes;
+    const bool many = r.grid >= kManyPieces * (long long)s.B * s.Hkv * r.passes &&
+                      (long long)s.T * s.Hq <= kFewRows * compute_units();
     const dim3 grid(s.T, many ? s.Hq : s.Hkv);
     if (many && s.D == 128)
       attn_rows_merge_many_kernel<128><<<grid, 256, 0, stream>>>(p);
