@@ -22,7 +22,7 @@
 // 16 bits. (One bf16 value, 8 bits, would show beside the output's own rounding:
 // 2.1e-3 of the norm instead of 1.65e-3.)
 //
-// Two kernels. Up to 16 rows (decode attention): the waves of a work-group take the
+// Two kernels. Up to 16 rows (decode attention; 8-bit cache: 32): the waves of a work-group take the
 // tokens in turns, keys and values go from memory straight into the matrix
 // operands' registers, a step ahead. More rows: the waves share the tokens, 64 a
 // step, which the work-group turns into 16-bit operands in LDS once, and each has
@@ -40,9 +40,9 @@
 // (barrier, widening into LDS, barrier, operands, products, softmax, products) with two
 // waves on a SIMD. 32 sequences of median 4096 tokens, up to 8 drafts each, 328 MB: 96
 // us, 3.4 TB/s, the vector units busy for 41% of it, the matrix units 18%, LDS 39%; one
-// context of 65536 with 64 drafts: 194 us, 0.71 PFLOP/s (a large matrix product reaches
+// context of 65536 with 64 drafts: 196 us, 0.70 PFLOP/s (a large matrix product reaches
 // 1.41), 52%, 31% and 44%; 8 sequences of median 8192, up to 32 drafts, 32 / 8 heads,
-// bf16, 301 MB: 84 us, 3.6 TB/s.
+// bf16, 301 MB: 83 us, 3.6 TB/s.
 #include <math.h>
 
 #include <atomic>
@@ -512,6 +512,26 @@ __device__ __forceinline__ float row_sum(float l) {
   return F8 ? l + l : l;
 }
 
+// A lane's share of a row's partial to LDS and from there to another wave's: O, then (m, l).
+template <int D>
+__device__ __forceinline__ void put_partial(float* o, int qg, float m, float l, const f32x4 (&acc)[D / 16]) {
+#pragma unroll
+  for (int mt = 0; mt < D / 16; ++mt) *reinterpret_cast<f32x4*>(o + mt * 16 + 4 * qg) = acc[mt];
+  if (qg == 0) *reinterpret_cast<float2*>(o + D) = make_float2(m, l);
+}
+
+template <int D>
+__device__ __forceinline__ void add_partial(const float* o, int qg, float& m, float& l, f32x4 (&acc)[D / 16]) {
+  const float2 ml = *reinterpret_cast<const float2*>(o + D);
+  const float mn = fmaxf(m, ml.x);
+  const float mu = (mn == kNegInf) ? 0.f : mn;
+  const float wa = fast_exp2(m - mu), wb = fast_exp2(ml.x - mu);
+  l = times_exp2(l, m - mu) + times_exp2(ml.y, ml.x - mu);
+  m = mn;
+#pragma unroll
+  for (int mt = 0; mt < D / 16; ++mt) acc[mt] = acc[mt] * wa + *reinterpret_cast<const f32x4*>(o + mt * 16 + 4 * qg) * wb;
+}
+
 // Block ids of a piece's steps of two blocks by scalar loads: raw ones are fetched a
 // step ahead, and become ids (-1: no such block) when their step's loads are made.
 struct BlockIds {
@@ -546,7 +566,7 @@ __device__ __forceinline__ void wait_for_loads() { __builtin_amdgcn_s_waitcnt(0x
 // Work-groups that a CU holds at once. Few rows: two, D = 64 three (at D = 128 a third
 // costs the registers of the step ahead: 139.9 us instead of 136.8 for 64 sequences,
 // 153.7 instead of 145.8 for one of 400000).
-constexpr int few_per_cu(int D) { return D == 64 ? 3 : 2; }
+constexpr int few_per_cu(int D, int RT) { return D == 64 && RT == 1 ? 3 : 2; }
 
 // Least positions of a work-group: a step for each wave, two steps.
 constexpr int kFewLeast = 2 * kRowWaves, kManyLeast = 8;
@@ -557,18 +577,23 @@ constexpr int kManyPerCu = 2;
 }  // namespace
 
 // ---------------------------------------------------------------------------
-// Up to 16 rows: a step is 32 tokens (two blocks) of one wave. (64: 146 us instead of
-// 138 for 64 sequences, as fewer loads are on their way.) DRAFTS: rows may differ in the
-// tokens that they see.
-template <int D, bool F8, bool DRAFTS>
-__global__ __launch_bounds__(64 * kRowWaves, few_per_cu(D)) void attn_few_kernel(RowsParams p) {
+// Up to 16 rows, or RT tiles of 16: a step is 32 tokens (two blocks) of one wave. (64:
+// 146 us instead of 138 for 64 sequences, as fewer loads are on their way.) DRAFTS: rows
+// may differ in the tokens that they see. Two tiles for an 8-bit cache alone: 4 drafts
+// of 64 / 8 heads x 128 over 400000 tokens 149.6 us instead of the other kernel's 166, of
+// 32 / 4 x 64 in 32 sequences 30.1 instead of 35.4; over bf16, whose step ahead takes
+// twice the registers, 145.6 instead of 135.4 (200000 tokens). Four tiles, one
+// work-group a CU: 118 us for 32 sequences with 8 drafts instead of 96.
+template <int D, bool F8, bool DRAFTS, int RT>
+__global__ __launch_bounds__(64 * kRowWaves, few_per_cu(D, RT)) void attn_few_kernel(RowsParams p) {
   constexpr int NC = D / 32;       // k-chunks of the first product
   constexpr int NMT = D / 16;      // d-tiles of the second
   constexpr int NK = F8 ? NC : 2 * NC;  // 16-byte loads of a step's keys
   constexpr int LDO = D + 4;       // row of a partial in LDS: O, then (m, l)
   typedef std::conditional_t<F8, u32x2, u32x4> VLoad;  // a lane's 8 tokens of a channel
   typedef std::conditional_t<F8, HalfWeights, TwoWeights> Weights;
-  __shared__ __attribute__((aligned(16))) float so[2 * 16 * LDO];  // partials of two waves
+  typedef std::conditional_t<F8, f16x8, bf16x8> VFrag;
+  __shared__ __attribute__((aligned(16))) float so[2 * RT * 16 * LDO];  // partials of two waves
   __shared__ int s_odd[kRowWaves];
 
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -642,40 +667,51 @@ __global__ __launch_bounds__(64 * kRowWaves, few_per_cu(D)) void attn_few_kernel
       ids.fetch(min(st + kRowWaves, steps - 1));
     }
 
-    const int row = min(r, c.rows - 1);
-    const uint16_t* qrow = p.q + row_of(p, s, c.kvh, row) * D;
-    const uint64_t mask = DRAFTS ? mask_of_row(p, s, row) : 0;
-    bf16x8 qf[NC];
+    uint64_t mask[RT];
+    bf16x8 qf[RT][NC];
+    float m_run[RT], l_run[RT];
+    f32x4 acc[RT][NMT];
 #pragma unroll
-    for (int i = 0; i < NC; ++i)
-      qf[i] = r < c.rows ? ld_bf16x8(qrow + (F8 ? (i >> 1) * 64 + qg * 16 + (i & 1) * 8 : i * 32 + qg * 8)) : zero_bf16x8();
-
-    float m_run[1] = {kNegInf}, l_run[1] = {0.f};
-    f32x4 acc[1][NMT];
+    for (int t = 0; t < RT; ++t) {
+      const int row = t * 16 + r, at = c.row0 + min(row, c.rows - 1);
+      const uint16_t* qrow = p.q + row_of(p, s, c.kvh, at) * D;
+      mask[t] = DRAFTS ? mask_of_row(p, s, at) : 0;
 #pragma unroll
-    for (int mt = 0; mt < NMT; ++mt) acc[0][mt] = f32x4{0.f, 0.f, 0.f, 0.f};
+      for (int i = 0; i < NC; ++i)
+        qf[t][i] =
+            row < c.rows ? ld_bf16x8(qrow + (F8 ? (i >> 1) * 64 + qg * 16 + (i & 1) * 8 : i * 32 + qg * 8)) : zero_bf16x8();
+      m_run[t] = kNegInf;
+      l_run[t] = 0.f;
+#pragma unroll
+      for (int mt = 0; mt < NMT; ++mt) acc[t][mt] = f32x4{0.f, 0.f, 0.f, 0.f};
+    }
 
     wait_for_loads();
     for (; st < steps; st += kRowWaves) {
-      const int next = st + kRowWaves < steps ? st + kRowWaves : st;  // (the last step's loads are repeated)
-      f32x4 sc[1][2] = {{f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}}};
+      const int next = st + kRowWaves;  // (behind the last step: block 0, which all waves read there)
+      f32x4 sc[RT][2];
 #pragma unroll
-      for (int t = 0; t < 2; ++t) {
+      for (int k = 0; k < 2; ++k) {
         bf16x8 kf[NC];
         if constexpr (F8) {
-          const float f = exp2_whole((int8_t)(kx[t] >> (8 * (r & 3))));
+          const float f = exp2_whole((int8_t)(kx[k] >> (8 * (r & 3))));
 #pragma unroll
           for (int i = 0; i < NC / 2; ++i) {
-            const u32x4 w = kraw[t * (NC / 2) + i];
+            const u32x4 w = kraw[k * (NC / 2) + i];
             kf[2 * i] = widen_bf16(w[0], w[1], f);
             kf[2 * i + 1] = widen_bf16(w[2], w[3], f);
           }
         } else {
 #pragma unroll
-          for (int i = 0; i < NC; ++i) kf[i] = __builtin_bit_cast(bf16x8, kraw[t * NC + i]);
+          for (int i = 0; i < NC; ++i) kf[i] = __builtin_bit_cast(bf16x8, kraw[k * NC + i]);
         }
 #pragma unroll
-        for (int i = 0; i < NC; ++i) sc[0][t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[i], qf[i], sc[0][t], 0, 0, 0);
+        for (int t = 0; t < RT; ++t) sc[t][k] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int i = 0; i < NC; ++i)
+#pragma unroll
+          for (int t = 0; t < RT; ++t)
+            sc[t][k] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[i], qf[t][i], sc[t][k], 0, 0, 0);
       }
       // (nothing moves across: the loads take the registers that the keys leave)
       __builtin_amdgcn_sched_barrier(0);
@@ -686,9 +722,13 @@ __global__ __launch_bounds__(64 * kRowWaves, few_per_cu(D)) void attn_few_kernel
       __builtin_amdgcn_sched_barrier(0);
 
       if (!((!DRAFTS || (jb_now + 2) * 16 <= start) && __all(nv_now >= 8))) {  // drafts, or places that hold nothing
-        const uint32_t seen = DRAFTS ? seen_bits(mask, tb_now, start, nv_now) : seen_bits(0, tb_now, tb_now + 8, nv_now);
 #pragma unroll
-        for (int e = 0; e < 8; ++e) sc[0][e / 4][e & 3] = (seen >> e & 1u) ? sc[0][e / 4][e & 3] : kNegInf;
+        for (int t = 0; t < RT; ++t) {
+          const uint32_t seen =
+              DRAFTS ? seen_bits(mask[t], tb_now, start, nv_now) : seen_bits(0, tb_now, tb_now + 8, nv_now);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) sc[t][e / 4][e & 3] = (seen >> e & 1u) ? sc[t][e / 4][e & 3] : kNegInf;
+        }
         // zeros behind the context, so that 0 times what lies there is 0
 #pragma unroll
         for (int mt = 0; mt < NMT; ++mt) vraw[mt] = keep_bytes(vraw[mt], F8 ? nv_now : 2 * nv_now);
@@ -701,58 +741,56 @@ __global__ __launch_bounds__(64 * kRowWaves, few_per_cu(D)) void attn_few_kernel
         if constexpr (F8) vx = keep_bytes(vx, nv_now);
       }
       const u32x2 ve = F8 ? vx ^ 0x80808080u : vx;
-      Weights w[1];
+      Weights w[RT];
       softmax_step<F8>(sc, ve, p.scale_log2, m_run, l_run, acc, w);
       __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
       for (int part = 0; part < Weights::kParts; ++part)
 #pragma unroll
         for (int mt = 0; mt < NMT; ++mt) {
+          VFrag v;
           if constexpr (F8)
-            acc[0][mt] = w[0].mul(part, widen_f16(vraw[mt][0], vraw[mt][1]), acc[0][mt]);
+            v = widen_f16(vraw[mt][0], vraw[mt][1]);
           else
-            acc[0][mt] = w[0].mul(part, __builtin_bit_cast(bf16x8, vraw[mt]), acc[0][mt]);
+            v = __builtin_bit_cast(bf16x8, vraw[mt]);
+#pragma unroll
+          for (int t = 0; t < RT; ++t) acc[t][mt] = w[t].mul(part, v, acc[t][mt]);
         }
       __builtin_amdgcn_sched_barrier(0);
       load_values(next);
     }
 
     // ---- merge the waves, in a fixed order: the upper half deposits, the lower adds ----
-    l_run[0] = row_sum<F8>(l_run[0]);
+#pragma unroll
+    for (int t = 0; t < RT; ++t) l_run[t] = row_sum<F8>(l_run[t]);
 #pragma unroll
     for (int half = kRowWaves / 2; half >= 1; half /= 2) {
-      float* o = so + ((wave % half) * 16 + r) * LDO;
       __syncthreads();
       if (wave >= half && wave < 2 * half) {
 #pragma unroll
-        for (int mt = 0; mt < NMT; ++mt) *reinterpret_cast<f32x4*>(o + mt * 16 + 4 * qg) = acc[0][mt];
-        if (qg == 0) *reinterpret_cast<float2*>(o + D) = make_float2(m_run[0], l_run[0]);
+        for (int t = 0; t < RT; ++t)
+          put_partial<D>(so + (((wave % half) * RT + t) * 16 + r) * LDO, qg, m_run[t], l_run[t], acc[t]);
       }
       __syncthreads();
       if (wave < half) {
-        const float2 ml = *reinterpret_cast<const float2*>(o + D);
-        const float mn = fmaxf(m_run[0], ml.x);
-        const float mu = (mn == kNegInf) ? 0.f : mn;
-        const float wa = fast_exp2(m_run[0] - mu), wb = fast_exp2(ml.x - mu);
-        l_run[0] = times_exp2(l_run[0], m_run[0] - mu) + times_exp2(ml.y, ml.x - mu);
-        m_run[0] = mn;
 #pragma unroll
-        for (int mt = 0; mt < NMT; ++mt)
-          acc[0][mt] = acc[0][mt] * wa + *reinterpret_cast<const f32x4*>(o + mt * 16 + 4 * qg) * wb;
+        for (int t = 0; t < RT; ++t)
+          add_partial<D>(so + ((wave * RT + t) * 16 + r) * LDO, qg, m_run[t], l_run[t], acc[t]);
       }
     }
     if (wave == 0) {
       if (lane == 0 && (int)blockIdx.x == c.first)
         p.span[((size_t)b * p.Hkv + c.kvh) * p.max_passes + c.pass] = make_int2(c.first, c.last);
-      store_rows<D>(p, s, c, c.row0 + r, qg, m_run[0], l_run[0], acc[0]);
+#pragma unroll
+      for (int t = 0; t < RT; ++t) store_rows<D>(p, s, c, c.row0 + t * 16 + r, qg, m_run[t], l_run[t], acc[t]);
     }
   }
   if constexpr (DRAFTS) add_odd<D, F8, 2>(kFewLeast, s_odd);
 }
 
 // ---------------------------------------------------------------------------
-// More rows, WR waves on row tiles of their own, and 4 / WR on halves of a step's
-// tokens: up to 64 rows WR = 2 (two tiles a wave share what it reads from LDS), else 4.
+// More rows (bf16 cache: from 17), WR waves on row tiles of their own, and 4 / WR on
+// halves of a step's tokens: up to 64 rows WR = 2 (two tiles a wave share what it reads from LDS), else 4.
 // A step is 64 tokens (four blocks) of the work-group. Its threads load
 // the tiles as they lie (16 bytes each, whole 128-byte lines), a step ahead, and put
 // them into LDS as 16-bit operands: K [token][D] with the tokens in the order of the
@@ -1005,28 +1043,14 @@ __global__ __launch_bounds__(64 * kRowWaves, kManyPerCu) void attn_many_kernel(R
         lds_barrier();
         if (half == 1) {
 #pragma unroll
-          for (int t = 0; t < N; ++t) {
-            float* o = so + ((group * kTiles + t) * 16 + r) * LDO;
-#pragma unroll
-            for (int mt = 0; mt < NMT; ++mt) *reinterpret_cast<f32x4*>(o + mt * 16 + 4 * qg) = acc[t][mt];
-            if (qg == 0) *reinterpret_cast<float2*>(o + D) = make_float2(m_run[t], l_run[t]);
-          }
+          for (int t = 0; t < N; ++t)
+            put_partial<D>(so + ((group * kTiles + t) * 16 + r) * LDO, qg, m_run[t], l_run[t], acc[t]);
         }
         lds_barrier();
         if (half == 0) {
 #pragma unroll
-          for (int t = 0; t < N; ++t) {
-            const float* o = so + ((group * kTiles + t) * 16 + r) * LDO;
-            const float2 ml = *reinterpret_cast<const float2*>(o + D);
-            const float mn = fmaxf(m_run[t], ml.x);
-            const float mu = (mn == kNegInf) ? 0.f : mn;
-            const float wa = fast_exp2(m_run[t] - mu), wb = fast_exp2(ml.x - mu);
-            l_run[t] = times_exp2(l_run[t], m_run[t] - mu) + times_exp2(ml.y, ml.x - mu);
-            m_run[t] = mn;
-#pragma unroll
-            for (int mt = 0; mt < NMT; ++mt)
-              acc[t][mt] = acc[t][mt] * wa + *reinterpret_cast<const f32x4*>(o + mt * 16 + 4 * qg) * wb;
-          }
+          for (int t = 0; t < N; ++t)
+            add_partial<D>(so + ((group * kTiles + t) * 16 + r) * LDO, qg, m_run[t], l_run[t], acc[t]);
         }
       }
       if (half == 0) {
@@ -1151,10 +1175,12 @@ __global__ __launch_bounds__(256) void attn_rows_merge_many_kernel(RowsParams p)
 // Host side.
 namespace {
 
-// What a launch takes: tiles 0 is the kernel for up to 16 rows, 1 that for up to 64, 2
-// that for more.
+// What a launch takes: the kernel for few rows with one or two row tiles, or the one
+// for more rows with two or four waves on them.
+enum RowsKind { kFewOne, kFewTwo, kManyTwo, kManyFour };
 struct RowsPlan {
-  int tiles, pass_tiles, passes, pass_rows, grid;
+  RowsKind kind;
+  int pass_tiles, passes, pass_rows, grid;
   bool whole;  // a work-group per unit, no merge
 };
 
@@ -1198,11 +1224,11 @@ long long positions_bound(const RowsShape& s, int passes) {
 RowsPlan rows_plan(const RowsShape& s) {
   RowsPlan r;
   const int rows = s.max_n * (s.Hq / s.Hkv), all = (rows + 15) / 16;
-  r.tiles = all <= 1 ? 0 : all <= kRowWaves ? 1 : kTiles;
-  r.pass_tiles = r.tiles == 0 ? 1 : r.tiles * kRowWaves;
+  r.kind = all <= 1 ? kFewOne : all <= 2 && s.f8 ? kFewTwo : all <= 2 * kTiles ? kManyTwo : kManyFour;
+  r.pass_tiles = r.kind == kFewOne ? 1 : r.kind == kFewTwo ? 2 : r.kind == kManyTwo ? 2 * kTiles : 4 * kTiles;
   r.passes = all > r.pass_tiles ? (all + r.pass_tiles - 1) / r.pass_tiles : 1;
   r.pass_rows = rows < r.pass_tiles * 16 ? rows : r.pass_tiles * 16;
-  const long long most = (long long)compute_units() * (r.tiles == 0 ? few_per_cu(s.D) : kManyPerCu);
+  const long long most = (long long)compute_units() * (r.kind == kFewOne ? few_per_cu(s.D, 1) : r.kind == kFewTwo ? few_per_cu(s.D, 2) : kManyPerCu);
   const long long units = (long long)s.B * s.Hkv * r.passes;
   r.whole = (s.max_ctx <= kWholeCtx && units <= most) || (s.max_ctx <= kWholeManyCtx && 4 * units >= 3 * most);
   const long long P = r.whole ? units : (positions_bound(s, r.passes) + 7) / 8;
@@ -1218,10 +1244,12 @@ template <int D, bool F8>
 void launch_tiles(const RowsParams& p, const RowsPlan& r, hipStream_t stream) {
   const dim3 grid(r.grid), block(64 * kRowWaves);
   if (!p.cu)
-    attn_few_kernel<D, true, false><<<grid, block, 0, stream>>>(p);
-  else if (r.tiles == 0)
-    attn_few_kernel<D, F8, true><<<grid, block, 0, stream>>>(p);
-  else if (r.tiles == 1)
+    attn_few_kernel<D, true, false, 1><<<grid, block, 0, stream>>>(p);
+  else if (r.kind == kFewOne)
+    attn_few_kernel<D, F8, true, 1><<<grid, block, 0, stream>>>(p);
+  else if (r.kind == kFewTwo)
+    attn_few_kernel<D, true, true, 2><<<grid, block, 0, stream>>>(p);
+  else if (r.kind == kManyTwo)
     attn_many_kernel<D, F8, 2><<<grid, block, 0, stream>>>(p);
   else
     attn_many_kernel<D, F8, 4><<<grid, block, 0, stream>>>(p);
