@@ -22,11 +22,11 @@
 // 16 bits. (One bf16 value, 8 bits, would show beside the output's own rounding:
 // 2.1e-3 of the norm instead of 1.65e-3.)
 //
-// Two kernels. Up to 16 rows (decode attention; 8-bit cache: 32): the waves of a work-group take the
-// tokens in turns, keys and values go from memory straight into the matrix
-// operands' registers, a step ahead. More rows: the waves share the tokens, 64 a
-// step, which the work-group turns into 16-bit operands in LDS once, and each has
-// row tiles of its own.
+// Two kernels. Up to 16 rows (decode attention; 8-bit cache: 32, with D = 64 also 64):
+// the waves of a work-group take the tokens in turns, keys and values go from memory
+// straight into the matrix operands' registers, a step ahead. More rows: the waves share
+// the tokens, 64 a step, which the work-group turns into 16-bit operands in LDS once, and
+// each has row tiles of its own.
 //
 // The blocks of all units (sequence, kv head, pass over the rows) are laid end to
 // end, and each work-group takes a consecutive range of them, so that long and
@@ -563,7 +563,7 @@ struct BlockIds {
 // with the loads of the next step.
 __device__ __forceinline__ void wait_for_loads() { __builtin_amdgcn_s_waitcnt(0x0f70); }  // vmcnt(0)
 
-// Work-groups that a CU holds at once. Few rows: two, D = 64 three (at D = 128 a third
+// Work-groups that a CU holds at once. Few rows: two, one tile of D = 64 three (at D = 128 a third
 // costs the registers of the step ahead: 139.9 us instead of 136.8 for 64 sequences,
 // 153.7 instead of 145.8 for one of 400000).
 constexpr int few_per_cu(int D, int RT) { return D == 64 && RT == 1 ? 3 : 2; }
@@ -571,7 +571,7 @@ constexpr int few_per_cu(int D, int RT) { return D == 64 && RT == 1 ? 3 : 2; }
 // Least positions of a work-group: a step for each wave, two steps.
 constexpr int kFewLeast = 2 * kRowWaves, kManyLeast = 8;
 
-// More rows: by registers.
+// More rows, or tiles: by registers.
 constexpr int kManyPerCu = 2;
 
 }  // namespace
@@ -582,8 +582,10 @@ constexpr int kManyPerCu = 2;
 // may differ in the tokens that they see. Two tiles for an 8-bit cache alone: 4 drafts
 // of 64 / 8 heads x 128 over 400000 tokens 149.6 us instead of the other kernel's 166, of
 // 32 / 4 x 64 in 32 sequences 30.1 instead of 35.4; over bf16, whose step ahead takes
-// twice the registers, 145.6 instead of 135.4 (200000 tokens). Four tiles, one
-// work-group a CU: 118 us for 32 sequences with 8 drafts instead of 96.
+// twice the registers, 145.6 instead of 135.4 (200000 tokens). Four tiles where D = 64:
+// 8 drafts of 32 / 4 heads over 400000 tokens 63.7 us instead of 77.5, in 32 sequences
+// 40.8 instead of 42.5; where D = 128 they would take the registers of a second
+// work-group a CU (118 us for 32 sequences with 8 drafts instead of 96).
 template <int D, bool F8, bool DRAFTS, int RT>
 __global__ __launch_bounds__(64 * kRowWaves, few_per_cu(D, RT)) void attn_few_kernel(RowsParams p) {
   constexpr int NC = D / 32;       // k-chunks of the first product
@@ -789,7 +791,7 @@ __global__ __launch_bounds__(64 * kRowWaves, few_per_cu(D, RT)) void attn_few_ke
 }
 
 // ---------------------------------------------------------------------------
-// More rows (bf16 cache: from 17), WR waves on row tiles of their own, and 4 / WR on
+// More rows, WR waves on row tiles of their own, and 4 / WR on
 // halves of a step's tokens: up to 64 rows WR = 2 (two tiles a wave share what it reads from LDS), else 4.
 // A step is 64 tokens (four blocks) of the work-group. Its threads load
 // the tiles as they lie (16 bytes each, whole 128-byte lines), a step ahead, and put
@@ -1175,9 +1177,9 @@ __global__ __launch_bounds__(256) void attn_rows_merge_many_kernel(RowsParams p)
 // Host side.
 namespace {
 
-// What a launch takes: the kernel for few rows with one or two row tiles, or the one
-// for more rows with two or four waves on them.
-enum RowsKind { kFewOne, kFewTwo, kManyTwo, kManyFour };
+// What a launch takes: the kernel for few rows with one, two or four row tiles, or the
+// one for more rows with two or four waves on them.
+enum RowsKind { kFewOne, kFewTwo, kFewFour, kManyTwo, kManyFour };
 struct RowsPlan {
   RowsKind kind;
   int pass_tiles, passes, pass_rows, grid;
@@ -1196,6 +1198,7 @@ constexpr int kRowsUnitCost = 8;
 // drafts: 61.7 and 71.4).
 constexpr int kWholeCtx = 512;
 constexpr int kWholeManyCtx = 2048;
+constexpr long long kWholeUnits = 1ll << 23;  // (a launch has less than 2^32 threads)
 
 // Pieces per unit from which the merge shares a unit's pieces among lanes, if there are
 // few rows: at most kFewRows a CU (one row of 64 heads in 64 pieces: 139.6 us in all, 148.5
@@ -1224,13 +1227,20 @@ long long positions_bound(const RowsShape& s, int passes) {
 RowsPlan rows_plan(const RowsShape& s) {
   RowsPlan r;
   const int rows = s.max_n * (s.Hq / s.Hkv), all = (rows + 15) / 16;
-  r.kind = all <= 1 ? kFewOne : all <= 2 && s.f8 ? kFewTwo : all <= 2 * kTiles ? kManyTwo : kManyFour;
-  r.pass_tiles = r.kind == kFewOne ? 1 : r.kind == kFewTwo ? 2 : r.kind == kManyTwo ? 2 * kTiles : 4 * kTiles;
+  r.kind = kManyFour;
+  if (all <= 1)
+    r.kind = kFewOne;
+  else if (all <= 2 && s.f8)
+    r.kind = kFewTwo;
+  else if (all <= 2 * kTiles)
+    r.kind = s.f8 && s.D == 64 ? kFewFour : kManyTwo;
+  r.pass_tiles = r.kind == kFewOne ? 1 : r.kind == kFewTwo ? 2 : r.kind == kManyFour ? 4 * kTiles : 4;
   r.passes = all > r.pass_tiles ? (all + r.pass_tiles - 1) / r.pass_tiles : 1;
   r.pass_rows = rows < r.pass_tiles * 16 ? rows : r.pass_tiles * 16;
-  const long long most = (long long)compute_units() * (r.kind == kFewOne ? few_per_cu(s.D, 1) : r.kind == kFewTwo ? few_per_cu(s.D, 2) : kManyPerCu);
+  const long long most = (long long)compute_units() * (r.kind == kFewOne ? few_per_cu(s.D, 1) : kManyPerCu);
   const long long units = (long long)s.B * s.Hkv * r.passes;
-  r.whole = (s.max_ctx <= kWholeCtx && units <= most) || (s.max_ctx <= kWholeManyCtx && 4 * units >= 3 * most);
+  r.whole = (s.max_ctx <= kWholeCtx && units <= most) ||
+            (s.max_ctx <= kWholeManyCtx && 4 * units >= 3 * most && units <= kWholeUnits);
   const long long P = r.whole ? units : (positions_bound(s, r.passes) + 7) / 8;
   r.grid = (int)(P < 1 ? 1 : P < most || r.whole ? P : most);
   return r;
@@ -1249,6 +1259,8 @@ void launch_tiles(const RowsParams& p, const RowsPlan& r, hipStream_t stream) {
     attn_few_kernel<D, F8, true, 1><<<grid, block, 0, stream>>>(p);
   else if (r.kind == kFewTwo)
     attn_few_kernel<D, true, true, 2><<<grid, block, 0, stream>>>(p);
+  else if (r.kind == kFewFour)
+    attn_few_kernel<64, true, true, 4><<<grid, block, 0, stream>>>(p);
   else if (r.kind == kManyTwo)
     attn_many_kernel<D, F8, 2><<<grid, block, 0, stream>>>(p);
   else
