@@ -35,12 +35,12 @@
 //
 // Bounds, and what was measured (caches that no call has read just before; 8-bit and
 // 64 / 8 heads x 128 but where it says otherwise). Decode attention: the cache's bytes.
-// 64 sequences of median 4096 tokens, 740 MB: 134.3 us, 5.5 TB/s; one of 400000, 826
-// MB: 139.2 us, 5.9 TB/s, where loads alone reach 6.4. Trees: the chain of a step
+// 64 sequences of median 4096 tokens, 740 MB: 132.4 us, 5.6 TB/s; one of 400000, 826
+// MB: 139.4 us, 5.9 TB/s, where loads alone reach 6.4. Trees: the chain of a step
 // (barrier, widening into LDS, barrier, operands, products, softmax, products) with two
-// waves on a SIMD. 32 sequences of median 4096 tokens, up to 8 drafts each, 328 MB: 96
-// us, 3.4 TB/s, the vector units busy for 41% of it, the matrix units 18%, LDS 39%; one
-// context of 65536 with 64 drafts: 196 us, 0.70 PFLOP/s (a large matrix product reaches
+// waves on a SIMD. 32 sequences of median 4096 tokens, up to 8 drafts each, 328 MB: 93
+// us, 3.5 TB/s, the vector units busy for 41% of it, the matrix units 18%, LDS 39%; one
+// context of 65536 with 64 drafts: 190 us, 0.72 PFLOP/s (a large matrix product reaches
 // 1.41), 52%, 31% and 44%; 8 sequences of median 8192, up to 32 drafts, 32 / 8 heads,
 // bf16, 301 MB: 83 us, 3.6 TB/s.
 #include <math.h>
@@ -1186,7 +1186,10 @@ struct RowsPlan {
   bool whole;  // a work-group per unit, no merge
 };
 
-constexpr int kRowsUnitCost = 8;
+// Blocks that a unit's piece is charged for (its queries, merge of waves, partials). 8
+// and 24 instead: 64 sequences of decode attention 134.3 and 133.1 us, now 132.4; 32 with 8
+// drafts 96.4 and 94.1, now 93.5.
+constexpr int kRowsUnitCost = 16;
 
 // Units take a work-group each, without partials and the merge's launch, where
 // contexts are at most kWholeCtx and one round of work-groups holds all units (4
