@@ -39,9 +39,9 @@
 // MB: 139.4 us, 5.9 TB/s, where loads alone reach 6.4. Trees: the chain of a step
 // (barrier, widening into LDS, barrier, operands, products, softmax, products) with two
 // waves on a SIMD. 32 sequences of median 4096 tokens, up to 8 drafts each, 328 MB: 93
-// us, 3.5 TB/s, the vector units busy for 41% of it, the matrix units 18%, LDS 39%; one
+// us, 3.5 TB/s, the vector units busy for 42% of it, the matrix units 19%, LDS 34%; one
 // context of 65536 with 64 drafts: 190 us, 0.72 PFLOP/s (a large matrix product reaches
-// 1.41), 52%, 31% and 44%; 8 sequences of median 8192, up to 32 drafts, 32 / 8 heads,
+// 1.41), 53%, 32% and 33%; 8 sequences of median 8192, up to 32 drafts, 32 / 8 heads,
 // bf16, 301 MB: 83 us, 3.6 TB/s.
 #include <math.h>
 
