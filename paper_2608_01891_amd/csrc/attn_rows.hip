@@ -42,7 +42,7 @@
 // us, 3.5 TB/s, the vector units busy for 42% of it, the matrix units 19%, LDS 34%; one
 // context of 65536 with 64 drafts: 190 us, 0.72 PFLOP/s (a large matrix product reaches
 // 1.41), 53%, 32% and 33%; 8 sequences of median 8192, up to 32 drafts, 32 / 8 heads,
-// bf16, 301 MB: 83 us, 3.6 TB/s.
+// bf16, 301 MB: 81 us, 3.7 TB/s.
 #include <math.h>
 
 #include <atomic>
