@@ -298,6 +298,22 @@ __device__ __forceinline__ V keep_bytes(V v, int n) {
   return v;
 }
 
+// Exponents (bytes) as they can be, -100 to 120. Those of tokens that no row sees may hold
+// anything, and a weight of 0 does not take away a 2^e that is not finite.
+constexpr int kLeastExp = -100, kMostExp = 120;
+
+__device__ __forceinline__ u32x2 legal_exponents(u32x2 v) {
+  typedef int16_t i16x2 __attribute__((ext_vector_type(2)));
+  const auto limit = [](uint32_t x) {  // the high byte of each half
+    const i16x2 least = {kLeastExp * 256, kLeastExp * 256}, most = {kMostExp * 256, kMostExp * 256};
+    return __builtin_bit_cast(
+        uint32_t, __builtin_elementwise_min(__builtin_elementwise_max(__builtin_bit_cast(i16x2, x), least), most));
+  };
+#pragma unroll
+  for (int i = 0; i < 2; ++i) v[i] = limit(v[i] & 0xff00ff00u) | limit(v[i] << 8 & 0xff00ff00u) >> 8;
+  return v;
+}
+
 // Which of the 8 tokens from place `tb` on a draft with these mask bits sees, as
 // bits; the first nv of them are cached, and the sequence's drafts start at `start`.
 __device__ __forceinline__ uint32_t seen_bits(uint64_t mask, int tb, int start, int nv) {
@@ -741,6 +757,7 @@ __global__ __launch_bounds__(64 * kRowWaves, few_per_cu(D, RT)) void attn_few_ke
           if (odd) s_odd[wave] = 1;
         }
         if constexpr (F8) vx = keep_bytes(vx, nv_now);
+        if constexpr (F8 && DRAFTS) vx = legal_exponents(vx);
       }
       const u32x2 ve = F8 ? vx ^ 0x80808080u : vx;
       Weights w[RT];
@@ -907,7 +924,7 @@ __global__ __launch_bounds__(64 * kRowWaves, kManyPerCu) void attn_many_kernel(R
         for (int i = 0; i < NL; ++i) {
           const int k = blk(i), nv = k == 0 ? n0 : k == 1 ? n1 : k == 2 ? n2 : n3;
           vraw[i] = without_odd<F8>(keep_bytes(vraw[i], F8 ? nv : 2 * (nv - (within(i) & 1) * 8)), odd);
-          if constexpr (F8) vx[i] = (lane & 15) < nv ? vx[i] : 0;
+          if constexpr (F8) vx[i] = (lane & 15) < nv ? min(max(vx[i], kLeastExp), kMostExp) : 0;
         }
         if (odd) s_odd[wave] = 1;
       }

@@ -467,6 +467,30 @@ def test_values_of_any_size(gpu_lib, heads, counts, order):
     _check_attn(got, ref, 6000, heads[2], exps=128)
 
 
+# A group of heads for each of the kernels that six drafts of an 8-bit cache take.
+KERNELS = [(2, 1, 64), (4, 1, 128), (8, 1, 64), (8, 1, 128), (14, 1, 128)]
+
+
+@pytest.mark.parametrize("heads", KERNELS)
+@pytest.mark.parametrize("ctx", [6, 39, 6001])
+@pytest.mark.parametrize("exp", [127, 121, -101, -128])
+def test_exponents_of_drafts_that_nobody_sees(gpu_lib, heads, ctx, exp):
+    """Whatever a cached draft holds that no row sees, rows that see nothing among them."""
+    counts, lens = [6, 3], [ctx, 20]
+    a, b = (_cache(113, heads, lens, True) for _ in range(2))
+    masks = _trees(114, counts) & ~(1 << 4) | 1  # nobody sees draft 4
+    masks[1] = 0
+    place = ctx - 2
+    blk, o = int(b.block_table[0, place // 16]), place % 16
+    b.kv_exp[blk, :, :, o] = exp
+    b.k_cache.view(torch.uint8)[blk, :, o] = 0x7f
+    b.v_cache.view(torch.uint8)[blk, :, :, o] = torch.tensor([0x7f, 0x7e, 0xfe, 0x00] * (heads[2] // 4), dtype=torch.uint8)
+    clean, ref = _tree(a, counts, 115, masks)
+    _check_attn(clean, ref, ctx, heads[2])
+    got, _ = _tree(b, counts, 115, masks)
+    assert torch.equal(got, clean)
+
+
 @pytest.mark.parametrize("f8", [False, True])
 @pytest.mark.parametrize("heads,most", [((8, 8, 64), 1), ((64, 8, 128), 2), ((64, 8, 128), 6), ((32, 4, 64), 16)])
 def test_units_that_share_work_groups(gpu_lib, f8, heads, most):
