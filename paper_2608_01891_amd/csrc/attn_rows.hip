@@ -453,13 +453,18 @@ __device__ __forceinline__ float times_exp2(float x, float d) {
 
 constexpr float kSlack = 8.f;
 
+// Of a value's exponent where it is a byte (9 to 229), and what the weights' sum counts u in.
+constexpr int kExpBias = 109;
+constexpr float kSumUnit = 0x1p-18f;  // 2^(kExpBias - 127)
+
 // The softmax of N row tiles over 8 tokens per lane: scores x (masked: -inf) to
 // weights, the references m and sums l, and the accumulators' rescaling.
-// F8: ve holds the tokens' value exponents, a byte each with 128 added, in the
-// references too. p = 2^(s - m) joins the sum; one shift makes 2^(e + 1) of the byte,
-// and P' = p 2^(e + 1), so the sum is doubled at the end. p is 2^-e where P' is
-// largest: it stays within floats, and what of the sum is too small for them is below
-// 2^(e - 126) of that.
+// F8: ve holds the tokens' value exponents, a byte each with kExpBias added, in the
+// references too. u = 2^(s - m + 128) is 2^(19 - e) where P' is largest; one shift makes
+// 2^(e - 18) of the byte, and P' = u 2^(e - 18). The sum is that of u 2^-18, product and sum
+// in one instruction. No u overflows for an e of -100; exp2 gives nothing below 2^-126, so that
+// what the sum loses is below 2^-25 of the largest p where that token's e is 120, and a bit less
+// for each below. (The sum itself is 2^-119 or more, and floats below 2^-126 count.)
 template <bool F8, int N, int NMT, class Weights>
 __device__ __forceinline__ void softmax_step(f32x4 (&x)[N][2], u32x2 ve, float scale_log2, float (&m)[N], float (&l)[N],
                                              f32x4 (&acc)[N][NMT], Weights (&w)[N]) {
@@ -503,14 +508,17 @@ __device__ __forceinline__ void softmax_step(f32x4 (&x)[N][2], u32x2 ve, float s
   for (int e = 0; e < 8; e += 2) {
     float f[2];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) f[i] = F8 ? __uint_as_float(byte(e + i) << 23) : 1.f;  // 2^(exponent + 1)
+    for (int i = 0; i < 2; ++i) f[i] = F8 ? __uint_as_float(byte(e + i) << 23) : 1.f;  // 2^(exponent - 18)
 #pragma unroll
     for (int t = 0; t < N; ++t) {
       float u[2];
 #pragma unroll
       for (int i = 0; i < 2; ++i) {
         u[i] = fast_exp2(fmaf(x[t][(e + i) / 4][(e + i) & 3], scale_log2, -m_use[t]));
-        ps[t][i] = e == 0 ? u[i] : ps[t][i] + u[i];
+        if constexpr (F8)
+          ps[t][i] = e == 0 ? u[i] * kSumUnit : fmaf(u[i], kSumUnit, ps[t][i]);
+        else
+          ps[t][i] = e == 0 ? u[i] : ps[t][i] + u[i];
         if constexpr (F8) u[i] *= f[i];
       }
       w[t].set(e, u[0], u[1]);
@@ -521,11 +529,10 @@ __device__ __forceinline__ void softmax_step(f32x4 (&x)[N][2], u32x2 ve, float s
 }
 
 // A row's sum over the lanes that hold it.
-template <bool F8>
 __device__ __forceinline__ float row_sum(float l) {
   l += __shfl_xor(l, 16);
   l += __shfl_xor(l, 32);
-  return F8 ? l + l : l;
+  return l;
 }
 
 // A lane's share of a row's partial to LDS and from there to another wave's: O, then (m, l).
@@ -759,7 +766,7 @@ __global__ __launch_bounds__(64 * kRowWaves, few_per_cu(D, RT)) void attn_few_ke
         if constexpr (F8) vx = keep_bytes(vx, nv_now);
         if constexpr (F8 && DRAFTS) vx = legal_exponents(vx);
       }
-      const u32x2 ve = F8 ? vx ^ 0x80808080u : vx;
+      const u32x2 ve = F8 ? (vx ^ 0x80808080u) - (128 - kExpBias) * 0x01010101u : vx;  // (no byte borrows)
       Weights w[RT];
       softmax_step<F8>(sc, ve, p.scale_log2, m_run, l_run, acc, w);
       __builtin_amdgcn_sched_barrier(0);
@@ -781,7 +788,7 @@ __global__ __launch_bounds__(64 * kRowWaves, few_per_cu(D, RT)) void attn_few_ke
 
     // ---- merge the waves, in a fixed order: the upper half deposits, the lower adds ----
 #pragma unroll
-    for (int t = 0; t < RT; ++t) l_run[t] = row_sum<F8>(l_run[t]);
+    for (int t = 0; t < RT; ++t) l_run[t] = row_sum(l_run[t]);
 #pragma unroll
     for (int half = kRowWaves / 2; half >= 1; half /= 2) {
       __syncthreads();
@@ -833,7 +840,7 @@ __global__ __launch_bounds__(64 * kRowWaves, kManyPerCu) void attn_many_kernel(R
   typedef std::conditional_t<F8, f16x8, bf16x8> VFrag;
   constexpr int kTileBytes = (64 * LDK + D * LDV) * 2, kPartBytes = TS == 2 ? WR * kTiles * 16 * LDO * 4 : 0;
   __shared__ __attribute__((aligned(16))) uint8_t sm[kTileBytes > kPartBytes ? kTileBytes : kPartBytes];
-  __shared__ __attribute__((aligned(16))) uint8_t sx[F8 ? 64 : 8];  // the values' exponents, 128 added
+  __shared__ __attribute__((aligned(16))) uint8_t sx[F8 ? 64 : 8];  // the values' exponents, kExpBias added
   __shared__ int s_odd[kRowWaves];
   uint16_t* sk = reinterpret_cast<uint16_t*>(sm);
   uint16_t* sv = sk + 64 * LDK;
@@ -942,7 +949,7 @@ __global__ __launch_bounds__(64 * kRowWaves, kManyPerCu) void attn_many_kernel(R
           uint16_t* vd = sv + w * LDV + k * 16;
           *reinterpret_cast<f16x8*>(vd) = widen_f16(v[0], v[1]);
           *reinterpret_cast<f16x8*>(vd + 8) = widen_f16(v[2], v[3]);
-          if (heads_block(i) && lane < 16) sx[k * 16 + lane] = (uint8_t)(vx[i] + 128);
+          if (heads_block(i) && lane < 16) sx[k * 16 + lane] = (uint8_t)(vx[i] + kExpBias);
         } else {
           *reinterpret_cast<u32x4*>(kd) = kraw[i];
           *reinterpret_cast<u32x4*>(sv + (w >> 1) * LDV + k * 16 + (w & 1) * 8) = v;
@@ -1057,7 +1064,7 @@ __global__ __launch_bounds__(64 * kRowWaves, kManyPerCu) void attn_many_kernel(R
         }
       }
 #pragma unroll
-      for (int t = 0; t < N; ++t) l_run[t] = row_sum<F8>(l_run[t]);
+      for (int t = 0; t < N; ++t) l_run[t] = row_sum(l_run[t]);
       if constexpr (TS == 2) {  // the second half's waves deposit, the first half's add
         lds_barrier();
         if (half == 1) {

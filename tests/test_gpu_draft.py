@@ -491,6 +491,46 @@ def test_exponents_of_drafts_that_nobody_sees(gpu_lib, heads, ctx, exp):
     assert torch.equal(got, clean)
 
 
+def _peak(heads, ctx, above, big, seed, exps=None):
+    """A cache whose token 0 lies `above` (log2) over the others of each sequence, which are all alike in their
+    scores, with the queries and the scale for it; token 0's values are zero but for channel 0."""
+    c = _cache(seed, heads, [ctx, 40], True)
+    for t in (c.k_cache, c.v_cache):
+        t.view(torch.uint8).fill_(0)
+    c.kv_exp.zero_()
+    if exps is not None:
+        c.kv_exp[:, :, 1] = exps
+    c.v_cache.view(torch.uint8).fill_(big)
+    for b in range(2):
+        blk = int(c.block_table[b, 0])
+        c.k_cache.view(torch.uint8)[blk, :, 0, 0] = 0x38  # 1
+        c.v_cache.view(torch.uint8)[blk, :, 1:, 0] = 0
+    q = torch.zeros(9, heads[0], heads[2], dtype=torch.bfloat16)
+    q[:, :, 0] = 1.0
+    return c, q, above * 0.6931471805599453
+
+
+@pytest.mark.parametrize("heads", KERNELS)
+@pytest.mark.parametrize("exp", [104, 112, 120])
+@pytest.mark.parametrize("kind", ["flat", "peak", "beside -100"])
+def test_values_of_the_largest_exponents(gpu_lib, heads, exp, kind):
+    """Value rows of up to 2^120: many light tokens hold much of the weight."""
+    lens, counts = [6001, 40], [6, 3]
+    if kind == "peak":
+        c, q, scale = _peak(heads, 6001, 18.3, 0x38, 117, exp)
+    else:
+        c, q, scale = _cache(117, heads, lens, True), None, 0.0
+        e = c.kv_exp[:, :, 1]
+        e.fill_(exp)
+        codes = c.v_cache.view(torch.uint8)
+        codes.copy_(torch.where(codes & 0x7f > 0x38, 0x34, codes).to(torch.uint8))  # (what they stand for is finite)
+        if kind == "beside -100":
+            e.masked_fill_(torch.randint(0, 2, e.shape, generator=torch.Generator().manual_seed(118)) == 0, -100)
+    got, ref = _tree(c, counts, 119, None, q=q, scale=scale)
+    assert bool(got.isfinite().all())
+    _check_attn(got, ref, 6001, heads[2], exps=128)
+
+
 @pytest.mark.parametrize("f8", [False, True])
 @pytest.mark.parametrize("heads,most", [((8, 8, 64), 1), ((64, 8, 128), 2), ((64, 8, 128), 6), ((32, 4, 64), 16)])
 def test_units_that_share_work_groups(gpu_lib, f8, heads, most):
