@@ -16,7 +16,7 @@
 // 8-bit rows are c 2^e. A key's codes become bf16 with its 2^e on the way, exactly.
 // A value's exponent joins the weight: P' = p 2^e enters the product with the codes
 // as fp16, exactly, and the row's sum is that of p. p = 2^(s - M') with M' the
-// largest s + e, to within 2^kSlack: the largest contribution has a P' of 2 to 2^9,
+// largest s + e, to within 2^kSlack: the largest contribution has a P' of 2^7 to 2^15,
 // and P' is rounded to fp16 (11 bits; below 2^-14 steps of 2^-24). Over a bf16 cache
 // a weight enters as two bf16 values, the rounded weight and what its rounding left:
 // 16 bits. (One bf16 value, 8 bits, would show beside the output's own rounding:
@@ -453,18 +453,21 @@ __device__ __forceinline__ float times_exp2(float x, float d) {
 
 constexpr float kSlack = 8.f;
 
-// Of a value's exponent where it is a byte (9 to 229), and what the weights' sum counts u in.
-constexpr int kExpBias = 109;
-constexpr float kSumUnit = 0x1p-18f;  // 2^(kExpBias - 127)
+// Of a value's exponent where it is a byte (15 to 235); what the weights' sum counts u in, and
+// what that takes of the product at the end: 2^(kExpBias - 127) in all.
+constexpr int kExpBias = 115;
+constexpr float kSumUnit = 0x1p-20f, kProductUnit = 0x1p-8f;
 
 // The softmax of N row tiles over 8 tokens per lane: scores x (masked: -inf) to
 // weights, the references m and sums l, and the accumulators' rescaling.
 // F8: ve holds the tokens' value exponents, a byte each with kExpBias added, in the
-// references too. u = 2^(s - m + 128) is 2^(19 - e) where P' is largest; one shift makes
-// 2^(e - 18) of the byte, and P' = u 2^(e - 18). The sum is that of u 2^-18, product and sum
-// in one instruction. No u overflows for an e of -100; exp2 gives nothing below 2^-126, so that
-// what the sum loses is below 2^-25 of the largest p where that token's e is 120, and a bit less
-// for each below. (The sum itself is 2^-119 or more, and floats below 2^-126 count.)
+// references too. u = 2^(s - m + 134) is 2^(19 - e) where P' is largest; one shift makes
+// 2^(e - 12) of the byte, and P' = u 2^(e - 12), at least 2^7 there: fp16 holds 11 bits of
+// weights down to 2^-21 of the largest, and what it drops is below 2^-32 of that. The sum is
+// that of u 2^-20, product and sum in one instruction. No u overflows for an e of -100; exp2
+// gives nothing below 2^-126, so that what the sum loses is below 2^-25 of the largest p where
+// that token's e is 120, and a bit less for each below. (The sum itself is 2^-121 or more, and
+// floats below 2^-126 count. At e = -100 it holds 2^20 tokens.)
 template <bool F8, int N, int NMT, class Weights>
 __device__ __forceinline__ void softmax_step(f32x4 (&x)[N][2], u32x2 ve, float scale_log2, float (&m)[N], float (&l)[N],
                                              f32x4 (&acc)[N][NMT], Weights (&w)[N]) {
@@ -502,13 +505,13 @@ __device__ __forceinline__ void softmax_step(f32x4 (&x)[N][2], u32x2 ve, float s
   }
   float m_use[N];
 #pragma unroll
-  for (int t = 0; t < N; ++t) m_use[t] = m[t] == kNegInf ? 0.f : F8 ? m[t] - 128.f : m[t];
+  for (int t = 0; t < N; ++t) m_use[t] = m[t] == kNegInf ? 0.f : F8 ? m[t] - 134.f : m[t];
   float ps[N][2];
 #pragma unroll
   for (int e = 0; e < 8; e += 2) {
     float f[2];
 #pragma unroll
-    for (int i = 0; i < 2; ++i) f[i] = F8 ? __uint_as_float(byte(e + i) << 23) : 1.f;  // 2^(exponent - 18)
+    for (int i = 0; i < 2; ++i) f[i] = F8 ? __uint_as_float(byte(e + i) << 23) : 1.f;  // 2^(exponent - 12)
 #pragma unroll
     for (int t = 0; t < N; ++t) {
       float u[2];
@@ -528,11 +531,14 @@ __device__ __forceinline__ void softmax_step(f32x4 (&x)[N][2], u32x2 ve, float s
   for (int t = 0; t < N; ++t) l[t] += ps[t][0] + ps[t][1];
 }
 
-// A row's sum over the lanes that hold it.
-__device__ __forceinline__ float row_sum(float l) {
+// A row's sum over the lanes that hold it, and its product in the same unit.
+template <bool F8, int NMT>
+__device__ __forceinline__ void finish_row(float& l, f32x4 (&acc)[NMT]) {
   l += __shfl_xor(l, 16);
   l += __shfl_xor(l, 32);
-  return l;
+#pragma unroll
+  for (int mt = 0; mt < NMT; ++mt)
+    if constexpr (F8) acc[mt] *= kProductUnit;
 }
 
 // A lane's share of a row's partial to LDS and from there to another wave's: O, then (m, l).
@@ -788,7 +794,7 @@ __global__ __launch_bounds__(64 * kRowWaves, few_per_cu(D, RT)) void attn_few_ke
 
     // ---- merge the waves, in a fixed order: the upper half deposits, the lower adds ----
 #pragma unroll
-    for (int t = 0; t < RT; ++t) l_run[t] = row_sum(l_run[t]);
+    for (int t = 0; t < RT; ++t) finish_row<F8>(l_run[t], acc[t]);
 #pragma unroll
     for (int half = kRowWaves / 2; half >= 1; half /= 2) {
       __syncthreads();
@@ -931,7 +937,7 @@ __global__ __launch_bounds__(64 * kRowWaves, kManyPerCu) void attn_many_kernel(R
         for (int i = 0; i < NL; ++i) {
           const int k = blk(i), nv = k == 0 ? n0 : k == 1 ? n1 : k == 2 ? n2 : n3;
           vraw[i] = without_odd<F8>(keep_bytes(vraw[i], F8 ? nv : 2 * (nv - (within(i) & 1) * 8)), odd);
-          if constexpr (F8) vx[i] = (lane & 15) < nv ? min(max(vx[i], kLeastExp), kMostExp) : 0;
+          if constexpr (F8) vx[i] = (lane & 15) < nv ? vx[i] : 0;
         }
         if (odd) s_odd[wave] = 1;
       }
@@ -949,7 +955,8 @@ __global__ __launch_bounds__(64 * kRowWaves, kManyPerCu) void attn_many_kernel(R
           uint16_t* vd = sv + w * LDV + k * 16;
           *reinterpret_cast<f16x8*>(vd) = widen_f16(v[0], v[1]);
           *reinterpret_cast<f16x8*>(vd + 8) = widen_f16(v[2], v[3]);
-          if (heads_block(i) && lane < 16) sx[k * 16 + lane] = (uint8_t)(vx[i] + kExpBias);
+          // (0 to 242, whatever a draft that nobody sees holds: its 2^e is finite)
+          if (heads_block(i) && lane < 16) sx[k * 16 + lane] = (uint8_t)max(vx[i] + kExpBias, 0);
         } else {
           *reinterpret_cast<u32x4*>(kd) = kraw[i];
           *reinterpret_cast<u32x4*>(sv + (w >> 1) * LDV + k * 16 + (w & 1) * 8) = v;
@@ -1064,7 +1071,7 @@ __global__ __launch_bounds__(64 * kRowWaves, kManyPerCu) void attn_many_kernel(R
         }
       }
 #pragma unroll
-      for (int t = 0; t < N; ++t) l_run[t] = row_sum(l_run[t]);
+      for (int t = 0; t < N; ++t) finish_row<F8>(l_run[t], acc[t]);
       if constexpr (TS == 2) {  // the second half's waves deposit, the first half's add
         lds_barrier();
         if (half == 1) {

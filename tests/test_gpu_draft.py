@@ -531,6 +531,17 @@ def test_values_of_the_largest_exponents(gpu_lib, heads, exp, kind):
     _check_attn(got, ref, 6001, heads[2], exps=128)
 
 
+@pytest.mark.parametrize("heads", KERNELS)
+@pytest.mark.parametrize("ctx,above", [(100, 16.4), (300, 24.45), (6001, 25.5)])
+def test_small_weights_beside_a_large_one(gpu_lib, heads, ctx, above):
+    """Channels in which the token that takes nearly all of the weight holds 0. An fp16 weight's least step is 2^-24
+    beside a largest weight of 2^7 or more: 2^-32 of the largest p 2^e on a code (`small`), not the 2^-25 above."""
+    c, q, scale = _peak(heads, ctx, above, 0x38, 116)
+    for counts in ([6, 3], [1, 1]):
+        got, (out, mag, size, small) = _tree(c, counts, 0, None, scale=scale, q=q[:sum(counts)])
+        _check_attn(got, (out, mag, size, small * 2.0 ** -7), ctx, heads[2])
+
+
 @pytest.mark.parametrize("f8", [False, True])
 @pytest.mark.parametrize("heads,most", [((8, 8, 64), 1), ((64, 8, 128), 2), ((64, 8, 128), 6), ((32, 4, 64), 16)])
 def test_units_that_share_work_groups(gpu_lib, f8, heads, most):
