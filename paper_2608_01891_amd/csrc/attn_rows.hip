@@ -453,6 +453,11 @@ __device__ __forceinline__ float times_exp2(float x, float d) {
 
 constexpr float kSlack = 8.f;
 
+// Over a bf16 cache weights are 2^-24 where they are largest, up to 2^-16 with the slack: the
+// sum of 2^16 values of any magnitude is a float, as their mean is. (Values below 2^-113 lose
+// bits for that, as the least float is 2^-149.)
+constexpr float kBf16Shift = -24.f;
+
 // Of a value's exponent where it is a byte (15 to 235); what the weights' sum counts u in, and
 // what that takes of the product at the end: 2^(kExpBias - 127) in all.
 constexpr int kExpBias = 115;
@@ -505,7 +510,7 @@ __device__ __forceinline__ void softmax_step(f32x4 (&x)[N][2], u32x2 ve, float s
   }
   float m_use[N];
 #pragma unroll
-  for (int t = 0; t < N; ++t) m_use[t] = m[t] == kNegInf ? 0.f : F8 ? m[t] - 134.f : m[t];
+  for (int t = 0; t < N; ++t) m_use[t] = m[t] == kNegInf ? 0.f : m[t] - (F8 ? 134.f : kBf16Shift);
   float ps[N][2];
 #pragma unroll
   for (int e = 0; e < 8; e += 2) {

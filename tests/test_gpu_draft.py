@@ -542,6 +542,21 @@ def test_small_weights_beside_a_large_one(gpu_lib, heads, ctx, above):
         _check_attn(got, (out, mag, size, small * 2.0 ** -7), ctx, heads[2])
 
 
+@pytest.mark.parametrize("heads,most", [((8, 2, 64), 2), ((16, 2, 128), 6), ((12, 1, 128), 11)])
+@pytest.mark.parametrize("ctx", [100, 6001])
+def test_large_values_over_a_bf16_cache(gpu_lib, heads, most, ctx):
+    """Values of the largest magnitudes: a sum of them with its weights stays within floats where their mean does.
+    (And small ones keep their bits.)"""
+    a = _cache(120, heads, [ctx, 40], False)
+    size = torch.rand(a.v_cache.shape, generator=torch.Generator().manual_seed(121)) * 0.5 + 0.25
+    size[:, :, 1::2] *= -1
+    for exp, scale in ((127, 0.0), (127, 1e-6), (-105, 0.0)):
+        a.v_cache = (size * 2.0 ** exp).bfloat16()
+        got, ref = _tree(a, [most, 1], 122, None, scale=scale)
+        assert bool(got.isfinite().all())
+        _check_attn(got, ref, ctx, heads[2])
+
+
 @pytest.mark.parametrize("f8", [False, True])
 @pytest.mark.parametrize("heads,most", [((8, 8, 64), 1), ((64, 8, 128), 2), ((64, 8, 128), 6), ((32, 4, 64), 16)])
 def test_units_that_share_work_groups(gpu_lib, f8, heads, most):
