@@ -18,7 +18,7 @@
 // as fp16, exactly, and the row's sum is that of p. p = 2^(s - M') with M' the
 // largest s + e, to within 2^kSlack: the largest contribution has a P' of 2^7 to 2^15,
 // and P' is rounded to fp16 (11 bits; below 2^-14 steps of 2^-24). Over a bf16 cache
-// a weight enters as two bf16 values, the rounded weight and what its rounding left:
+// a weight enters as two bf16 values, its leading 8 bits and what they leave:
 // 16 bits. (One bf16 value, 8 bits, would show beside the output's own rounding:
 // 2.1e-3 of the norm instead of 1.65e-3.)
 //
@@ -334,7 +334,9 @@ __device__ __forceinline__ float row_max(float x) {
 }
 
 // The weights of 8 tokens as operands of the second product: fp16 (8-bit cache), or
-// the rounded bf16 and what the rounding left.
+// the leading 8 bits as bf16 and what they leave, rounded to bf16: 2^-16 of the weight is
+// lost at most. (Neither part of a weight is 0 or negative: both times an infinity are
+// that infinity.)
 struct HalfWeights {
   f16x8 w;
   __device__ __forceinline__ void set(int i, float a, float b) {
@@ -350,12 +352,14 @@ struct HalfWeights {
 struct TwoWeights {
   u32x4 hi, lo;
   __device__ __forceinline__ void set(int i, float a, float b) {
-    uint32_t h = __builtin_bit_cast(uint32_t, bf16x2{static_cast<__bf16>(a), static_cast<__bf16>(b)});
-    asm("" : "+v"(h));  // (the rounded values are taken from the pair, not made again one by one)
+    const uint32_t h = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);  // the upper halves
+    uint32_t r = __builtin_bit_cast(uint32_t, bf16x2{static_cast<__bf16>(fmaf(a, kAbove, -__uint_as_float(h << 16))),
+                                                     static_cast<__bf16>(fmaf(b, kAbove, -__uint_as_float(h & 0xffff0000u)))});
+    asm("" : "+v"(r));  // (made here, not beside its product: 4 spilled registers instead of 14)
     hi[i / 2] = h;
-    lo[i / 2] = __builtin_bit_cast(uint32_t, bf16x2{static_cast<__bf16>(a - __uint_as_float(h << 16)),
-                                                    static_cast<__bf16>(b - __uint_as_float(h & 0xffff0000u))});
+    lo[i / 2] = r;
   }
+  static constexpr float kAbove = 1.f + 0x1p-22f;
   static constexpr int kParts = 2;
   __device__ __forceinline__ f32x4 mul(int part, bf16x8 v, f32x4 acc) const {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, __builtin_bit_cast(bf16x8, part ? lo : hi), acc, 0, 0, 0);

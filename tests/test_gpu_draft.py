@@ -557,6 +557,23 @@ def test_large_values_over_a_bf16_cache(gpu_lib, heads, most, ctx):
         _check_attn(got, ref, ctx, heads[2])
 
 
+@pytest.mark.parametrize("heads,most", [((8, 2, 64), 2), ((16, 2, 128), 6), ((12, 1, 128), 11)])
+@pytest.mark.parametrize("ctx", [200, 6001])
+def test_infinities_that_every_row_sees(gpu_lib, heads, most, ctx):
+    """p times an infinity is that infinity, whichever parts p has, as over the cache's other attention calls."""
+    a = _cache(123, heads, [ctx, 40], False)
+    clean, _ = _tree(a, [most, 1], 124, None)
+    inf = float("inf")
+    for place, at in [(3, {5: inf, 6: inf, 7: -inf}), (77, {6: -inf, 8: inf}), (78, {8: inf, 9: float("nan")})]:
+        blk = int(a.block_table[0, place // 16])
+        for d, v in at.items():
+            a.v_cache[blk, :, d, place % 16] = v
+    got, ref = _tree(a, [most, 1], 124, None)
+    assert _same(got.cpu()[:most, :, 5:10], ref[0][:most, :, 5:10])
+    rest = [d for d in range(heads[2]) if not 5 <= d < 10]
+    assert torch.equal(got[:, :, rest], clean[:, :, rest]) and torch.equal(got[most:], clean[most:])
+
+
 @pytest.mark.parametrize("f8", [False, True])
 @pytest.mark.parametrize("heads,most", [((8, 8, 64), 1), ((64, 8, 128), 2), ((64, 8, 128), 6), ((32, 4, 64), 16)])
 def test_units_that_share_work_groups(gpu_lib, f8, heads, most):
