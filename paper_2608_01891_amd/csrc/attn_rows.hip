@@ -17,7 +17,8 @@
 // A value's exponent joins the weight: P' = p 2^e enters the product with the codes
 // as fp16, exactly, and the row's sum is that of p. p = 2^(s - M') with M' the
 // largest s + e, to within 2^kSlack: the largest contribution has a P' of 2^7 to 2^15,
-// and P' is rounded to fp16 (11 bits; below 2^-14 steps of 2^-24). Over a bf16 cache
+// and P' is rounded to fp16 (11 bits; below 2^-14 steps of 2^-24), with up to 16 rows to two
+// of them. Over a bf16 cache
 // a weight enters as two bf16 values, its leading 8 bits and what they leave:
 // 16 bits. (One bf16 value, 8 bits, would show beside the output's own rounding:
 // 2.1e-3 of the norm instead of 1.65e-3.)
@@ -333,10 +334,17 @@ __device__ __forceinline__ float row_max(float x) {
   return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
 }
 
-// The weights of 8 tokens as operands of the second product: fp16 (8-bit cache), or
-// the leading 8 bits as bf16 and what they leave, rounded to bf16: 2^-16 of the weight is
-// lost at most. (Neither part of a weight is 0 or negative: both times an infinity are
-// that infinity.)
+// The weights of 8 tokens as operands of the second product. 8-bit cache: fp16, which
+// loses up to 2^-11 of a weight, or fp16 and what it leaves as fp16, 2^-22. With one row tile
+// the second part costs little, as the call waits for memory: 64 sequences of decode attention
+// 132.9 us with one part, 133.5 with two, one of 400000 tokens 139.7 and 140.4; what
+// the weights add to the output's rounding falls from 8.5e-4 of its norm to 6e-5. With more
+// rows there is one: two take 105.5 us instead of 94.9 for 32 sequences with 8 drafts, 230.6
+// instead of 191.2 for 64 drafts over 65536 tokens, 84.9 instead of 83.8 for 64 sequences with 4,
+// 46.3 instead of 40.5 for 32 with 8 of D = 64, where the output is 1.67e-3 of its norm off in
+// place of 1.66e-3. bf16 cache: the leading 8 bits as bf16 and what they
+// leave, rounded to bf16: 2^-16. (Neither part of a weight is 0 or negative: both times
+// an infinity are that infinity.)
 struct HalfWeights {
   f16x8 w;
   __device__ __forceinline__ void set(int i, float a, float b) {
@@ -346,6 +354,20 @@ struct HalfWeights {
   static constexpr int kParts = 1;
   __device__ __forceinline__ f32x4 mul(int, f16x8 v, f32x4 acc) const {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(v, w, acc, 0, 0, 0);
+  }
+};
+
+struct TwoHalfWeights {
+  f16x8 hi, lo;
+  __device__ __forceinline__ void set(int i, float a, float b) {
+    hi[i] = static_cast<_Float16>(a);
+    hi[i + 1] = static_cast<_Float16>(b);
+    lo[i] = static_cast<_Float16>(a - static_cast<float>(hi[i]));
+    lo[i + 1] = static_cast<_Float16>(b - static_cast<float>(hi[i + 1]));
+  }
+  static constexpr int kParts = 2;
+  __device__ __forceinline__ f32x4 mul(int part, f16x8 v, f32x4 acc) const {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(v, part ? lo : hi, acc, 0, 0, 0);
   }
 };
 
@@ -631,7 +653,7 @@ __global__ __launch_bounds__(64 * kRowWaves, few_per_cu(D, RT)) void attn_few_ke
   constexpr int NK = F8 ? NC : 2 * NC;  // 16-byte loads of a step's keys
   constexpr int LDO = D + 4;       // row of a partial in LDS: O, then (m, l)
   typedef std::conditional_t<F8, u32x2, u32x4> VLoad;  // a lane's 8 tokens of a channel
-  typedef std::conditional_t<F8, HalfWeights, TwoWeights> Weights;
+  typedef std::conditional_t<!F8, TwoWeights, std::conditional_t<RT == 1, TwoHalfWeights, HalfWeights>> Weights;
   typedef std::conditional_t<F8, f16x8, bf16x8> VFrag;
   __shared__ __attribute__((aligned(16))) float so[2 * RT * 16 * LDO];  // partials of two waves
   __shared__ int s_odd[kRowWaves];

@@ -542,6 +542,26 @@ def test_small_weights_beside_a_large_one(gpu_lib, heads, ctx, above):
         _check_attn(got, (out, mag, size, small * 2.0 ** -7), ctx, heads[2])
 
 
+@pytest.mark.parametrize("heads", [(8, 8, 64), (16, 1, 64), (12, 2, 128), (16, 1, 128)])
+def test_weights_of_up_to_16_rows_have_two_parts(gpu_lib, heads):
+    """Opposite values whose weights nearly cancel: with up to 16 rows a kv head a weight is two fp16 values, the second
+    rounded to 2^-11 of at most 2^-11 of it, so the bound of a bf16 cache's two holds (no `small`, w = 2^-16)."""
+    lens = [2, 2, 2, 3, 40, 2]
+    c = _cache(127, heads, lens, True)
+    codes = c.v_cache.view(torch.uint8)
+    codes[..., 1::2] = codes[..., 0::2] ^ 0x80
+    c.kv_exp[:, :, 1] = 0
+    both = min(16 // (heads[0] // heads[1]), 2)  # drafts
+    for counts, most in (([1] * 6, 1), ([1, both] * 3, None)):
+        got, (out, mag, size, small) = _tree(c, counts, 128, None, scale=0.01, max_drafts=most)
+        _check_attn(got, (out, mag, size, torch.zeros_like(small)), 40, heads[2])
+    q = _rand(129, 6, heads[0], heads[2]).bfloat16()
+    got = aflex.attn_decode_f8(_to(c), q.to(DEV), scale=0.01)
+    out, mag, size, small = draft.attention_tree(q, c.k_cache, c.v_cache, c.kv_exp, c.block_table, c.context_lens,
+                                                 list(range(7)), None, 0.01)
+    _check_attn(got, (out, mag, size, torch.zeros_like(small)), 40, heads[2])
+
+
 @pytest.mark.parametrize("heads,most", [((8, 2, 64), 2), ((16, 2, 128), 6), ((12, 1, 128), 11)])
 @pytest.mark.parametrize("ctx", [100, 6001])
 def test_large_values_over_a_bf16_cache(gpu_lib, heads, most, ctx):
