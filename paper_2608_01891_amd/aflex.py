@@ -297,6 +297,16 @@ def _stream(s):
     return s.cuda_stream
 
 
+def _longest(cu_seqlens, stream):
+    """Largest n of a sequence, read behind the work of the stream that the call runs on."""
+    if stream is None:
+        c = cu_seqlens.cpu()
+    else:
+        with torch.cuda.stream(stream):
+            c = cu_seqlens.cpu()
+    return int((c[1:] - c[:-1]).max()) if c.numel() > 1 else 0
+
+
 def _need_gpu(device):
     if torch.device(device).type != "cuda":
         raise ValueError(f"expected tensors on a cuda device, but got: {device}")
@@ -464,8 +474,7 @@ def kv_write(a, k_new, v_new, cu_seqlens, max_seqlen=None, stream=None):
     lib = load()
     T = k_new.shape[0]
     if max_seqlen is None:
-        c = cu_seqlens.cpu()
-        max_seqlen = int((c[1:] - c[:-1]).max()) if c.numel() > 1 else 0
+        max_seqlen = _longest(cu_seqlens, stream)
     args = KvWriteArgs(k_new=_ptr(k_new), v_new=_ptr(v_new), cu_seqlens=_ptr(cu_seqlens),
                        k_cache=_ptr(a.k_cache), v_cache=_ptr(a.v_cache), block_table=_ptr(a.block_table),
                        context_lens=_ptr(a.context_lens), B=a.B, T=T, Hkv=a.Hkv, D=a.D,
@@ -766,8 +775,7 @@ def rope_write(a, q, k_new, v_new, cu_seqlens, rope, max_seqlen=None, interleave
     ``max_seqlen`` bounds the prompts' lengths (None: read from cu_seqlens, which waits for the device)."""
     if max_seqlen is None:
         _need_gpu(q.device)
-        c = cu_seqlens.cpu()
-        max_seqlen = int((c[1:] - c[:-1]).max()) if c.numel() > 1 else 0
+        max_seqlen = _longest(cu_seqlens, stream)
     return _rope(q, "aflex_rope_write", a, q, k_new, v_new, rope, cu_seqlens, max_seqlen, interleaved, positions,
                  summary, q_out, stream)
 
@@ -893,14 +901,9 @@ def rope_write_f8(a, q, k_new, v_new, cu_seqlens, rope, max_seqlen=None, interle
     cu_seqlens, which waits for the device)."""
     if max_seqlen is None:
         _need_gpu(q.device)
-        max_seqlen = _longest(cu_seqlens)
+        max_seqlen = _longest(cu_seqlens, stream)
     return _rope_f8(q, "aflex_rope_write_f8", a, q, k_new, v_new, rope, cu_seqlens, max_seqlen, interleaved, positions,
                     q_out, stream)
-
-
-def _longest(cu_seqlens):
-    c = cu_seqlens.cpu()
-    return int((c[1:] - c[:-1]).max()) if c.numel() > 1 else 0
 
 
 @_on_device
@@ -950,7 +953,7 @@ def attn_tree(a, q, cu_seqlens, masks=None, max_drafts=None, out=None, scale: fl
     sequence (None: read from cu_seqlens, which waits for the device)."""
     if max_drafts is None:
         _need_gpu(q.device)
-        max_drafts = _longest(cu_seqlens)
+        max_drafts = _longest(cu_seqlens, stream)
     return _attn_tree(q, a, q, cu_seqlens, masks, max_drafts, out, scale, stream, ws)
 
 

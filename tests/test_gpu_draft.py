@@ -831,6 +831,27 @@ def test_streams_and_host_threads(gpu_lib):
         assert torch.equal(aflex.attn_decode_f8(c, q[i], ws=ws), ref[i])
 
 
+def test_bounds_are_read_on_the_call_s_stream(gpu_lib):
+    """Without a bound from the caller, the starts are read behind the work of the stream that the call runs on."""
+    heads, counts = (8, 2, 64), [40, 2]
+    for f8 in (False, True):
+        c = _dev(_cache(125, heads, [60, 30], f8))
+        (_, dev), new, side = _tokens(126, 42, heads, False), _i32(_cu(counts)), torch.cuda.Stream()
+        write = aflex.rope_write_f8 if f8 else aflex.rope_write
+        want = [write(c, *dev, new, None, max_seqlen=40), aflex.attn_tree(c, dev[0], new, max_drafts=40)]
+        calls = [lambda cu: write(c, *dev, cu, None, stream=side),
+                 lambda cu: aflex.attn_tree(c, dev[0], cu, stream=side)]
+        for call, ref in zip(calls, want):
+            cu = _i32([0, 1, 2])
+            torch.cuda.synchronize()
+            with torch.cuda.stream(side):
+                torch.cuda._sleep(20_000_000)
+                cu.copy_(new)
+            got = call(cu)
+            torch.cuda.synchronize()
+            assert torch.equal(got, ref)
+
+
 def test_profile_names(gpu_lib):
     c = _to(_cache(103, (8, 2, 64), [100, 90], True))
     (q, k, v), dev = _tokens(104, 2, (8, 2, 64), False)
