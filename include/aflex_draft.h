@@ -170,7 +170,7 @@ typedef struct aflex_cache_accept_args {
   const int32_t *cu_seqlens;   /* [B+1] device, as in aflex_attn_tree_args */
   const int32_t *accepted;     /* [B, max_accepted] drafts, ascending */
   const int32_t *accepted_counts; /* [B] */
-  int32_t *context_out;        /* [B] (written) */
+  int32_t *context_out;        /* [B] (written; overlaps none of the arrays above) */
   int32_t B, Hkv, D;
   int32_t max_accepted;        /* row stride of accepted, in [1, 64] */
   int32_t block_size;          /* must be 16 */

@@ -145,12 +145,20 @@ aflex_status aflex_cache_accept(const aflex_cache_accept_args* a, aflex_stream s
           kMostDrafts);
   REQUIRE(a->B <= 65535 && a->Hkv <= 65535, AFLEX_ERR_UNSUPPORTED, "%s: B (%d) or Hkv (%d) above 65535", who, a->B,
           a->Hkv);
-  REQUIRE(a->context_out != a->context_lens, AFLEX_ERR_INVALID_ARG, "%s: context_out must not be context_lens", who);
   REQUIRE(aligned16(a->k_cache) && aligned16(a->v_cache) && aligned16(a->kv_exp), AFLEX_ERR_ALIGNMENT,
           "%s: pools must be 16-byte aligned", who);
   REQUIRE(aligned4(a->block_table) && aligned4(a->context_lens) && aligned4(a->cu_seqlens) && aligned4(a->accepted) &&
               aligned4(a->accepted_counts) && aligned4(a->context_out),
           AFLEX_ERR_ALIGNMENT, "%s: index arrays must be 4-byte aligned", who);
+  // (each work-group of a sequence reads them, while the first writes context_out)
+  const auto apart = [a](const int32_t* p, long long n) {
+    const uintptr_t x = reinterpret_cast<uintptr_t>(a->context_out), y = reinterpret_cast<uintptr_t>(p);
+    return x + a->B * sizeof(int32_t) <= y || y + n * sizeof(int32_t) <= x;
+  };
+  REQUIRE(apart(a->context_lens, a->B) && apart(a->cu_seqlens, a->B + 1ll) && apart(a->accepted_counts, a->B) &&
+              apart(a->accepted, (long long)a->B * a->max_accepted) &&
+              apart(a->block_table, (long long)a->B * a->max_blocks_per_seq),
+          AFLEX_ERR_INVALID_ARG, "%s: context_out must not overlap the index arrays", who);
   return hip_status(aflex::launch_cache_accept(*a, (hipStream_t)stream), who);
 }
 

@@ -153,6 +153,16 @@ def test_cache_accept_rejects(lib, kw, status):
     assert lib.aflex_last_error().startswith(b"cache_accept")
 
 
+@pytest.mark.parametrize("name,count", [("context_lens", 2), ("cu_seqlens", 3), ("accepted_counts", 2),
+                                        ("accepted", 10), ("block_table", 8)])
+def test_cache_accept_keeps_its_output_apart(lib, name, count):
+    """New lengths in an array that other work-groups of the sequence read, wholly or in part."""
+    out = FAKE + 4096
+    for at in (out, out + 4, out - 4 * (count - 1)):
+        assert lib.aflex_cache_accept(ctypes.byref(_accept(context_out=out, **{name: at})), None) == INVALID
+        assert b"overlap" in lib.aflex_last_error()
+
+
 # ------------------------------------------------------------------ the binding
 def _state():
     a = synth.custom_attention(0, 2, 8, 2, 64, [20, 33], ctx_hi=64)
