@@ -183,6 +183,10 @@ typedef struct aflex_cache_accept_args {
 /* and gets context_out[b] = context_lens[b]; entries whose source or target    */
 /* block id is outside [0, num_blocks) are not copied. A block must not appear  */
 /* twice among the slots written. No workspace.                                 */
+/* Block summaries (aflex_longctx.h) do not follow: blocks that drafts fill have */
+/* none, and those that the move changes have none of their new keys. Behind it, */
+/* aflex_block_summary with the new lengths makes them for the next              */
+/* aflex_block_select.                                                           */
 aflex_status aflex_cache_accept(const aflex_cache_accept_args *a, aflex_stream stream);
 
 /* Kernel names for aflex_profile_start: rope_append_f8, rope_write_f8,        */

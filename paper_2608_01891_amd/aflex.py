@@ -994,5 +994,6 @@ def _cache_accept(dev, a, cu_seqlens, accepted, counts, context_out, stream):
 def cache_accept(a, cu_seqlens, accepted, counts, context_out=None, stream=None):
     """Move the accepted drafts' cache entries of each sequence together, in place: draft accepted[b, i] (int32
     [B, most], ascending, the first counts[b] of them) to place i behind the context before the drafts. Returns the
-    new context lengths [B] (a.context_lens keeps the old ones)."""
+    new context lengths [B] (a.context_lens keeps the old ones). Block summaries of a bf16 cache do not follow: with
+    the new lengths in a.context_lens, block_summary makes them for the next block_select."""
     return _cache_accept(a.k_cache, a, cu_seqlens, accepted, counts, context_out, stream)

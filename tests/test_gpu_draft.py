@@ -775,6 +775,35 @@ def test_prompt_drafts_accept_and_decode(gpu_lib, f8):
             assert bool(((last[b].cpu().double() - want[0][-1]).abs() <= 3 * 2.0 ** -8 * want[1][-1] + 1e-6).all())
 
 
+def test_summaries_after_accepted_drafts(gpu_lib):
+    """Drafts and their move leave no summaries; block_summary over the new lengths makes those of every full block,
+    as the next choice of blocks needs them."""
+    heads = Hq, Hkv, D = 16, 2, 128
+    lens, counts = [45, 30, 100], [6, 20, 9]
+    a = synth.custom_attention(130, 3, *heads, lens, ctx_hi=128)
+    a.block_table = torch.arange(24, dtype=torch.int32).view(3, 8)
+    a.num_blocks = 24
+    a.k_cache, a.v_cache = torch.zeros(24, Hkv, 16, D).bfloat16(), torch.zeros(24, Hkv, D, 16).bfloat16()
+    c, rope = a.to(DEV), aflex.rope_table(128, D).to(DEV)
+    s = aflex.BlockSummary.of(c)
+    (_, dev) = _tokens(131, sum(lens), heads, False)
+    aflex.rope_write(c, *dev, _i32(_cu(lens)), rope, max_seqlen=100, summary=s)
+    c.context_lens = _i32([n + m for n, m in zip(lens, counts)])
+    (_, dev), cu = _tokens(132, sum(counts), heads, False), _i32(_cu(counts))
+    aflex.rope_write(c, *dev, cu, rope, max_seqlen=20)
+    acc = torch.full((3, 20), -1, dtype=torch.int32)
+    for b, path in enumerate([[0, 2, 5], list(range(1, 20)), [0, 1, 2, 3, 4, 5, 6, 7, 8]]):
+        acc[b, :len(path)] = torch.tensor(path)
+    c.context_lens = aflex.cache_accept(c, cu, acc.to(DEV), _i32([3, 19, 9]))
+    assert c.context_lens.tolist() == [48, 49, 109]
+    aflex.block_summary(c, s)
+    zero = aflex.BlockSummary.of(a)
+    keys, exp = lc.block_summary(c.k_cache.cpu(), a.block_table, c.context_lens.cpu(), zero.keys, zero.exp)
+    full = [int(a.block_table[b, j]) for b, n in enumerate((48, 49, 109)) for j in range(n // 16)]
+    assert len(full) == 12
+    assert torch.equal(s.keys.cpu()[full], keys[full]) and torch.equal(s.exp.cpu()[full], exp[full])
+
+
 @pytest.mark.parametrize("f8", [False, True])
 def test_captured_steps_replay(gpu_lib, f8):
     """Two graphs of a step each and eager calls between their replays; each graph has its own workspace."""
