@@ -1326,19 +1326,19 @@ void launch_tiles(const RowsParams& p, const RowsPlan& r, hipStream_t stream) {
     attn_few_kernel<D, true, true, 2><<<grid, block, 0, stream>>>(p);
   else if (r.kind == kFewFour)
     attn_few_kernel<64, true, true, 4><<<grid, block, 0, stream>>>(p);
-  else if (r.kind == kManyTwo)
-    attn_many_kernel<D, F8, 2><<<grid, block, 0, stream>>>(p);
-  else
+  else if (r.kind == kManyFour)
     attn_many_kernel<D, F8, 4><<<grid, block, 0, stream>>>(p);
+  else if constexpr (!(F8 && D == 64))  // (that takes kFewFour in its place)
+    attn_many_kernel<D, F8, 2><<<grid, block, 0, stream>>>(p);
 }
 
 }  // namespace
 
 bool rows_shape_fits(const RowsShape& s) {
+  static_assert(kRowsUnitCost == 16, "the bound as the header states it");
   const int rows = s.max_n * (s.Hq / s.Hkv), most = kTiles * kRowWaves * 16;
-  const long long passes = rows > most ? (rows + most - 1) / most : 1;
-  return (long long)s.B * s.Hkv * passes * ((s.max_ctx + 15) / 16 + 16) < (1ll << 30) &&
-         (long long)s.T * s.Hq < (1ll << 30);
+  const int passes = rows > most ? (rows + most - 1) / most : 1;
+  return positions_bound(s, passes) < (1ll << 30) && (long long)s.T * s.Hq < (1ll << 30);
 }
 
 size_t rows_workspace_bytes(const RowsShape& s) {
