@@ -1256,11 +1256,18 @@ constexpr int kRowsUnitCost = 16;
 // Units take a work-group each, without partials and the merge's launch, where
 // contexts are at most kWholeCtx and one round of work-groups holds all units (4
 // sequences of about 80 tokens, 8 / 2 heads x 64: 6.3 us a call, 9.5 with the even
-// split), and where contexts are at most kWholeManyCtx and the units are at least
-// 3/4 of what the GPU holds at once: dealt out as work-groups end, they balance
-// themselves (256 sequences of median 500 tokens, 64 / 8 heads x 128: 79.6 us, 86.8 with
-// the even split; 128 of median 1000: 64.4 and 66.7; 128 of median 400 with up to 8
-// drafts: 61.7 and 71.4).
+// split), and where contexts are at most kWholeManyCtx and the units fill 3/4 to one
+// round of what the GPU holds at once, or 3/2 rounds and more: dealt out as
+// work-groups end, they balance themselves (256 sequences of median 500 tokens, 64 / 8
+// heads x 128: 79.6 us, 86.8 with the even split; 128 of median 1000: 64.4 and 66.7; 128 of
+// median 400 with up to 8 drafts: 61.7 and 71.4). Between one round and 3/2 the last units run
+// alone. Numbers of rounds, 64 / 8 heads x 128, us with a work-group per unit and with
+// the even split:
+//                             0.75       1          1.02       1.25       1.5        2
+//   one token, 2048 each    44.6 44.2  48.1 50.1  64.1 59.3  66.9 69.0  70.9 79.4  93.3 106
+//   one token, median 1000  33.4 29.2  40.0 36.7  40.7 38.1  44.1 42.6  46.6 49.5  64.7 64.5
+//   8 drafts, 2048 each     68.4 70.6  69.4 76.8   108 93.2   109 107    111 125    139 158
+//   8 drafts, median 1000   59.1 50.8  66.0 64.6  67.0 65.2  83.6 72.7  86.3 83.4   105 107
 constexpr int kWholeCtx = 512;
 constexpr int kWholeManyCtx = 2048;
 constexpr long long kWholeUnits = 1ll << 23;  // (a launch has less than 2^32 threads)
@@ -1305,7 +1312,8 @@ RowsPlan rows_plan(const RowsShape& s) {
   const long long most = (long long)compute_units() * (r.kind == kFewOne ? few_per_cu(s.D, 1) : kManyPerCu);
   const long long units = (long long)s.B * s.Hkv * r.passes;
   r.whole = (s.max_ctx <= kWholeCtx && units <= most) ||
-            (s.max_ctx <= kWholeManyCtx && 4 * units >= 3 * most && units <= kWholeUnits);
+            (s.max_ctx <= kWholeManyCtx && 4 * units >= 3 * most && (units <= most || 2 * units >= 3 * most) &&
+             units <= kWholeUnits);
   const long long P = r.whole ? units : (positions_bound(s, r.passes) + 7) / 8;
   r.grid = (int)(P < 1 ? 1 : P < most || r.whole ? P : most);
   return r;

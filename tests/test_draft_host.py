@@ -136,6 +136,16 @@ def test_workspaces(lib):
     assert 8 * 64 * 64 * 130 * 4 < n.value < 1 << 30
 
 
+@pytest.mark.parametrize("B,whole", [(40, False), (48, True), (64, True), (65, False), (95, False), (96, True), (256, True)])
+def test_units_of_short_contexts_are_cut_where_they_do_not_balance(lib, B, whole):
+    """Up to 2048 tokens units stay whole where they fill 3/4 to one round of work-groups (512 on 256 compute units) or
+    3/2 and more: between those the last ones would run alone. Cut units need room for their partial rows."""
+    n = ctypes.c_size_t()
+    tree = _tree(B=B, T=B * 8, Hq=64, Hkv=8, D=128, max_drafts=8, max_blocks_per_seq=128, max_context_len=2048)
+    assert lib.aflex_attn_tree_workspace(ctypes.byref(tree), ctypes.byref(n)) == aflex.OK
+    assert (n.value < 1 << 20) == whole and (n.value > B * 8 * 64 * 128 * 4) == (not whole)
+
+
 def _accept(**kw):
     return _fill(aflex.CacheAcceptArgs, kw, k_cache=FAKE, v_cache=FAKE, kv_exp=FAKE, block_table=FAKE,
                  context_lens=FAKE, cu_seqlens=FAKE, accepted=FAKE, accepted_counts=FAKE, context_out=FAKE + 64,
