@@ -19,7 +19,7 @@
 // largest s + e, to within 2^kSlack: the largest contribution has a P' of 2^7 to 2^15,
 // and P' is rounded to fp16 (11 bits; below 2^-14 steps of 2^-24), with up to 16 rows to two
 // of them. Over a bf16 cache
-// a weight enters as two bf16 values, its leading 8 bits and what they leave:
+// a weight enters as two bf16 values, the rounded weight and what its rounding left:
 // 16 bits. (One bf16 value, 8 bits, would show beside the output's own rounding:
 // 2.1e-3 of the norm instead of 1.65e-3.)
 //
@@ -240,11 +240,24 @@ __device__ __forceinline__ void clear_empty(const RowsParams& p) {
   }
 }
 
+// What a work-group has to do behind its pieces (add_odd): values that are not finite were
+// taken out of products, or a result over a bf16 cache is not finite.
+constexpr int kOddTaken = 1, kOddResult = 2;
+constexpr uint16_t kNoSum = 0x7fff;  // the NaN of rows whose weights' sum is none (others are made as 0x7fc0)
+
 // A row tile's result (lane: row `row`, channels 16 mt + 4 qg ..) to out, or to the piece's partial.
-template <int D>
+template <int D, bool F8>
 __device__ __forceinline__ void store_rows(const RowsParams& p, const Seq& s, const Piece& c, int row, int qg, float m,
-                                           float l, const f32x4 (&acc)[D / 16]) {
+                                           float l, const f32x4 (&acc)[D / 16], int* odd) {
   if (row >= c.row0 + c.rows) return;
+  if constexpr (!F8) {
+    float zero = 0.f;
+#pragma unroll
+    for (int mt = 0; mt < D / 16; ++mt)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) zero = fmaf(acc[mt][i], 0.f, zero);
+    if (zero != 0.f) *odd |= kOddResult;
+  }
   if (c.first == c.last) {
     const float inv = l > 0.f ? 1.f / l : 0.f;
     uint16_t* o = p.out + row_of(p, s, c.kvh, row) * D + 4 * qg;
@@ -255,6 +268,7 @@ __device__ __forceinline__ void store_rows(const RowsParams& p, const Seq& s, co
       v.y = f2bf(acc[mt][1] * inv);
       v.z = f2bf(acc[mt][2] * inv);
       v.w = f2bf(acc[mt][3] * inv);
+      if (!F8 && l != l) v.x = v.y = v.z = v.w = kNoSum;
       *reinterpret_cast<ushort4*>(o + mt * 16) = v;
     }
   } else {
@@ -342,9 +356,8 @@ __device__ __forceinline__ float row_max(float x) {
 // rows there is one: two take 105.5 us instead of 94.9 for 32 sequences with 8 drafts, 230.6
 // instead of 191.2 for 64 drafts over 65536 tokens, 84.9 instead of 83.8 for 64 sequences with 4,
 // 46.3 instead of 40.5 for 32 with 8 of D = 64, where the output is 1.67e-3 of its norm off in
-// place of 1.66e-3. bf16 cache: the leading 8 bits as bf16 and what they
-// leave, rounded to bf16: 2^-16. (Neither part of a weight is 0 or negative: both times
-// an infinity are that infinity.)
+// place of 1.66e-3. bf16 cache: the rounded bf16 and what the
+// rounding left, 2^-17. (The weight's leading 8 bits and what those leave lose 2^-16.)
 struct HalfWeights {
   f16x8 w;
   __device__ __forceinline__ void set(int i, float a, float b) {
@@ -374,14 +387,12 @@ struct TwoHalfWeights {
 struct TwoWeights {
   u32x4 hi, lo;
   __device__ __forceinline__ void set(int i, float a, float b) {
-    const uint32_t h = __builtin_amdgcn_perm(__float_as_uint(b), __float_as_uint(a), 0x07060302u);  // the upper halves
-    uint32_t r = __builtin_bit_cast(uint32_t, bf16x2{static_cast<__bf16>(fmaf(a, kAbove, -__uint_as_float(h << 16))),
-                                                     static_cast<__bf16>(fmaf(b, kAbove, -__uint_as_float(h & 0xffff0000u)))});
-    asm("" : "+v"(r));  // (made here, not beside its product: 4 spilled registers instead of 14)
+    uint32_t h = __builtin_bit_cast(uint32_t, bf16x2{static_cast<__bf16>(a), static_cast<__bf16>(b)});
+    asm("" : "+v"(h));  // (the rounded values are taken from the pair, not made again one by one)
     hi[i / 2] = h;
-    lo[i / 2] = r;
+    lo[i / 2] = __builtin_bit_cast(uint32_t, bf16x2{static_cast<__bf16>(a - __uint_as_float(h << 16)),
+                                                    static_cast<__bf16>(b - __uint_as_float(h & 0xffff0000u))});
   }
-  static constexpr float kAbove = 1.f + 0x1p-22f;
   static constexpr int kParts = 2;
   __device__ __forceinline__ f32x4 mul(int part, bf16x8 v, f32x4 acc) const {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(v, __builtin_bit_cast(bf16x8, part ? lo : hi), acc, 0, 0, 0);
@@ -406,16 +417,20 @@ __device__ __forceinline__ V without_odd(V v, bool& odd) {
   return v;
 }
 
-// A work-group's pieces once more, if s_odd says so for one of its waves: the values
-// that without_odd took out of the products (of steps of BLOCKS blocks), added to what
-// store_rows has stored of the rows that see them. A pass of its own that reads the
-// kernel's arguments (a RowsParams alone) again, so that the loop of the products need
-// not keep anything for it.
+// A work-group's pieces once more, if s_odd says so for one of its waves. First, where a
+// result over a bf16 cache is not finite: it is the sum of the values that are not, if there
+// are such values in the steps (of BLOCKS blocks) whose products took them. (The second
+// part of a weight is 0 or negative at times, and times an infinity a NaN or one of the other sign.)
+// Then the values that without_odd took out of the other steps' products, added to what is
+// stored of the rows that see them. A pass of its own that reads the kernel's
+// arguments (a RowsParams alone) again, so that the loop of the products need not keep
+// anything for it.
 template <int D, bool F8, int BLOCKS>
 __device__ __forceinline__ void add_odd(int least, const int* s_odd) {
   const int tid = threadIdx.x, lane = tid & 63;
   __syncthreads();  // (and what was stored is there for the others)
-  if (!(s_odd[0] | s_odd[1] | s_odd[2] | s_odd[3])) return;
+  const int odd = s_odd[0] | s_odd[1] | s_odd[2] | s_odd[3];
+  if (!odd) return;
   auto* args = __builtin_amdgcn_kernarg_segment_ptr();
   asm volatile("" : "+s"(args));
   RowsParams p;
@@ -436,28 +451,59 @@ __device__ __forceinline__ void add_odd(int least, const int* s_odd) {
     if (c.j1 <= c.j0) break;
     const int start = s.ctx - s.n;
     const int32_t* table = p.bt + (size_t)b * p.max_blocks;
-    for (int step = c.j0; step < c.j1; step += BLOCKS) {
+    const auto whole_step = [&](int step) {
       bool whole = (step + BLOCKS) * 16 <= start && step + BLOCKS <= c.j1;
       for (int j = step; j < min(step + BLOCKS, c.j1); ++j) whole = whole && (uint32_t)table[j] < (uint32_t)p.num_blocks;
-      if (whole) continue;
+      return whole;
+    };
+    // the sum of the values of channel d in block j that are not finite, of tokens of the set bits
+    const auto odd_sum = [&](int j, int d, uint32_t seen) {
+      const uint8_t* at = p.vc + (((size_t)table[j] * p.Hkv + c.kvh) * D + d) * (F8 ? 16 : 32);
+      bool any = false;
+#pragma unroll
+      for (int i = 0; i < (F8 ? 1 : 2); ++i) without_odd<F8>(reinterpret_cast<const u32x4*>(at)[i], any);
+      float sum = 0.f;
+      for (int k = 0; any && k < 16; ++k) {
+        float v;
+        if constexpr (F8)
+          v = (at[k] & 0x7f) == 0x7f ? __builtin_nanf("") : 0.f;
+        else
+          v = bf2f(reinterpret_cast<const uint16_t*>(at)[k]);
+        sum += (seen >> k & 1u) && !(fabsf(v) < __builtin_inff()) ? v : 0.f;
+      }
+      return sum;
+    };
+    if (!F8 && (odd & kOddResult)) {
+      for (int it = tid; it < c.rows * D; it += 64 * kRowWaves) {
+        const int row = c.row0 + it / D, d = it % D;
+        uint16_t* o = p.out + row_of(p, s, c.kvh, row) * D + d;
+        const size_t part = part_row(p, s, c.kvh, row, blockIdx.x);
+        const bool direct = c.first == c.last;
+        const float have = direct ? bf2f(*o) : p.part_o[part * D + d];
+        if (fabsf(have) < __builtin_inff()) continue;
+        if (direct ? *o == kNoSum : p.part_ml[part * 2 + 1] != p.part_ml[part * 2 + 1]) continue;
+        float sum = 0.f;
+        for (int step = c.j0; step < c.j1; step += BLOCKS) {
+          if (!whole_step(step)) continue;
+          for (int j = step; j < step + BLOCKS; ++j) sum += odd_sum(j, d, 0xffffu);
+        }
+        if (sum == 0.f) continue;
+        if (direct)
+          *o = f2bf(sum);
+        else
+          p.part_o[part * D + d] = sum;
+      }
+    }
+    for (int step = c.j0; step < c.j1; step += BLOCKS) {
+      if (whole_step(step)) continue;
       for (int j = step; j < min(step + BLOCKS, c.j1); ++j) {
-        const int id = table[j], cached = s.ctx - j * 16;
-        if ((uint32_t)id >= (uint32_t)p.num_blocks) continue;
+        const int cached = s.ctx - j * 16;
+        if ((uint32_t)table[j] >= (uint32_t)p.num_blocks) continue;
         for (int it = tid; it < c.rows * D; it += 64 * kRowWaves) {
           const int row = c.row0 + it / D, d = it % D;
           const uint64_t mask = mask_of_row(p, s, row);
-          const uint32_t seen =
-              seen_bits(mask, j * 16, start, cached) | seen_bits(mask, j * 16 + 8, start, cached - 8) << 8;
-          const size_t at = (((size_t)id * p.Hkv + c.kvh) * D + d) * 16;
-          float sum = 0.f;
-          for (int k = 0; k < 16; ++k) {
-            float v;
-            if constexpr (F8)
-              v = (p.vc[at + k] & 0x7f) == 0x7f ? __builtin_nanf("") : 0.f;
-            else
-              v = bf2f(reinterpret_cast<const uint16_t*>(p.vc)[at + k]);
-            sum += (seen >> k & 1u) && !(fabsf(v) < __builtin_inff()) ? v : 0.f;
-          }
+          const float sum = odd_sum(
+              j, d, seen_bits(mask, j * 16, start, cached) | seen_bits(mask, j * 16 + 8, start, cached - 8) << 8);
           if (sum == 0.f) continue;
           if (c.first == c.last) {
             uint16_t* o = p.out + row_of(p, s, c.kvh, row) * D + d;
@@ -798,7 +844,7 @@ __global__ __launch_bounds__(64 * kRowWaves, few_per_cu(D, RT)) void attn_few_ke
           bool odd = false;
 #pragma unroll
           for (int mt = 0; mt < NMT; ++mt) vraw[mt] = without_odd<F8>(vraw[mt], odd);
-          if (odd) s_odd[wave] = 1;
+          if (odd) s_odd[wave] |= kOddTaken;
         }
         if constexpr (F8) vx = keep_bytes(vx, nv_now);
         if constexpr (F8 && DRAFTS) vx = legal_exponents(vx);
@@ -845,7 +891,7 @@ __global__ __launch_bounds__(64 * kRowWaves, few_per_cu(D, RT)) void attn_few_ke
       if (lane == 0 && (int)blockIdx.x == c.first)
         p.span[((size_t)b * p.Hkv + c.kvh) * p.max_passes + c.pass] = make_int2(c.first, c.last);
 #pragma unroll
-      for (int t = 0; t < RT; ++t) store_rows<D>(p, s, c, c.row0 + t * 16 + r, qg, m_run[t], l_run[t], acc[t]);
+      for (int t = 0; t < RT; ++t) store_rows<D, F8>(p, s, c, c.row0 + t * 16 + r, qg, m_run[t], l_run[t], acc[t], s_odd);
     }
   }
   if constexpr (DRAFTS) add_odd<D, F8, 2>(kFewLeast, s_odd);
@@ -970,7 +1016,7 @@ __global__ __launch_bounds__(64 * kRowWaves, kManyPerCu) void attn_many_kernel(R
           vraw[i] = without_odd<F8>(keep_bytes(vraw[i], F8 ? nv : 2 * (nv - (within(i) & 1) * 8)), odd);
           if constexpr (F8) vx[i] = (lane & 15) < nv ? vx[i] : 0;
         }
-        if (odd) s_odd[wave] = 1;
+        if (odd) s_odd[wave] |= kOddTaken;
       }
 #pragma unroll
       for (int i = 0; i < NL; ++i) {
@@ -1120,7 +1166,7 @@ __global__ __launch_bounds__(64 * kRowWaves, kManyPerCu) void attn_many_kernel(R
       if (half == 0) {
 #pragma unroll
         for (int t = 0; t < N; ++t)
-          store_rows<D>(p, s, c, c.row0 + (t0 + t) * 16 + r, qg, m_run[t], l_run[t], acc[t]);
+          store_rows<D, F8>(p, s, c, c.row0 + (t0 + t) * 16 + r, qg, m_run[t], l_run[t], acc[t], s_odd + wave);
       }
     };
     if (mine == 0) run_steps(std::integral_constant<int, 0>{});

@@ -592,6 +592,12 @@ def test_infinities_that_every_row_sees(gpu_lib, heads, most, ctx):
     assert _same(got.cpu()[:most, :, 5:10], ref[0][:most, :, 5:10])
     rest = [d for d in range(heads[2]) if not 5 <= d < 10]
     assert torch.equal(got[:, :, rest], clean[:, :, rest]) and torch.equal(got[most:], clean[most:])
+    # a NaN among one kv head's scores: its rows are NaN, infinite values or not
+    a.k_cache[int(a.block_table[0, 5]), -1, 9, 1] = float("nan")
+    again, _ = _tree(a, [most, 1], 124, None)
+    G = heads[0] // heads[1]
+    assert bool(again[:most, -G:].isnan().all())
+    assert _same(again[:most, :-G].cpu(), got[:most, :-G].cpu()) and torch.equal(again[most:], clean[most:])
 
 
 @pytest.mark.parametrize("f8", [False, True])
