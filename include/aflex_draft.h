@@ -147,7 +147,8 @@ typedef struct aflex_attn_tree_args {
 /* do not exist, and the drafts there are not seen); rows of a sequence beyond */
 /* max_drafts are not written. A context of 0 yields 0. Tokens of block ids    */
 /* outside [0, num_blocks) are masked. The workspace needs no initialisation.  */
-/* The same result on every call with the same inputs (bitwise).               */
+/* The same result on every call with the same inputs (bitwise). Values of a   */
+/* bf16 cache below 2^-113 in magnitude lose bits.                             */
 aflex_status aflex_attn_tree_workspace(const aflex_attn_tree_args *a, size_t *bytes);
 aflex_status aflex_attn_tree(const aflex_attn_tree_args *a, void *workspace, size_t workspace_bytes,
                              aflex_stream stream);

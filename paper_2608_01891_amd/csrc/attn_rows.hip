@@ -36,14 +36,14 @@
 //
 // Bounds, and what was measured (caches that no call has read just before; 8-bit and
 // 64 / 8 heads x 128 but where it says otherwise). Decode attention: the cache's bytes.
-// 64 sequences of median 4096 tokens, 740 MB: 132.4 us, 5.6 TB/s; one of 400000, 826
-// MB: 139.4 us, 5.9 TB/s, where loads alone reach 6.4. Trees: the chain of a step
+// 64 sequences of median 4096 tokens, 740 MB: 133.0 us, 5.6 TB/s; one of 400000, 826
+// MB: 140.4 us, 5.9 TB/s, where loads alone reach 6.4. Trees: the chain of a step
 // (barrier, widening into LDS, barrier, operands, products, softmax, products) with two
-// waves on a SIMD. 32 sequences of median 4096 tokens, up to 8 drafts each, 328 MB: 93
-// us, 3.5 TB/s, the vector units busy for 42% of it, the matrix units 19%, LDS 34%; one
+// waves on a SIMD. 32 sequences of median 4096 tokens, up to 8 drafts each, 328 MB: 94
+// us, 3.5 TB/s, the vector units busy for 43% of it, the matrix units 19%, LDS 34%; one
 // context of 65536 with 64 drafts: 190 us, 0.72 PFLOP/s (a large matrix product reaches
-// 1.41), 53%, 32% and 33%; 8 sequences of median 8192, up to 32 drafts, 32 / 8 heads,
-// bf16, 301 MB: 81 us, 3.7 TB/s.
+// 1.41), 55%, 32% and 33%; 8 sequences of median 8192, up to 32 drafts, 32 / 8 heads,
+// bf16, 301 MB: 82 us, 3.7 TB/s.
 #include <math.h>
 
 #include <atomic>
@@ -350,14 +350,14 @@ __device__ __forceinline__ float row_max(float x) {
 
 // The weights of 8 tokens as operands of the second product. 8-bit cache: fp16, which
 // loses up to 2^-11 of a weight, or fp16 and what it leaves as fp16, 2^-22. With one row tile
-// the second part costs little, as the call waits for memory: 64 sequences of decode attention
-// 132.9 us with one part, 133.5 with two, one of 400000 tokens 139.7 and 140.4; what
-// the weights add to the output's rounding falls from 8.5e-4 of its norm to 6e-5. With more
-// rows there is one: two take 105.5 us instead of 94.9 for 32 sequences with 8 drafts, 230.6
-// instead of 191.2 for 64 drafts over 65536 tokens, 84.9 instead of 83.8 for 64 sequences with 4,
-// 46.3 instead of 40.5 for 32 with 8 of D = 64, where the output is 1.67e-3 of its norm off in
-// place of 1.66e-3. bf16 cache: the rounded bf16 and what the
-// rounding left, 2^-17. (The weight's leading 8 bits and what those leave lose 2^-16.)
+// the second part costs little, as the call waits for memory: 64 sequences of decode
+// attention 132.9 us with one part, 133.5 with two, one of 400000 tokens 139.7 and 140.4. The
+// output's difference from one of 32-bit weights falls from 8.5e-4 of its norm to 6e-5. With
+// more rows there is one part: two take 102.3 us instead of 94.3 for 32 sequences with 8
+// drafts, 223 instead of 190 for 64 drafts over 65536 tokens, 84.5 instead of 83.5 for 64
+// sequences with 4, 43.8 instead of 40.9 for 32 with 8 of D = 64, and the output, whose own
+// rounding is 1.66e-3 of its norm, is 1.67e-3 off with either. bf16 cache: the rounded bf16
+// and what the rounding left, 2^-17. (Its leading 8 bits and what those leave: 2^-16.)
 struct HalfWeights {
   f16x8 w;
   __device__ __forceinline__ void set(int i, float a, float b) {
@@ -1295,8 +1295,8 @@ struct RowsPlan {
 };
 
 // Blocks that a unit's piece is charged for (its queries, merge of waves, partials). 8
-// and 24 instead: 64 sequences of decode attention 134.3 and 133.1 us, now 132.4; 32 with 8
-// drafts 96.4 and 94.1, now 93.5.
+// and 24 instead: 64 sequences of decode attention 134.3 and 133.1 us, with 16 132.4; 32 with 8
+// drafts 96.4 and 94.1, with 16 93.5.
 constexpr int kRowsUnitCost = 16;
 
 // Units take a work-group each, without partials and the merge's launch, where
