@@ -17,11 +17,10 @@
 // A value's exponent joins the weight: P' = p 2^e enters the product with the codes
 // as fp16, exactly, and the row's sum is that of p. p = 2^(s - M') with M' the
 // largest s + e, to within 2^kSlack: the largest contribution has a P' of 2^7 to 2^15,
-// and P' is rounded to fp16 (11 bits; below 2^-14 steps of 2^-24), with up to 16 rows to two
-// of them. Over a bf16 cache
-// a weight enters as two bf16 values, the rounded weight and what its rounding left:
-// 16 bits. (One bf16 value, 8 bits, would show beside the output's own rounding:
-// 2.1e-3 of the norm instead of 1.65e-3.)
+// and P' is rounded to fp16 (11 bits; below 2^-14 steps of 2^-24), with up to 16 rows to
+// two fp16 values. Over a bf16 cache a weight enters as two bf16 values, the rounded
+// weight and what its rounding left: 16 bits. (One bf16 value, 8 bits, would show beside
+// the output's own rounding: 2.1e-3 of the norm instead of 1.65e-3.)
 //
 // Two kernels. Up to 16 rows (decode attention; 8-bit cache: 32, with D = 64 also 64):
 // the waves of a work-group take the tokens in turns, keys and values go from memory
